@@ -287,6 +287,200 @@ int sdp4_read_f32(const float *x, int64_t n, uint32_t *sink, void *stream);
  */
 int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Training-step operators
+ *
+ * The streaming passes of a decoder's training step that stand between its
+ * matrix products and make the gradients sdp4_grad_quant takes: bias +
+ * dropout + residual, norm and rotation of queries and keys, and the log
+ * probabilities of the target tokens, each with its backward pass.
+ *
+ * They keep the conventions above (caller-owned device memory, checked
+ * arguments, one stream, no state) with these differences:
+ *  Arrays     Two-dimensional arrays have unit stride in a row and any stride
+ *             (in elements, >= the width) from row to row; sizes are
+ *             arbitrary.  Element types are SDP4_F32 and SDP4_BF16.
+ *  Alignment  Addresses need only their element's alignment; a workspace
+ *             needs 16 bytes.
+ *  Aliasing   An output may be the input it replaces (the same address,
+ *             element type and strides), or rows of an array whose other
+ *             columns are an input; other overlap is EINVAL.
+ *  Inputs     May be infinite or NaN, with the results stated below.
+ *  Workspace  Scratch memory for one call, of at least the bytes its helper
+ *             names; its contents before and after do not matter.
+ *  Numerics   Arithmetic is float32, rounded once to bfloat16 at the end;
+ *             sums are float32 in a fixed order (results do not depend on
+ *             timing).
+ * ------------------------------------------------------------------------- */
+
+/* Limits. */
+#define SDP4_MAX_TOP 32                      /* alternatives of a row */
+#define SDP4_MAX_VOCAB ((int64_t)1 << 20)    /* logits of a row */
+#define SDP4_MAX_HEAD_DIM 512                /* elements of a head */
+
+/*
+ * Bias, dropout and residual:
+ *      y[r][c] = residual[r][c] + (keep ? (x[r][c] + bias[c]) * s : 0)
+ * keep is drawn for element e = offset + r * ceil8(cols) + c, ceil8 rounding
+ * up to a multiple of 8: its 16-bit uniform h (the generator of
+ * sdp4_grad_quant_sr, h = 65536 u) must be at least T = rint(65536 p), and
+ * s = 65536 / (65536 - T) (all is dropped for T = 65536), so E[y] = residual
+ * + x + bias exactly.  The mask is not stored: the same (seed, offset) draws
+ * it again.  A dropped element contributes 0 whatever it holds.
+ *
+ *   x         [rows][cols] x_dtype, row stride x_stride
+ *   bias      [cols] x_dtype or NULL (no bias)
+ *   residual  [rows][cols] y_dtype or NULL (none), row stride residual_stride
+ *   p         in [0, 1]
+ *   seed      64-bit key; offset: multiple of 8 (EALIGN otherwise).  Calls that
+ *             must not share a mask take ranges [offset, offset + rows * ceil8(cols))
+ *             that do not overlap, or other seeds
+ *   y         [rows][cols] y_dtype out, row stride y_stride; may be x or residual
+ */
+int sdp4_dropout_add(const void *x, int x_dtype, int64_t x_stride, const void *bias, const void *residual,
+                     int64_t residual_stride, int64_t rows, int64_t cols, float p, uint64_t seed, uint64_t offset,
+                     void *y, int y_dtype, int64_t y_stride, void *stream);
+
+/*
+ * Its backward pass: dx[r][c] = keep ? dy[r][c] * s : 0 with the mask drawn
+ * again, and dbias[c] = the float32 sum of dx[r][c] over r before rounding.
+ * (The gradient of the residual is dy itself.)
+ *
+ *   dy     [rows][cols] y_dtype, row stride dy_stride
+ *   dx     [rows][cols] x_dtype out, row stride dx_stride; may be dy
+ *   dbias  [cols] float32 out, or NULL (then no workspace is needed)
+ *   workspace  sdp4_dropout_grad_workspace(rows, cols) bytes
+ */
+int sdp4_dropout_add_grad(const void *dy, int y_dtype, int64_t dy_stride, int64_t rows, int64_t cols, float p,
+                          uint64_t seed, uint64_t offset, void *dx, int x_dtype, int64_t dx_stride, float *dbias,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+int64_t sdp4_dropout_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes out of range */
+
+/*
+ * Log probabilities of given tokens.  For each row x of `vocab` logits:
+ *      lse = log sum_j exp(x_j), logp = x_target - lse,
+ *      entropy = - sum_j p_j log p_j with p_j = exp(x_j - lse),
+ * and its top_k largest logits (ties: the lower index first) as token ids
+ * and log probabilities.  Logits of -inf have probability 0; a row of
+ * nothing else has lse = logp = -inf and entropy 0; a NaN or +inf in a row
+ * makes its lse, logp, entropy and top_logp NaN and its top_ids -1.
+ *
+ *   logits   [rows][vocab] dtype, row stride `stride`; what lies between
+ *            vocab and stride is not read
+ *   vocab    1 .. SDP4_MAX_VOCAB
+ *   targets  [rows] or NULL; a negative target means none (logp = 0), one
+ *            >= vocab is a mistake (logp = NaN)
+ *   logp, lse, entropy   [rows] out, each may be NULL (logp needs targets)
+ *   top_k    0 .. min(vocab, SDP4_MAX_TOP); top_logp, top_ids [rows][top_k] out
+ *   workspace  sdp4_token_logprob_workspace(rows, vocab, top_k) bytes
+ */
+int sdp4_token_logprob(const void *logits, int dtype, int64_t stride, int64_t rows, int64_t vocab,
+                       const int64_t *targets, int top_k, float *logp, float *lse, float *entropy, float *top_logp,
+                       int64_t *top_ids, void *workspace, int64_t workspace_bytes, void *stream);
+int64_t sdp4_token_logprob_workspace(int64_t rows, int64_t vocab, int top_k); /* -1 for sizes out of range */
+
+/*
+ * Gradient of a loss with respect to the logits, from its gradients with
+ * respect to logp, entropy and lse:
+ *      dlogits_j = p_j (g_lse - g_logp - g_entropy (log p_j + entropy))
+ *                  + (j = target ? g_logp : 0).
+ * Columns from vocab to width (a vocabulary padded for the output product)
+ * are set to 0.  A row without a finite logit gets zeros, one whose lse is
+ * NaN gets NaN, and so does one whose target is >= vocab; a negative target
+ * takes no g_logp.
+ *
+ *   logits, dtype, stride, rows, vocab, targets   as for sdp4_token_logprob
+ *   lse, entropy   [rows] as it returned them (entropy only with g_entropy)
+ *   g_logp, g_entropy, g_lse   [rows] or NULL for zero (g_logp needs targets)
+ *   dlogits  [rows][width] dtype out, row stride dlogits_stride; may be logits
+ */
+int sdp4_token_logprob_grad(const void *logits, int dtype, int64_t stride, int64_t rows, int64_t vocab,
+                            const int64_t *targets, const float *lse, const float *entropy, const float *g_logp,
+                            const float *g_entropy, const float *g_lse, void *dlogits, int64_t dlogits_stride,
+                            int64_t width, void *stream);
+
+/*
+ * Both at once for a loss whose gradients by logp, entropy and lse are known
+ * before (a weighted mean of log probabilities: g_logp = -weight): the same
+ * outputs as sdp4_token_logprob with top_k = 0 followed by
+ * sdp4_token_logprob_grad, the logits read once where a row fits one
+ * compute unit's registers (16384 chunks of 16 bytes).
+ *
+ *   logp  [rows] or NULL; lse, entropy [rows] out, not NULL
+ *   workspace  sdp4_token_logprob_workspace(rows, vocab, 0) bytes
+ */
+int sdp4_token_loss(const void *logits, int dtype, int64_t stride, int64_t rows, int64_t vocab,
+                    const int64_t *targets, const float *g_logp, const float *g_entropy, const float *g_lse,
+                    float *logp, float *lse, float *entropy, void *dlogits, int64_t dlogits_stride, int64_t width,
+                    void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Query or key heads of all tokens: element d of head h of token t lies at
+ * data[t * token_stride + h * head_stride + d].  Both strides are at least
+ * head_dim and heads do not overlap: token_stride >= (heads - 1) *
+ * head_stride + head_dim, or the same with tokens and heads exchanged. */
+typedef struct {
+    void *data;
+    int64_t token_stride, head_stride;
+    int heads;
+} sdp4_heads;
+
+/* How heads are normed and rotated, shared by the forward and backward pass. */
+typedef struct {
+    int dtype;               /* of heads and weights */
+    int head_dim;            /* 1 .. SDP4_MAX_HEAD_DIM */
+    int norm;                /* 0: no norm (the weights are NULL) */
+    float eps;               /* >= 0, finite */
+    const void *q_weight;    /* [head_dim], or NULL for ones */
+    const void *k_weight;
+    const float *table;      /* [table_rows][rot_dim]: rot_dim / 2 cosines, then the sines; NULL with rot_dim = 0 */
+    int64_t table_rows;
+    int rot_dim;             /* rotated elements of a head: even, 0 .. head_dim */
+    int interleaved;         /* pairs (2i, 2i+1); 0: pairs (i, i + rot_dim / 2) */
+    const int64_t *positions; /* [tokens] table rows, or NULL for 0, 1, 2, ... */
+} sdp4_qk_params;
+
+/*
+ * RMS norm of each head and rotation by its token's position, in one pass:
+ *      u = x / sqrt(mean(x^2) + eps) * weight,
+ *      pair i of the first rot_dim elements (a, b) -> (a c - b s, b c + a s)
+ * with (c, s) = (table[pos][i], table[pos][rot_dim / 2 + i]); the other
+ * elements are u.  A position outside the table makes the rotated elements
+ * NaN.
+ *
+ *   q, k          inputs; k may be NULL (queries only)
+ *   q_out, k_out  outputs with the same numbers of heads, any strides; each
+ *                 may be its input.  k_out is NULL where k is
+ */
+int sdp4_qk_norm_rope(const sdp4_heads *q, const sdp4_heads *k, const sdp4_qk_params *params, int64_t tokens,
+                      const sdp4_heads *q_out, const sdp4_heads *k_out, void *stream);
+
+/*
+ * Its backward pass: gradients of inputs and weights from those of the
+ * outputs.
+ *
+ *   dq_out, dk_out   gradients of q_out, k_out
+ *   q, k             the inputs (not read, and may be NULL, without norm)
+ *   dq, dk           out, may be dq_out, dk_out
+ *   dq_weight, dk_weight   [head_dim] float32 out, sums over tokens and heads;
+ *                    NULL where not wanted (each needs norm and its weight)
+ *   workspace        sdp4_qk_grad_workspace() bytes, with a weight gradient
+ */
+int sdp4_qk_norm_rope_grad(const sdp4_heads *dq_out, const sdp4_heads *dk_out, const sdp4_heads *q,
+                           const sdp4_heads *k, const sdp4_qk_params *params, int64_t tokens, const sdp4_heads *dq,
+                           const sdp4_heads *dk, float *dq_weight, float *dk_weight, void *workspace,
+                           int64_t workspace_bytes, void *stream);
+int64_t sdp4_qk_grad_workspace(int64_t tokens, int q_heads, int k_heads, int head_dim); /* -1: out of range */
+
+/*
+ * The table of sdp4_qk_norm_rope: row r holds scale * cos and scale * sin of
+ * (start + r) * inv_freq[i] for i < half, computed in float64 and rounded
+ * once.  Frequencies and scale carry any rule for long contexts (stretched
+ * positions, another base, a ramp between both, a factor on queries and keys).
+ *   inv_freq [half] float64; table [rows][2 * half] out
+ */
+int sdp4_rope_table(const double *inv_freq, int half, int64_t start, int64_t rows, double scale, float *table,
+                    void *stream);
+
 /* Pure helpers (no device work). */
 int64_t sdp4_codes_bytes(int64_t n, int bits);  /* n * bits / 8, or -1 if bits not 4 or 8 */
 int64_t sdp4_num_groups(int64_t n, int group); /* n / group, or -1 if not a valid group */

@@ -21,7 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsdp4.so")
 SOURCES = ["k_qwd.hip", "k_grad.hip", "k_sr.hip", "k_reduce.hip", "k_reduce_f32_in8.hip", "k_reduce_f32_in4.hip",
-           "launch.cpp", "abi.cpp"]
+           "launch.cpp", "abi.cpp",
+           *(os.path.join("..", "csrc_step", f) for f in ("k_dropout.hip", "k_logprob.hip", "k_qk.hip", "abi_step.cpp"))]
 BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
@@ -30,7 +31,7 @@ FLAGS = [
     "-ffp-contract=off",                               # every fused multiply-add is written out
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
-    "-I", INCLUDE, "-I", CSRC,
+    "-I", INCLUDE, "-I", CSRC, "-I", os.path.join(PKG, "csrc_step"),
 ]
 
 
@@ -42,7 +43,7 @@ def hipcc() -> str:
 
 
 def _compile(src: str, bdir: str, defines) -> str:
-    obj = os.path.join(bdir, src + ".o")
+    obj = os.path.join(bdir, os.path.basename(src) + ".o")
     cmd = [hipcc(), *FLAGS, *[f"-D{d}" for d in defines], "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -19,6 +19,7 @@
 
 #include <cstdint>
 #include <exception>
+#include <type_traits>
 
 namespace {
 
@@ -31,6 +32,13 @@ struct Entry {
     decltype(&sdp4_grad_quant_sr) grad_quant_sr;
     decltype(&sdp4_dequant_reduce) dequant_reduce;
     decltype(&sdp4_dequant_reduce_sr) dequant_reduce_sr;
+    decltype(&sdp4_dropout_add) dropout_add;
+    decltype(&sdp4_dropout_add_grad) dropout_add_grad;
+    decltype(&sdp4_token_logprob) token_logprob;
+    decltype(&sdp4_token_logprob_grad) token_logprob_grad;
+    decltype(&sdp4_token_loss) token_loss;
+    decltype(&sdp4_qk_norm_rope) qk_norm_rope;
+    decltype(&sdp4_qk_norm_rope_grad) qk_norm_rope_grad;
 } lib; // set once by bind()
 
 // Arguments of one call; `ok` turns false at the first that is not ordinary.
@@ -372,15 +380,357 @@ PyObject *py_chunk_addresses(PyObject *, PyObject *const *v, Py_ssize_t nargs)
     return lists;
 }
 
+// ---------------------------------------------------------------------------
+// training-step operators
+// ---------------------------------------------------------------------------
+// Tensors of these calls: matrices and heads may be strided, the others are contiguous and of one exact shape.
+struct StepArgs : Args {
+    const at::Tensor *device_tensor(PyObject *o)
+    {
+        if (!THPVariable_CheckExact(o)) {
+            ok = false;
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || !t.has_storage()) {
+            ok = false;
+            return nullptr;
+        }
+        return &t;
+    }
+    int element(const at::Tensor &t)
+    {
+        const at::ScalarType s = t.scalar_type();
+        if (s != at::kFloat && s != at::kBFloat16)
+            ok = false;
+        return s == at::kFloat ? SDP4_F32 : SDP4_BF16;
+    }
+    struct Mat {
+        void *p = nullptr;
+        int dtype = 0;
+        int64_t rows = 0, cols = 0, stride = 0;
+    };
+    Mat matrix(PyObject *o)
+    {
+        Mat m;
+        const at::Tensor *t = device_tensor(o);
+        if (!t)
+            return m;
+        if (t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) {
+            ok = false;
+            return m;
+        }
+        m = Mat{t->data_ptr(), element(*t), t->size(0), t->size(1), t->stride(0)};
+        return m;
+    }
+    Mat matrix(PyObject *o, const Mat &like)
+    {
+        const Mat m = matrix(o);
+        if (m.rows != like.rows || m.cols != like.cols)
+            ok = false;
+        return m;
+    }
+    // contiguous tensor of one type and shape, or None
+    void *exact(PyObject *o, at::ScalarType type, int64_t n0, int64_t n1 = -1)
+    {
+        if (o == Py_None)
+            return nullptr;
+        const at::Tensor *t = tensor(o);
+        if (!t)
+            return nullptr;
+        if (t->scalar_type() != type || t->dim() != (n1 < 0 ? 1 : 2) || t->size(0) != n0 || (n1 >= 0 && t->size(1) != n1)) {
+            ok = false;
+            return nullptr;
+        }
+        return t->data_ptr();
+    }
+    template <class T>
+    T *exact_as(PyObject *o, int64_t n0, int64_t n1 = -1)
+    {
+        return static_cast<T *>(exact(o, std::is_same<T, float>::value || std::is_same<T, const float>::value ? at::kFloat : at::kLong, n0, n1));
+    }
+    void *scratch(PyObject *o, int64_t &bytes)
+    {
+        bytes = 0;
+        if (o == Py_None)
+            return nullptr;
+        const at::Tensor *t = tensor(o);
+        if (!t)
+            return nullptr;
+        bytes = (int64_t)t->nbytes();
+        return t->data_ptr();
+    }
+    float real(PyObject *o)
+    {
+        if (!PyFloat_CheckExact(o)) {
+            ok = false;
+            return 0.0f;
+        }
+        return (float)PyFloat_AS_DOUBLE(o);
+    }
+    bool flag(PyObject *o)
+    {
+        if (!PyBool_Check(o))
+            ok = false;
+        return o == Py_True;
+    }
+    // heads [tokens, heads, head_dim]
+    struct Arr {
+        sdp4_heads h{};
+        int64_t tokens = 0, dim = 0;
+        int dtype = 0;
+        const sdp4_heads *get() const { return h.data ? &h : nullptr; }
+    };
+    Arr heads(PyObject *o, const Arr *like = nullptr)
+    {
+        Arr r;
+        const at::Tensor *t = device_tensor(o);
+        if (!t)
+            return r;
+        if (t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1) || t->size(1) > INT32_MAX) {
+            ok = false;
+            return r;
+        }
+        r.h = sdp4_heads{t->data_ptr(), t->stride(0), t->stride(1), (int)t->size(1)};
+        r.tokens = t->size(0), r.dim = t->size(2), r.dtype = element(*t);
+        if (!r.h.data || (like && (r.tokens != like->tokens || r.h.heads != like->h.heads || r.dim != like->dim ||
+                                   r.dtype != like->dtype)))
+            ok = false; // an empty tensor has no address: the general path passes its sizes on
+        return r;
+    }
+};
+
+// Like run(), for the step operators' arguments.
+template <class F>
+PyObject *run_step(bool bound, Py_ssize_t given, Py_ssize_t wanted, F body)
+{
+    if (!bound || given != wanted)
+        Py_RETURN_NONE;
+    int rc = 0;
+    try {
+        StepArgs a;
+        auto call = body(a);
+        if (!a.ok)
+            Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        rc = call();
+        Py_END_ALLOW_THREADS
+    } catch (const std::exception &) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(rc);
+}
+
+// x, bias, residual, p, seed, offset, y, stream
+PyObject *py_dropout_add(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.dropout_add, nargs, 8, [&](StepArgs &a) {
+        const auto x = a.matrix(v[0]), y = a.matrix(v[6], x);
+        auto r = StepArgs::Mat{};
+        if (v[2] != Py_None) {
+            r = a.matrix(v[2], x);
+            if (r.dtype != y.dtype)
+                a.ok = false;
+        }
+        const void *bias = a.exact(v[1], x.dtype == SDP4_F32 ? at::kFloat : at::kBFloat16, x.cols);
+        const float p = a.real(v[3]);
+        const uint64_t seed = a.bits64(v[4]), offset = a.bits64(v[5]);
+        void *stream = a.stream(v[7]);
+        return [=] {
+            return lib.dropout_add(x.p, x.dtype, x.stride, bias, r.p, r.stride, x.rows, x.cols, p, seed, offset, y.p,
+                                   y.dtype, y.stride, stream);
+        };
+    });
+}
+
+// dy, p, seed, offset, dx, dbias, workspace, stream
+PyObject *py_dropout_add_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.dropout_add_grad, nargs, 8, [&](StepArgs &a) {
+        const auto dy = a.matrix(v[0]), dx = a.matrix(v[4], dy);
+        const float p = a.real(v[1]);
+        const uint64_t seed = a.bits64(v[2]), offset = a.bits64(v[3]);
+        float *dbias = a.exact_as<float>(v[5], dy.cols);
+        int64_t bytes;
+        void *work = a.scratch(v[6], bytes), *stream = a.stream(v[7]);
+        return [=] {
+            return lib.dropout_add_grad(dy.p, dy.dtype, dy.stride, dy.rows, dy.cols, p, seed, offset, dx.p, dx.dtype,
+                                        dx.stride, dbias, work, bytes, stream);
+        };
+    });
+}
+
+// The number of columns that count: a number, or None for all.
+int64_t vocab_of(StepArgs &a, PyObject *o, const StepArgs::Mat &logits)
+{
+    return o == Py_None ? logits.cols : a.integer(o, 1, logits.cols);
+}
+
+// logits, targets, top_k, logp, lse, entropy, top_logp, top_ids, workspace, vocab, stream
+PyObject *py_token_logprob(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.token_logprob, nargs, 11, [&](StepArgs &a) {
+        const auto x = a.matrix(v[0]);
+        const int64_t vocab = vocab_of(a, v[9], x);
+        auto targets = a.exact_as<const int64_t>(v[1], x.rows);
+        const int top = (int)a.integer(v[2], 0, SDP4_MAX_TOP);
+        auto logp = a.exact_as<float>(v[3], x.rows), lse = a.exact_as<float>(v[4], x.rows),
+             entropy = a.exact_as<float>(v[5], x.rows);
+        auto top_logp = top ? a.exact_as<float>(v[6], x.rows, top) : nullptr;
+        auto top_ids = top ? a.exact_as<int64_t>(v[7], x.rows, top) : nullptr;
+        if (top && (v[6] == Py_None || v[7] == Py_None))
+            a.ok = false;
+        int64_t bytes;
+        void *work = a.scratch(v[8], bytes), *stream = a.stream(v[10]);
+        return [=] {
+            return lib.token_logprob(x.p, x.dtype, x.stride, x.rows, vocab, targets, top, logp, lse, entropy, top_logp,
+                                     top_ids, work, bytes, stream);
+        };
+    });
+}
+
+struct TokenGradArgs {
+    StepArgs::Mat x, dx;
+    int64_t vocab;
+    const int64_t *targets;
+    const float *g[3];
+    TokenGradArgs(StepArgs &a, PyObject *logits, PyObject *t, PyObject *g0, PyObject *g1, PyObject *g2, PyObject *dlogits,
+                  PyObject *voc)
+    {
+        x = a.matrix(logits), dx = a.matrix(dlogits), vocab = vocab_of(a, voc, x);
+        if (dx.dtype != x.dtype || dx.rows != x.rows || dx.cols < vocab)
+            a.ok = false;
+        targets = a.exact_as<const int64_t>(t, x.rows);
+        PyObject *const gs[3] = {g0, g1, g2};
+        for (int i = 0; i < 3; ++i)
+            g[i] = a.exact_as<const float>(gs[i], x.rows);
+    }
+};
+
+// logits, targets, lse, entropy, g_logp, g_entropy, g_lse, dlogits, vocab, stream
+PyObject *py_token_logprob_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.token_logprob_grad, nargs, 10, [&](StepArgs &a) {
+        const TokenGradArgs s(a, v[0], v[1], v[4], v[5], v[6], v[7], v[8]);
+        auto lse = a.exact_as<const float>(v[2], s.x.rows), entropy = a.exact_as<const float>(v[3], s.x.rows);
+        if (v[2] == Py_None)
+            a.ok = false;
+        void *stream = a.stream(v[9]);
+        return [=] {
+            return lib.token_logprob_grad(s.x.p, s.x.dtype, s.x.stride, s.x.rows, s.vocab, s.targets, lse, entropy,
+                                          s.g[0], s.g[1], s.g[2], s.dx.p, s.dx.stride, s.dx.cols, stream);
+        };
+    });
+}
+
+// logits, targets, g_logp, g_entropy, g_lse, logp, lse, entropy, dlogits, workspace, vocab, stream
+PyObject *py_token_loss(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.token_loss, nargs, 12, [&](StepArgs &a) {
+        const TokenGradArgs s(a, v[0], v[1], v[2], v[3], v[4], v[8], v[10]);
+        auto logp = a.exact_as<float>(v[5], s.x.rows), lse = a.exact_as<float>(v[6], s.x.rows),
+             entropy = a.exact_as<float>(v[7], s.x.rows);
+        if (v[6] == Py_None || v[7] == Py_None)
+            a.ok = false;
+        int64_t bytes;
+        void *work = a.scratch(v[9], bytes), *stream = a.stream(v[11]);
+        return [=] {
+            return lib.token_loss(s.x.p, s.x.dtype, s.x.stride, s.x.rows, s.vocab, s.targets, s.g[0], s.g[1], s.g[2],
+                                  logp, lse, entropy, s.dx.p, s.dx.stride, s.dx.cols, work, bytes, stream);
+        };
+    });
+}
+
+// weights, eps, table, positions, interleaved, for heads like `q`
+sdp4_qk_params qk_params(StepArgs &a, const StepArgs::Arr &q, PyObject *qw, PyObject *kw, PyObject *eps,
+                         PyObject *table, PyObject *positions, PyObject *interleaved)
+{
+    sdp4_qk_params p{};
+    const at::ScalarType type = q.dtype == SDP4_F32 ? at::kFloat : at::kBFloat16;
+    if (q.dim < 1 || q.dim > SDP4_MAX_HEAD_DIM) {
+        a.ok = false;
+        return p;
+    }
+    p.dtype = q.dtype, p.head_dim = (int)q.dim;
+    p.norm = eps != Py_None;
+    p.eps = p.norm ? a.real(eps) : 0.0f;
+    p.q_weight = a.exact(qw, type, q.dim), p.k_weight = a.exact(kw, type, q.dim);
+    if (table != Py_None) {
+        const at::Tensor *t = a.tensor(table);
+        if (!t || t->dim() != 2 || t->scalar_type() != at::kFloat || t->size(1) > q.dim || t->size(1) < 1) {
+            a.ok = false;
+            return p;
+        }
+        p.table = static_cast<const float *>(t->data_ptr()), p.table_rows = t->size(0), p.rot_dim = (int)t->size(1);
+    }
+    p.interleaved = a.flag(interleaved);
+    p.positions = a.exact_as<const int64_t>(positions, q.tokens);
+    return p;
+}
+
+// Keys beside queries: their tokens, head_dim and type.
+bool beside(const StepArgs::Arr &k, const StepArgs::Arr &q)
+{
+    return k.tokens == q.tokens && k.dim == q.dim && k.dtype == q.dtype;
+}
+
+// q, k, q_weight, k_weight, eps, table, positions, q_out, k_out, interleaved, stream
+PyObject *py_qk_norm_rope(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.qk_norm_rope, nargs, 11, [&](StepArgs &a) {
+        const auto q = a.heads(v[0]), qo = a.heads(v[7], &q);
+        StepArgs::Arr k, ko;
+        if (v[1] != Py_None || v[8] != Py_None) {
+            k = a.heads(v[1]), ko = a.heads(v[8], &k);
+            if (!beside(k, q))
+                a.ok = false;
+        }
+        const sdp4_qk_params p = qk_params(a, q, v[2], v[3], v[4], v[5], v[6], v[9]);
+        void *stream = a.stream(v[10]);
+        return [=] { return lib.qk_norm_rope(q.get(), k.get(), &p, q.tokens, qo.get(), ko.get(), stream); };
+    });
+}
+
+// dq_out, dk_out, q, k, q_weight, k_weight, eps, table, positions, dq, dk, dq_weight, dk_weight, workspace,
+// interleaved, stream
+PyObject *py_qk_norm_rope_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.qk_norm_rope_grad, nargs, 16, [&](StepArgs &a) {
+        const bool norm = v[6] != Py_None;
+        const auto gq = a.heads(v[0]), dq = a.heads(v[9], &gq);
+        StepArgs::Arr gk, dk, q, k;
+        if (v[1] != Py_None || v[10] != Py_None) {
+            gk = a.heads(v[1]), dk = a.heads(v[10], &gk);
+            if (!beside(gk, gq))
+                a.ok = false;
+        }
+        if (norm) {
+            q = a.heads(v[2], &gq);
+            if (dk.get())
+                k = a.heads(v[3], &gk);
+        }
+        const sdp4_qk_params p = qk_params(a, gq, v[4], v[5], v[6], v[7], v[8], v[14]);
+        auto dqw = a.exact_as<float>(v[11], gq.dim), dkw = a.exact_as<float>(v[12], gq.dim);
+        int64_t bytes;
+        void *work = a.scratch(v[13], bytes), *stream = a.stream(v[15]);
+        return [=] {
+            return lib.qk_norm_rope_grad(gq.get(), gk.get(), q.get(), k.get(), &p, gq.tokens, dq.get(), dk.get(), dqw,
+                                         dkw, work, bytes, stream);
+        };
+    });
+}
+
 // Addresses of the C entry points, in the order of Entry.
 PyObject *py_bind(PyObject *, PyObject *const *v, Py_ssize_t nargs)
 {
-    void *p[8];
-    if (nargs != 8) {
-        PyErr_SetString(PyExc_TypeError, "bind: eight addresses");
+    constexpr int kEntries = 15;
+    void *p[kEntries];
+    if (nargs != kEntries) {
+        PyErr_SetString(PyExc_TypeError, "bind: one address for each entry point");
         return nullptr;
     }
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kEntries; ++i) {
         p[i] = PyLong_AsVoidPtr(v[i]);
         if (!p[i]) {
             if (!PyErr_Occurred())
@@ -396,6 +746,13 @@ PyObject *py_bind(PyObject *, PyObject *const *v, Py_ssize_t nargs)
     lib.grad_quant_sr = (decltype(lib.grad_quant_sr))p[5];
     lib.dequant_reduce = (decltype(lib.dequant_reduce))p[6];
     lib.dequant_reduce_sr = (decltype(lib.dequant_reduce_sr))p[7];
+    lib.dropout_add = (decltype(lib.dropout_add))p[8];
+    lib.dropout_add_grad = (decltype(lib.dropout_add_grad))p[9];
+    lib.token_logprob = (decltype(lib.token_logprob))p[10];
+    lib.token_logprob_grad = (decltype(lib.token_logprob_grad))p[11];
+    lib.token_loss = (decltype(lib.token_loss))p[12];
+    lib.qk_norm_rope = (decltype(lib.qk_norm_rope))p[13];
+    lib.qk_norm_rope_grad = (decltype(lib.qk_norm_rope_grad))p[14];
     Py_RETURN_NONE;
 }
 
@@ -403,7 +760,9 @@ PyObject *py_bind(PyObject *, PyObject *const *v, Py_ssize_t nargs)
 PyMethodDef methods[] = {
     SDP4_METHOD(bind),          SDP4_METHOD(qwd_encode),      SDP4_METHOD(qwd_decode),     SDP4_METHOD(qwd_encode_sym),
     SDP4_METHOD(qwd_decode_sym), SDP4_METHOD(grad_quant),     SDP4_METHOD(grad_quant_sr),  SDP4_METHOD(dequant_reduce),
-    SDP4_METHOD(dequant_reduce_sr), SDP4_METHOD(chunk_addresses), {nullptr, nullptr, 0, nullptr},
+    SDP4_METHOD(dequant_reduce_sr), SDP4_METHOD(chunk_addresses),
+    SDP4_METHOD(dropout_add),   SDP4_METHOD(dropout_add_grad), SDP4_METHOD(token_logprob), SDP4_METHOD(token_logprob_grad),
+    SDP4_METHOD(token_loss),    SDP4_METHOD(qk_norm_rope),    SDP4_METHOD(qk_norm_rope_grad), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,179 @@
+// step_device.hpp -- device building blocks of the training-step operators.
+//
+// Rows have any stride and any width, so a row may start at an address that
+// is only as aligned as one element.  Global memory serves 16-byte accesses
+// at any element address, and a wave that reads 64 neighbouring chunks
+// touches one cache line more than from an aligned start: rows are read and
+// written in whole 16-byte chunks wherever they begin, and only a row's last
+// chunk, where it is not whole, goes element by element.
+#pragma once
+
+#include "device.hpp"
+#include "step.hpp"
+
+#include <type_traits>
+
+namespace sdp4 {
+
+using bf16_t = uint16_t; // bfloat16 bits
+
+template <class T>
+constexpr int kChunk = 16 / sizeof(T); // elements of a 16-byte chunk
+
+// Work block of the launch.
+SDP4_DEV int64_t work_block() { return (int64_t)blockIdx.y << kGridXLog2 | blockIdx.x; }
+
+// Division by a number known on the host, exact for every dividend: the
+// multiplication by floor((2^64 - 1) / d) is at most one short.
+struct Divisor {
+    uint64_t d, inv;
+    Divisor() = default;
+    explicit Divisor(uint64_t n) : d(n), inv(~uint64_t(0) / n) {}
+};
+SDP4_DEV uint64_t divide(uint64_t n, const Divisor &v, uint64_t &rest)
+{
+    uint64_t q = __umul64hi(n, v.inv);
+    rest = n - q * v.d;
+    if (rest >= v.d) {
+        rest -= v.d;
+        ++q;
+    }
+    return q;
+}
+
+// A value that is the same in all lanes of a wave, on the scalar unit.
+SDP4_DEV uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+SDP4_DEV uint64_t uniform(uint64_t v)
+{
+    return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v);
+}
+
+template <class T>
+SDP4_DEV float to_f32(T v)
+{
+    if constexpr (sizeof(T) == 4)
+        return v;
+    else
+        return __uint_as_float((uint32_t)v << 16);
+}
+
+template <class T>
+SDP4_DEV T from_f32(float v)
+{
+    if constexpr (sizeof(T) == 4)
+        return v;
+    else
+        return (T)(bf16x2_rne(v, 0.0f) & 0xFFFFu);
+}
+
+// Vectors at element addresses.
+typedef u32x4 u32x4_b2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_b4 __attribute__((aligned(4)));
+typedef u32x2 u32x2_b2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_b4 __attribute__((aligned(4)));
+template <class T>
+using chunk_at = std::conditional_t<sizeof(T) == 4, u32x4_b4, u32x4_b2>;
+
+// One chunk, streamed past the caches (NT) or kept in them.
+template <bool NT, class T>
+SDP4_DEV u32x4 load_chunk(const T *p)
+{
+    auto q = reinterpret_cast<const chunk_at<T> *>(p);
+    if constexpr (NT)
+        return __builtin_nontemporal_load(q);
+    else
+        return *q;
+}
+
+template <class T>
+SDP4_DEV void store_chunk(T *p, u32x4 v)
+{
+    __builtin_nontemporal_store((chunk_at<T>)v, reinterpret_cast<chunk_at<T> *>(p));
+}
+
+template <class T>
+SDP4_DEV void unpack(u32x4 c, float (&v)[kChunk<T>])
+{
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            v[j] = __uint_as_float(w[j]);
+        } else {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+    }
+}
+
+template <class T>
+SDP4_DEV u32x4 pack(const float (&v)[kChunk<T>])
+{
+    if constexpr (sizeof(T) == 4)
+        return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else
+        return u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])};
+}
+
+// N elements (a multiple of a chunk, or fewer than one) from element address p, of which `valid`
+// exist; the others read as `fill`.
+template <class T, int N>
+SDP4_DEV void load_elems(const T *p, int64_t valid, float (&v)[N], float fill = 0.0f)
+{
+    if (valid >= N) {
+#pragma unroll
+        for (int k = 0; k < N / kChunk<T>; ++k)
+            unpack<T>(load_chunk<true>(p + k * kChunk<T>), *reinterpret_cast<float(*)[kChunk<T>]>(v + k * kChunk<T>));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] = j < valid ? to_f32<T>(p[j]) : fill;
+    }
+}
+
+template <class T, int N>
+SDP4_DEV void store_elems(T *p, int64_t valid, const float (&v)[N])
+{
+    if (valid >= N) {
+#pragma unroll
+        for (int k = 0; k < N / kChunk<T>; ++k)
+            store_chunk<T>(p + k * kChunk<T>, pack<T>(*reinterpret_cast<const float(*)[kChunk<T>]>(v + k * kChunk<T>)));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < valid)
+                p[j] = from_f32<T>(v[j]);
+    }
+}
+
+// Sum and largest value over an aligned block of `lanes` lanes (a power of
+// two), in every lane of it; always joined in the same order.
+SDP4_DEV float sum_lanes(float v, int lanes)
+{
+    if (lanes > 1) v += dpp_f32<kDppXor1>(v);
+    if (lanes > 2) v += dpp_f32<kDppXor2>(v);
+    if (lanes > 4) v += dpp_f32<kDppHalfMirror>(v);
+    if (lanes > 8) v += dpp_f32<kDppRor8>(v);
+    if (lanes > 16) v += xor_lane<16>(v);
+    if (lanes > 32) v += xor_lane<32>(v);
+    return v;
+}
+
+SDP4_DEV float max_wave(float v)
+{
+    v = fmaxf(v, dpp_f32<kDppXor1>(v));
+    v = fmaxf(v, dpp_f32<kDppXor2>(v));
+    v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+    v = fmaxf(v, dpp_f32<kDppRor8>(v));
+    v = fmaxf(v, xor_lane<16>(v));
+    return fmaxf(v, xor_lane<32>(v));
+}
+
+// Two calls of a body, for the element types.
+template <class F>
+int with_type(int dtype, F body)
+{
+    return dtype == SDP4_BF16 ? body(bf16_t{}) : body(float{});
+}
+
+} // namespace sdp4
