@@ -258,7 +258,7 @@ int sdp4_dropout_add_grad(const void *dy, int y_dtype, int64_t dy_stride, int64_
     if (clash(out, {in}, {sums, work}) || clash(sums, {}, {in, work}) || overlap(work, in))
         return SDP4_EINVAL;
     if (rows == 0) // an empty sum
-        return sdp4::launch_sum_parts(nullptr, 0, 0, cols, dbias, as_stream(stream));
+        return sdp4::launch_sum_parts({{nullptr, 0, dbias}, {}}, cols, cols, as_stream(stream));
     return sdp4::launch_dropout_grad(d, y_dtype, {dy, dy_stride}, x_dtype, {dx, dx_stride}, dbias,
                                      static_cast<float *>(workspace), as_stream(stream));
 }
@@ -429,10 +429,9 @@ int sdp4_qk_norm_rope_grad(const sdp4_heads *dq_out, const sdp4_heads *dk_out, c
     const int dim = params->head_dim;
     const int64_t s = size_of(params->dtype);
     if (tokens == 0) { // empty sums
-        for (float *w : {dq_weight, dk_weight})
-            if (w && (rc = sdp4::launch_sum_parts(nullptr, 0, 0, dim, w, as_stream(stream))))
-                return rc;
-        return SDP4_OK;
+        return dq_weight || dk_weight
+                   ? sdp4::launch_sum_parts({{nullptr, 0, dq_weight}, {nullptr, 0, dk_weight}}, dim, dim, as_stream(stream))
+                   : SDP4_OK;
     }
     const sdp4_heads *gs[2] = {dq_out, dk_out}, *xs[2] = {q, k}, *os[2] = {dq, dk};
     sdp4_heads gh[2]{}, xh[2]{}, oh[2]{};

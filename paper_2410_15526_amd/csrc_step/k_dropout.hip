@@ -13,115 +13,253 @@ namespace sdp4 {
 
 namespace {
 
-// Sets dropped elements to 0 and scales the others.  A select, not a product: what is dropped may be infinite or NaN.
-SDP4_DEV void apply_mask(uint64_t seed, uint64_t block, uint32_t drop, float scale, float (&v)[8])
+// The generator's words for one block of eight elements.
+SDP4_DEV void draw(const Dropout &d, uint64_t block, uint32_t (&c)[4])
 {
-    uint32_t c[4] = {(uint32_t)block, (uint32_t)(block >> 32), 0u, 0u};
-    philox4x32_10(c, (uint32_t)seed, (uint32_t)(seed >> 32));
+    const uint64_t n = d.offset / 8 + block;
+    c[0] = (uint32_t)n, c[1] = (uint32_t)(n >> 32), c[2] = c[3] = 0u;
+    philox4x32_10(c, (uint32_t)d.seed, (uint32_t)(d.seed >> 32));
+}
+
+// Sets dropped elements to 0 and scales the others.  A select, not a product: what is dropped may be infinite or NaN.
+template <int N>
+SDP4_DEV void apply_mask(const uint32_t *words, uint32_t drop, float scale, float (&v)[N])
+{
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        v[2 * w] = (c[w] & 0xFFFFu) >= drop ? v[2 * w] * scale : 0.0f;
-        v[2 * w + 1] = (c[w] >> 16) >= drop ? v[2 * w + 1] * scale : 0.0f;
+    for (int w = 0; w < N / 2; ++w) {
+        v[2 * w] = (words[w] & 0xFFFFu) >= drop ? v[2 * w] * scale : 0.0f;
+        v[2 * w + 1] = (words[w] >> 16) >= drop ? v[2 * w + 1] * scale : 0.0f;
     }
 }
 
-// Eight elements per lane, 256 lanes in a block, rows one after the other.
+// A wave's 64 blocks of eight elements, as its lanes hold them: N elements per access and lane, neighbouring lanes at
+// neighbouring addresses.  bfloat16 rows: a lane's eight elements are one 16-byte access.  With float32 on either side
+// they would be two, 32 bytes apart between lanes: there a lane takes the same half (lane % 2) of blocks lane / 2 and
+// 32 + lane / 2, evaluates the generator for one of them and swaps two words with its neighbour.
+template <bool HALVES>
+struct Lanes {
+    static constexpr int N = HALVES ? 4 : 8, COUNT = HALVES ? 2 : 1;
+    SDP4_DEV static int block(int i) { return HALVES ? 32 * i + lane_id() / 2 : lane_id(); }
+    SDP4_DEV static int start() { return HALVES ? 4 * (lane_id() & 1) : 0; } // first element in the block
+    SDP4_DEV static int mine() { return HALVES ? block(lane_id() & 1) : block(0); } // the block it evaluates
+    // words of the lane's elements in access i, from the number of the block it evaluates
+    SDP4_DEV static void draw(const Dropout &d, uint64_t block, uint32_t (&words)[COUNT][N / 2])
+    {
+        uint32_t c[4];
+        sdp4::draw(d, block, c);
+        if constexpr (HALVES) {
+            const bool odd = lane_id() & 1;
+            const uint32_t a = dpp_u32<kDppXor1>(odd ? c[0] : c[2]), b = dpp_u32<kDppXor1>(odd ? c[1] : c[3]);
+            words[0][0] = odd ? a : c[0], words[0][1] = odd ? b : c[1];
+            words[1][0] = odd ? c[2] : a, words[1][1] = odd ? c[3] : b;
+        } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                words[0][w] = c[w];
+        }
+    }
+};
+
+// 512 elements per wave, four waves in a block, rows one after the other.  A wave whose blocks are all whole and in one
+// row addresses them as a scalar base plus a lane offset; the others find each lane's row.
 template <class In, class Out, bool BIAS, bool RES>
 __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row, int64_t total, Rows<const In *> x,
                                                      const In *bias, Rows<const Out *> res, Rows<Out *> y)
 {
-    const int64_t t = work_block() * 256 + threadIdx.x;
-    if (t >= total)
+    using L = Lanes<sizeof(In) == 4 || sizeof(Out) == 4>;
+    constexpr int N = L::N, C = L::COUNT;
+    const uint64_t first = (uint64_t)work_block() * 256 + uniform(threadIdx.x / kWave) * kWave;
+    if (first >= (uint64_t)total)
         return;
-    uint64_t k;
-    const int64_t r = (int64_t)divide((uint64_t)t, per_row, k);
-    const int64_t c = 8 * (int64_t)k, valid = d.cols - c;
-    float v[8], b[8], a[8];
-    load_elems(x.p + r * x.stride + c, valid, v);
-    if constexpr (BIAS)
-        load_elems(bias + c, valid, b);
-    if constexpr (RES)
-        load_elems(res.p + r * res.stride + c, valid, a);
-    if constexpr (BIAS) {
+    uint64_t k0;
+    const uint64_t r0 = divide(first, per_row, k0);
+    float v[C][N], b[C][N], a[C][N];
+    uint32_t words[C][N / 2];
+    auto finish = [&](int i) {
+        if constexpr (BIAS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] += b[j];
+            for (int j = 0; j < N; ++j)
+                v[i][j] += b[i][j];
+        }
+        if (d.drop)
+            apply_mask(words[i], d.drop, d.scale, v[i]);
+        if constexpr (RES) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[i][j] += a[i][j];
+        }
+    };
+    if ((int64_t)k0 + kWave <= d.cols / 8) {
+        const In *xw = x.p + (int64_t)r0 * x.stride + 8 * k0, *bw = bias + 8 * k0;
+        const Out *rw = res.p + (int64_t)r0 * res.stride + 8 * k0;
+        Out *yw = y.p + (int64_t)r0 * y.stride + 8 * k0;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const uint32_t at = 8 * L::block(i) + L::start();
+            load_whole(xw + at, v[i]);
+            if constexpr (RES)
+                load_whole(rw + at, a[i]);
+            if constexpr (BIAS)
+                load_whole(bw + at, b[i]);
+        }
+        if (d.drop)
+            L::draw(d, first + L::mine(), words);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            finish(i);
+            store_elems(yw + (8 * L::block(i) + L::start()), N, v[i]);
+        }
+        return;
+    }
+    int64_t r[C], c[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        uint64_t t = first + L::block(i), k;
+        t = t < (uint64_t)total ? t : (uint64_t)total - 1;
+        r[i] = (int64_t)divide(t, per_row, k);
+        c[i] = 8 * (int64_t)k + L::start();
+        load_row(x.p + r[i] * x.stride, c[i], d.cols, v[i]);
+        if constexpr (RES)
+            load_row(res.p + r[i] * res.stride, c[i], d.cols, a[i]);
+        if constexpr (BIAS)
+            load_row(bias, c[i], d.cols, b[i]);
     }
     if (d.drop)
-        apply_mask(d.seed, d.offset / 8 + (uint64_t)t, d.drop, d.scale, v);
-    if constexpr (RES) {
+        L::draw(d, first + L::mine(), words);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] += a[j];
+    for (int i = 0; i < C; ++i) {
+        end_row(c[i], d.cols, v[i]);
+        if constexpr (RES)
+            end_row(c[i], d.cols, a[i]);
+        if constexpr (BIAS)
+            end_row(c[i], d.cols, b[i]);
+        finish(i);
+        store_elems(y.p + r[i] * y.stride + c[i], first + L::block(i) < (uint64_t)total ? d.cols - c[i] : 0, v[i]);
     }
-    store_elems(y.p + r * y.stride + c, valid, v);
 }
 
-// Backward with column sums.  A block takes `lx` neighbouring 8-element columns and a range of rows, 256 / lx rows
-// at a time; a lane adds up its eight columns in registers, the block's rows join through LDS, and the sums of the
-// row ranges go to the workspace, from where k_sum_parts adds them in order: no atomics, one result.
+// Backward with column sums.  A block takes 2^lx_log2 neighbouring 8-element columns and a range of rows; a lane adds up its
+// columns in registers, the block's lanes of one column join through LDS, and the sums of the row ranges go to the
+// workspace, from where k_sum_parts adds them in order: no atomics, one result.  The loop has the next rows' loads under
+// way before it stores the present ones: loads that follow stores wait for these.
 template <class In, class Out>
 __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, int64_t per_row, int64_t col_tiles,
                                                       int64_t rows_each, Rows<const In *> dy, Rows<Out *> dx,
                                                       float *parts)
 {
+    constexpr bool H = sizeof(In) == 4 || sizeof(Out) == 4;
+    using L = Lanes<H>;
+    constexpr int N = L::N, C = L::COUNT;
     __shared__ float lds[256 * 8];
     const int lx = 1 << lx_log2, ly = 256 >> lx_log2;
-    const uint32_t tile = (uint32_t)(work_block() % col_tiles);
-    const int64_t part = work_block() / col_tiles;
-    const int tx = threadIdx.x & (lx - 1), ty = threadIdx.x >> lx_log2;
-    const int64_t k = (int64_t)tile * lx + tx, c = 8 * k, valid = d.cols - c;
-    const int64_t end = (part + 1) * rows_each < d.rows ? (part + 1) * rows_each : d.rows;
-    float acc[8] = {};
-    if (k < per_row) {
-        for (int64_t r = part * rows_each + ty; r < end; r += ly) {
-            float v[8];
-            load_elems(dy.p + r * dy.stride + c, valid, v);
-            apply_mask(d.seed, d.offset / 8 + (uint64_t)(r * per_row + k), d.drop, d.scale, v);
+    const int64_t part = work_block() / col_tiles, tile = work_block() - part * col_tiles;
+    const int64_t start = part * rows_each, end = start + rows_each < d.rows ? start + rows_each : d.rows;
+    // the block's 256 (column, row) places, 64 to a wave: place -> column place % lx, row place / lx
+    const int wave = uniform(threadIdx.x / kWave) * kWave;
+    const int64_t col0 = tile * lx;
+    int64_t c[C];       // first element of the lane's columns
+    int64_t r[C];       // its next row
+    bool on[C];
+    float acc[C][N] = {};
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                acc[j] += v[j];
-            store_elems(dx.p + r * dx.stride + c, valid, v);
+    for (int i = 0; i < C; ++i) {
+        const int place = wave + L::block(i), k = place & (lx - 1);
+        on[i] = col0 + k < per_row;
+        c[i] = on[i] ? 8 * (col0 + k) + L::start() : 0;
+        r[i] = start + (place >> lx_log2);
+    }
+    // the generator's block of the lane's first row, and the step from row to row
+    const int drawn = wave + L::mine();
+    uint64_t block = (uint64_t)((start + (drawn >> lx_log2)) * per_row + col0 + (drawn & (lx - 1)));
+    const uint64_t block_step = (uint64_t)(ly * per_row);
+    float next[C][N];
+    auto fetch = [&](int64_t ahead) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int64_t at = r[i] + ahead < end ? r[i] + ahead : end - 1;
+            load_row(dy.p + at * dy.stride, c[i], d.cols, next[i]);
+        }
+    };
+    fetch(0);
+    for (int64_t r0 = start; r0 < end; r0 += ly) {
+        float v[C][N];
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[i][j] = next[i][j];
+        if (r0 + ly < end)
+            fetch(ly);
+        uint32_t words[C][N / 2];
+        if (d.drop)
+            L::draw(d, block, words);
+        block += block_step;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if (r[i] < end && on[i]) {
+                end_row(c[i], d.cols, v[i]);
+                if (d.drop)
+                    apply_mask(words[i], d.drop, d.scale, v[i]);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    acc[i][j] += v[i][j];
+                store_elems(dx.p + r[i] * dx.stride + c[i], d.cols - c[i], v[i]);
+            }
+            r[i] += ly;
         }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        lds[j * 256 + threadIdx.x] = acc[j];
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            lds[(L::start() + j) * 256 + wave + L::block(i)] = acc[i][j];
     __syncthreads();
-    // column j of lane tx: sum over ty, by consecutive threads
     for (int o = threadIdx.x; o < 8 * lx; o += 256) {
         const int j = o & 7, l = o >> 3;
         float sum = 0.0f;
         for (int i = 0; i < ly; ++i)
             sum += lds[j * 256 + (i << lx_log2) + l];
-        const int64_t col = 8 * ((int64_t)tile * lx) + o;
-        if (col < 8 * per_row)
-            parts[part * 8 * per_row + col] = sum;
+        if (8 * col0 + o < 8 * per_row)
+            parts[part * 8 * per_row + 8 * col0 + o] = sum;
     }
 }
 
-// 256 threads: CX columns by 256 / CX slices of the parts.
-template <int CX>
-__global__ __launch_bounds__(256) void k_sum_parts(const float *parts, int64_t nparts, int64_t pitch, int64_t cols,
-                                                   float *out)
+// Sums over parts: a block of 16 waves takes 16 columns, 64 threads share the parts of each.  Few columns and many parts
+// make this a matter of latency: a thread has 16 loads in flight, and one barrier joins the waves.
+constexpr int kSumColumns = 16;
+__global__ __launch_bounds__(1024) void k_sum_parts(Parts first, Parts second, int64_t blocks_each, int64_t pitch, int64_t cols)
 {
-    __shared__ float lds[256];
-    constexpr int SL = 256 / CX;
-    const int64_t c = work_block() * CX + threadIdx.x % CX;
-    const int sl = threadIdx.x / CX;
+    __shared__ float lds[16][kSumColumns];
+    const int64_t wb = work_block();
+    const Parts s = wb < blocks_each ? first : second;
+    if (!s.out)
+        return;
+    const int col = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns;
+    const int64_t c = (wb < blocks_each ? wb : wb - blocks_each) * kSumColumns + col;
     float sum = 0.0f;
     if (c < cols) {
-#pragma unroll 8
-        for (int64_t i = sl; i < nparts; i += SL)
-            sum += parts[i * pitch + c];
+        const float *p = s.p + c;
+        for (int64_t i = share; i < s.count; i += 64 * 16) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                v[j] = p[(i + 64 * j < s.count ? i + 64 * j : i) * pitch];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                sum += i + 64 * j < s.count ? v[j] : 0.0f;
+        }
     }
-    lds[threadIdx.x] = sum;
+    sum += xor_lane<16>(sum);
+    sum += xor_lane<32>(sum);
+    if (lane_id() < kSumColumns)
+        lds[threadIdx.x / kWave][col] = sum;
     __syncthreads();
-    if (sl == 0 && c < cols) {
-        float s = 0.0f;
-        for (int i = 0; i < SL; ++i)
-            s += lds[i * CX + threadIdx.x];
-        out[c] = s;
+    if (threadIdx.x < kSumColumns && c < cols) {
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w)
+            total += lds[w][col];
+        s.out[c] = total;
     }
 }
 
@@ -193,12 +331,13 @@ int launch_dropout_grad(const Dropout &d, int in, Rows<const void *> dy, int out
                              g.col_tiles, g.rows_each, typed<const In>(dy), typed<Out>(dx), workspace);
         });
     });
-    return rc ? rc : launch_sum_parts(workspace, g.parts, 8 * g.per_row, d.cols, dbias, s);
+    return rc ? rc : launch_sum_parts({{workspace, g.parts, dbias}, {}}, 8 * g.per_row, d.cols, s);
 }
 
-int launch_sum_parts(const float *parts, int64_t nparts, int64_t pitch, int64_t cols, float *out, hipStream_t s)
+int launch_sum_parts(const Parts (&parts)[2], int64_t pitch, int64_t cols, hipStream_t s)
 {
-    return launch<4>(k_sum_parts<16>, (cols + 15) / 16, kUncapped, s, parts, nparts, pitch, cols, out);
+    const int64_t each = (cols + kSumColumns - 1) / kSumColumns;
+    return launch<16>(k_sum_parts, parts[1].out ? 2 * each : each, kUncapped, s, parts[0], parts[1], each, pitch, cols);
 }
 
 } // namespace sdp4

@@ -7,10 +7,14 @@
 // A logit of -inf counts nothing; a row of nothing else has lse = logp = -inf
 // and H = 0; a NaN or +inf makes lse, logp and H NaN.
 //
-// Forward: a wave takes a slice of a row into registers (up to 4096 logits),
-// finds its maximum, then S and T, and leaves (m, S, T) and its largest
-// elements in the workspace; a second launch joins the slices of each row,
-// one wave per row.  A row of one slice is finished by its wave.
+// Forward: a wave takes a slice of a row into registers (up to 4096 logits) and leaves S and T, relative to a logit of
+// the slice, in the workspace; a second launch joins the slices of each row, one wave per row.  A row of one slice is
+// finished by its wave.  For the alternatives each lane also leaves the largest of its 64 logits, and the second launch
+// finds from these which few groups of 64 can hold the row's largest and reads only those again.
+//
+// What bounds it: with bfloat16 logits the vector units as much as HBM -- 3.5 T logits a second at the rate of reads
+// leave 11 issue slots for each, of which the exponential alone takes 4.  So the sums run without a pass for the maximum:
+// any logit of the slice serves as the reference, as long as the sum is finite at the end.
 #include "step_device.hpp"
 
 namespace sdp4 {
@@ -20,11 +24,10 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kMaxSlices = 256;  // of a row
 constexpr int kMaxTop = SDP4_MAX_TOP;
-constexpr int kListed = 256;     // candidates a wave lists for the alternatives
 
-// What a slice leaves of its row: S and T relative to m.
+// What a slice leaves of its row: S and T relative to `ref`, and its largest logit.
 struct alignas(16) Slice {
-    float m, S, T, unused;
+    float ref, S, T, top;
 };
 
 // Order of the alternatives as one number: larger values first (-0 and +0 equal), then lower indexes.
@@ -39,7 +42,29 @@ SDP4_DEV float from_order_bits(uint32_t k)
 }
 SDP4_DEV uint64_t entry_of(float v, uint32_t index) { return (uint64_t)order_bits(v) << 32 | (0xFFFFFFFFu - index); }
 SDP4_DEV uint32_t entry_index(uint64_t e) { return 0xFFFFFFFFu - (uint32_t)e; }
-constexpr uint64_t kNoEntry = 0; // below every element
+
+// A lane's largest logit in a slice and the position (of its chunk, in the slice) where it first stands.  Of bfloat16
+// order bits the upper 16 tell everything.
+template <class T>
+struct GroupKey;
+template <>
+struct GroupKey<bf16_t> {
+    using Word = uint32_t;
+    static constexpr int kValueBits = 16;
+    SDP4_DEV static Word make(uint32_t order, uint32_t pos) { return (order & 0xFFFF0000u) | pos; }
+    SDP4_DEV static uint32_t value(Word k) { return k >> 16; }
+    SDP4_DEV static uint32_t pos(Word k) { return k & 0xFFFFu; }
+    SDP4_DEV static uint32_t order(uint32_t value) { return value << 16 | (value & 0x8000u ? 0u : 0xFFFFu); }
+};
+template <>
+struct GroupKey<float> {
+    using Word = uint64_t;
+    static constexpr int kValueBits = 32;
+    SDP4_DEV static Word make(uint32_t order, uint32_t pos) { return (Word)order << 32 | pos; }
+    SDP4_DEV static uint32_t value(Word k) { return (uint32_t)(k >> 32); }
+    SDP4_DEV static uint32_t pos(Word k) { return (uint32_t)k; }
+    SDP4_DEV static uint32_t order(uint32_t value) { return value; }
+};
 
 SDP4_DEV float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
 SDP4_DEV float log2_of(float s) { return __builtin_amdgcn_logf(s); }
@@ -76,323 +101,380 @@ SDP4_DEV void finish_row(const TokenStats &out, int64_t row, int64_t vocab, floa
     }
 }
 
-// Chunks of a wave's slice: chunk i * 64 + lane of `count`, from chunk `first` of the row.  A row's last chunk, where
-// it is not whole, is read from the row's last whole chunk of elements instead and what lies before it masked; all
-// other places that hold nothing read a valid chunk too and are masked, so that no load waits for a test.
+// Largest of a lane's values; NaN counts nothing.
 template <class T, int NC>
-struct SliceRegs {
-    static constexpr int W = kChunk<T>;
-    u32x4 raw[NC];
-    uint32_t lane;
-    int64_t first, count, vocab;
+SDP4_DEV float chunk_max(const u32x4 &raw)
+{
+    float v[kChunk<T>], m;
+    unpack<T>(raw, v);
+    m = v[0];
+#pragma unroll
+    for (int j = 1; j < kChunk<T>; ++j)
+        m = fmaxf(m, v[j]);
+    return m;
+}
 
-    SDP4_DEV int64_t chunk_start(int i) const // element of the row at which the chunk's register begins
-    {
-        int64_t c = (int64_t)i * kWave + lane;
-        c = first + (c < count ? c : count - 1);
-        return c * W + W <= vocab ? c * W : vocab - W;
-    }
-    SDP4_DEV void load(const T *row, int64_t row_vocab, int64_t first_, int64_t count_)
-    {
-        lane = lane_id();
-        first = first_, count = count_, vocab = row_vocab;
-        if (vocab >= W) {
-#pragma unroll
-            for (int i = 0; i < NC; ++i)
-                raw[i] = load_chunk<true>(row + chunk_start(i));
-            const bool ragged = (first + count) * W > vocab;
-#pragma unroll
-            for (int i = 0; i < NC; ++i)
-                if (ragged || (i + 1) * kWave > count)
-                    mask(i);
-        } else { // fewer elements than a chunk
-#pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                float v[W];
-#pragma unroll
-                for (int j = 0; j < W; ++j)
-                    v[j] = i == 0 && lane == 0 && j < vocab ? to_f32<T>(row[j]) : -__builtin_inff();
-                raw[i] = pack<T>(v);
-            }
-        }
-    }
-    SDP4_DEV void mask(int i)
-    {
-        const int64_t c = (int64_t)i * kWave + lane;
-        const int64_t skip = c < count ? (first + c) * W - chunk_start(i) : W; // elements that are not this chunk's
-        float v[W];
-        unpack<T>(raw[i], v);
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            v[j] = j < skip ? -__builtin_inff() : v[j];
-        raw[i] = pack<T>(v);
-    }
-    // element of the row that value j of chunk i is; at least vocab for none
-    SDP4_DEV int64_t index(int i, int j) const
-    {
-        const int64_t c = (int64_t)i * kWave + lane;
-        if (vocab < W)
-            return c == 0 && j < vocab ? j : vocab;
-        if (c >= count)
-            return vocab;
-        const int64_t e = chunk_start(i) + j;
-        return e >= (first + c) * W ? e : vocab;
-    }
-};
-
-// The `k` largest elements of a slice, best first, into list[0..k) (missing ones kNoEntry).
+// S and T of the wave's `rounds` chunks per lane, relative to the `ref` it chooses (uniform over the wave).
 //
-// Every lane's largest element is known (cm: by chunk).  At least k elements are as good as the k-th best of these 64,
-// which a bisection over their bits finds by counting lanes; among lanes that tie there, a second one over the
-// positions of their chunks.  What is as good as that, k elements and few more, is listed in LDS, and each listed
-// element's place is the number of better ones.
+// The quick way (`whole`: every chunk holds logits only) takes the largest of the first round as reference, so that
+// every logit is seen once.  Where that does not do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is
+// not finite or far below the largest (T / S would cancel against log S), a type's lowest value, NaN -- the sums show
+// it, and the wave goes over its registers again with the true maximum and a lower bound on the exponent.
 template <class T, int NC>
-SDP4_DEV void slice_top(const SliceRegs<T, NC> &r, const float (&cm)[NC], float lane_max, int k, uint64_t *lds,
-                        uint32_t *lds_count, uint64_t *list)
+SDP4_DEV void slice_sums(const u32x4 (&raw)[NC], int rounds, bool whole, float &ref, float &S, float &T2)
 {
     constexpr int W = kChunk<T>;
-    const uint32_t lane = r.lane;
-    const uint32_t key = order_bits(lane_max);
-    uint32_t tau = 0;
-    constexpr int kLowest = sizeof(T) == 2 ? 16 : 0; // bfloat16 values differ in their upper bits only
-    const uint32_t probe = key >> kLowest;
-#pragma unroll 1
-    for (int b = 31 - kLowest; b >= 0; --b) {
-        const uint32_t mid = tau | (1u << b);
-        if (__builtin_popcountll(__ballot(probe >= mid)) >= k)
-            tau = mid;
-    }
-    // lanes whose largest is tau, in the order of its first chunk
-    const uint64_t ties = __ballot(probe == tau);
-    const int above = __builtin_popcountll(__ballot(probe > tau));
-    uint32_t last = ~0u; // position of the last chunk from which elements equal to tau are needed
-    const float tau_value = from_order_bits(kLowest ? (tau << 16) | (tau & 0x8000u ? 0u : 0xFFFFu) : tau);
-    if (above + __builtin_popcountll(ties) > k) {
-        uint32_t pos = ~0u;
-#pragma unroll
-        for (int i = NC - 1; i >= 0; --i)
-            if (probe == tau && cm[i] == lane_max)
-                pos = (uint32_t)i * kWave + lane;
-        last = 0;
-#pragma unroll 1
-        for (int b = 31 - __builtin_clz(NC * kWave); b >= 0; --b) { // the smallest position with enough at or before it
-            const uint32_t mid = last + (1u << b) - 1;
-            if (above + __builtin_popcountll(__ballot(pos <= mid)) < k)
-                last = mid + 1;
-        }
-    }
-    if (lane == 0)
-        *lds_count = 0;
-    wave_lds_sync();
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        if (!__ballot(cm[i] >= tau_value))
-            continue;
-        float v[W];
-        unpack<T>(r.raw[i], v);
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            if (v[j] > tau_value || (v[j] == tau_value && (uint32_t)i * kWave + lane <= last)) {
-                const int64_t e = r.index(i, j);
-                if (e < r.vocab) {
-                    const uint32_t slot = atomicAdd(lds_count, 1u);
-                    if (slot < kListed)
-                        lds[slot] = entry_of(v[j], (uint32_t)e);
-                }
-            }
-        }
-    }
-    wave_lds_sync();
-    const int listed = (int)uniform(*lds_count);
-    if (listed <= kListed) {
-        for (int a = (int)lane; a < (listed > k ? listed : k); a += kWave) {
-            const uint64_t mine = a < listed ? lds[a] : kNoEntry;
-            int rank = a < listed ? 0 : a;
-            if (a < listed)
-                for (int o = 0; o < listed; ++o)
-                    rank += lds[o] > mine;
-            if (rank < k)
-                list[rank] = mine;
-        }
-    } else {
-        // More than the list holds (a few lanes with most of the largest elements): best of the rest, k times.
-        uint64_t before = ~uint64_t(0);
-#pragma unroll 1
-        for (int a = 0; a < k; ++a) {
-            uint64_t best = kNoEntry;
-#pragma unroll 1
-            for (int i = 0; i < NC; ++i) {
-                float v[W];
-                u32x4 c = r.raw[0];
-#pragma unroll
-                for (int q = 1; q < NC; ++q)
-                    c = i == q ? r.raw[q] : c;
-                unpack<T>(c, v);
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const int64_t e = r.index(i, j);
-                    const uint64_t x = e < r.vocab ? entry_of(v[j], (uint32_t)e) : kNoEntry;
-                    best = x < before && x > best ? x : best;
-                }
-            }
-            for (int o = 1; o < kWave; o <<= 1) {
-                const uint64_t other = __shfl_xor(best, o);
-                best = other > best ? other : best;
-            }
-            if (lane == 0)
-                list[a] = best;
-            before = best;
-        }
-    }
-    wave_lds_sync();
-}
-
-// S: 0 for a row without a finite logit, NaN for one with a NaN or +inf.
-SDP4_DEV void write_top(const TokenStats &out, int64_t row, int i, uint64_t e, float m, float S)
-{
-    const bool bad = !(S - S == 0.0f);
-    const float v = S == 0.0f ? -__builtin_inff() : (from_order_bits((uint32_t)(e >> 32)) - m) - kLn2 * log2_of(S);
-    out.top_logp[row * out.top_k + i] = bad ? __builtin_nanf("") : v;
-    out.top_ids[row * out.top_k + i] = bad ? -1 : (int64_t)entry_index(e);
-}
-
-// One slice per wave, four waves in a block.
-template <class T, int NC, bool TOP>
-__global__ __launch_bounds__(256) void k_logprob_slices(Rows<const T *> x, int64_t rows, int64_t vocab,
-                                                        Divisor slices, int64_t chunks_each, TokenStats out,
-                                                        Slice *stats, uint64_t *lists)
-{
-    constexpr int W = kChunk<T>;
-    __shared__ uint64_t lds[TOP ? 4 * kListed : 1];
-    __shared__ uint64_t direct[TOP ? 4 * kMaxTop : 1];
-    __shared__ uint32_t lds_count[4];
-    const uint32_t wave = uniform(threadIdx.x / kWave);
-    const uint64_t w = (uint64_t)work_block() * 4 + wave;
-    uint64_t slice;
-    const int64_t row = (int64_t)divide(w, slices, slice);
-    if (row >= rows)
-        return;
-    const T *p = x.p + row * x.stride;
-    const int64_t chunks = (vocab + W - 1) / W, first = (int64_t)slice * chunks_each;
-    const int64_t count = chunks - first < chunks_each ? chunks - first : chunks_each;
-    SliceRegs<T, NC> r;
-    r.load(p, vocab, first, count);
-
-    float cm[NC], m = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        float v[W];
-        unpack<T>(r.raw[i], v);
-        cm[i] = v[0];
-#pragma unroll
-        for (int j = 1; j < W; ++j)
-            cm[i] = fmaxf(cm[i], v[j]);
-        m = fmaxf(m, cm[i]);
-    }
-    const float lane_max = m;
-    m = max_wave(m);
-    float S = 0.0f, T2 = 0.0f;
-    const float ref = m == -__builtin_inff() ? 0.0f : m;
-    with_exponent(ref, 0.0f, [&](auto exponent, float delta) {
+    if (whole) {
+        ref = max_wave(chunk_max<T, NC>(raw[0]));
+        const float c = ref * kLog2e;
+        S = T2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            float v[W];
-            unpack<T>(r.raw[i], v);
+            if (i < rounds) {
+                float v[W];
+                unpack<T>(raw[i], v);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float t = exponent(v[j]), e = exp2_of(t);
-                S += e;
-                T2 = __builtin_fmaf(e, fmaxf(t, -1000.0f), T2); // 2^-1000 is 0: -inf counts nothing
+                for (int j = 0; j < W; ++j) {
+                    const float t = __builtin_fmaf(v[j], kLog2e, -c), e = exp2_of(t);
+                    S += e;
+                    T2 = __builtin_fmaf(e, t, T2);
+                }
             }
         }
         S = sum_lanes(S, kWave);
         T2 = sum_lanes(T2, kWave);
-        const float f = exp2_of(-delta);
+        const float delta = __builtin_fmaf(ref, kLog2e, -c), f = exp2_of(-delta); // the rounding of c, taken out
         T2 = f * __builtin_fmaf(-delta, S, T2);
         S *= f;
-    });
-
-    const bool whole_row = slices.d == 1;
-    if constexpr (TOP) {
-        uint64_t *list = whole_row ? direct + wave * kMaxTop : lists + (int64_t)w * out.top_k;
-        slice_top<T, NC>(r, cm, lane_max, out.top_k, lds + wave * kListed, lds_count + wave, list);
-        if (whole_row && (int)r.lane < out.top_k)
-            write_top(out, row, r.lane, list[r.lane], m, S);
+        if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < 1e38f)))
+            return;
     }
-    if (r.lane == 0) {
-        if (whole_row) {
-            const int64_t target = out.targets ? out.targets[row] : -1;
-            finish_row(out, row, vocab, m, S, T2, target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f, target);
-        } else {
-            stats[w] = Slice{m, S, T2, 0.0f};
-        }
-    }
-}
-
-// Joins the slices of a row: one wave each.
-template <class T>
-__global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
-                                                      TokenStats out, const Slice *stats, const uint64_t *lists)
-{
-    const uint32_t lane = lane_id();
-    const int64_t row = work_block() * 4 + uniform(threadIdx.x / kWave);
-    if (row >= rows)
-        return;
-    const int64_t target = out.targets ? out.targets[row] : -1;
-    const float tx = target >= 0 && target < vocab ? to_f32<T>(x.p[row * x.stride + target]) : 0.0f;
-    constexpr int N = kMaxSlices / kWave;
-    Slice s[N];
-    uint64_t head[N];
-    int at[N];
-    const uint64_t *mine = lists + row * slices * (int64_t)out.top_k;
     float m = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int sl = i * kWave + (int)lane;
-        s[i] = Slice{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
-        head[i] = kNoEntry;
-        at[i] = 0;
-        if (sl < slices) {
-            s[i] = stats[row * slices + sl];
-            if (out.top_k)
-                head[i] = mine[(int64_t)sl * out.top_k];
-        }
-        m = fmaxf(m, s[i].m);
-    }
+    for (int i = 0; i < NC; ++i)
+        if (i < rounds)
+            m = fmaxf(m, chunk_max<T, NC>(raw[i]));
     m = max_wave(m);
-    float S = 0.0f, T2 = 0.0f;
+    ref = m == -__builtin_inff() ? 0.0f : m;
+    S = T2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        if (i < rounds) {
+            float v[W];
+            unpack<T>(raw[i], v);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const float t = (v[j] - ref) * kLog2e, e = exp2_of(t);
+                S += e;
+                T2 = __builtin_fmaf(e, fmaxf(t, -1000.0f), T2); // 2^-1000 is 0
+            }
+        }
+    }
+    S = sum_lanes(S, kWave);
+    T2 = sum_lanes(T2, kWave);
+}
+
+// Joins N sums that a lane holds with those of the other lanes: relative to the largest reference of those that count.
+template <int N>
+SDP4_DEV void join_sums(const Slice (&s)[N], float &ref, float &S, float &T2)
+{
+    ref = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (s[i].S != 0.0f) // a slice without a finite logit counts nothing
+            ref = fmaxf(ref, s[i].ref);
+    ref = max_wave(ref);
+    S = T2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (s[i].S != 0.0f) { // a slice without a finite logit counts nothing
-            const float d = (s[i].m - m) * kLog2e, f = exp2_of(d);
+        if (s[i].S != 0.0f) {
+            const float d = (s[i].ref - ref) * kLog2e, f = exp2_of(d);
             S += s[i].S * f;
             T2 += f * (f == 0.0f ? 0.0f : __builtin_fmaf(s[i].S, d, s[i].T));
         }
     }
     S = sum_lanes(S, kWave);
     T2 = sum_lanes(T2, kWave);
-    if (lane == 0)
-        finish_row(out, row, vocab, m, S, T2, tx, target);
-    if (out.top_k) {
-#pragma unroll 1
-        for (int a = 0; a < out.top_k; ++a) {
-            uint64_t best = head[0];
+}
+
+// One slice per wave, four waves in a block: round i of a wave is 64 neighbouring chunks.
+template <class T, int NC, bool TOP>
+__global__ __launch_bounds__(256) void k_logprob_slices(Rows<const T *> x, int64_t rows, int64_t vocab,
+                                                        Divisor slices, TokenStats out, Slice *stats,
+                                                        typename GroupKey<T>::Word *keys)
+{
+    constexpr int W = kChunk<T>;
+    const uint32_t wave = uniform(threadIdx.x / kWave), lane = lane_id();
+    const uint64_t w = (uint64_t)work_block() * 4 + wave;
+    uint64_t slice;
+    const int64_t row = (int64_t)divide(w, slices, slice);
+    if (row >= rows)
+        return;
+    const T *p = x.p + row * x.stride;
+    const int64_t first = (int64_t)slice * (NC * kWave * W); // element of the row
+    const int left = (int)(vocab - first < NC * kWave * W ? vocab - first : NC * kWave * W);
+    const int rounds = (left + kWave * W - 1) / (kWave * W);
+    const bool whole = left == NC * kWave * W;
+    u32x4 raw[NC];
+    if (whole) {
 #pragma unroll
-            for (int i = 1; i < N; ++i)
-                best = head[i] > best ? head[i] : best;
-            for (int o = 1; o < kWave; o <<= 1) {
-                const uint64_t other = __shfl_xor(best, o);
-                best = other > best ? other : best;
+        for (int i = 0; i < NC; ++i)
+            raw[i] = load_chunk<true>(p + first + (uint32_t)((i * kWave + lane) * W));
+    } else {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            if (i < rounds) {
+                float v[W];
+                const int64_t e = first + (i * kWave + (int)lane) * W;
+                load_row(p, e < vocab ? e : 0, vocab, v);
+                end_row(e, vocab, v, -__builtin_inff());
+                raw[i] = pack<T>(v);
             }
-            if (lane == 0)
-                write_top(out, row, a, best, m, S);
+        }
+    }
+    float ref, S, T2;
+    slice_sums<T, NC>(raw, rounds, whole, ref, S, T2);
+
+    float top = -__builtin_inff();
+    if constexpr (TOP) {
+        float cm[NC];
 #pragma unroll
-            for (int i = 0; i < N; ++i) { // entries differ: one lane moves on
-                if (head[i] == best && best != kNoEntry) {
-                    ++at[i];
-                    head[i] = at[i] < out.top_k ? mine[(int64_t)(i * kWave + (int)lane) * out.top_k + at[i]] : kNoEntry;
+        for (int i = 0; i < NC; ++i) {
+            cm[i] = i < rounds ? chunk_max<T, NC>(raw[i]) : -__builtin_inff();
+            top = fmaxf(top, cm[i]);
+        }
+        uint32_t pos = lane;
+#pragma unroll
+        for (int i = NC - 1; i >= 0; --i)
+            if (cm[i] == top)
+                pos = (uint32_t)i * kWave + lane;
+        keys[w * kWave + lane] = GroupKey<T>::make(order_bits(top), pos);
+        top = max_wave(top);
+    }
+    if (lane == 0) {
+        if (!TOP && slices.d == 1) {
+            const int64_t target = out.targets ? out.targets[row] : -1;
+            finish_row(out, row, vocab, ref, S, T2, target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f, target);
+        } else {
+            stats[w] = Slice{ref, S, T2, top};
+        }
+    }
+}
+
+// The statistics of a row's slices, joined.  Returns the largest of each of the lane's slices.
+template <class T, int N>
+SDP4_DEV void join_row(const Rows<const T *> &x, int64_t row, int64_t vocab, int slices, const TokenStats &out,
+                       const Slice *stats, float &ref, float &S, uint32_t (&tops)[N])
+{
+    const int lane = lane_id();
+    const int64_t target = out.targets ? out.targets[row] : -1;
+    const float tx = target >= 0 && target < vocab ? to_f32<T>(x.p[row * x.stride + target]) : 0.0f;
+    Slice s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        s[i] = Slice{0.0f, 0.0f, 0.0f, 0.0f};
+        if (i * kWave + lane < slices)
+            s[i] = stats[row * slices + i * kWave + lane];
+        tops[i] = i * kWave + lane < slices ? order_bits(s[i].top) : 0u;
+    }
+    float T2;
+    join_sums<N>(s, ref, S, T2);
+    if (lane == 0)
+        finish_row(out, row, vocab, ref, S, T2, tx, target);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
+                                                      TokenStats out, const Slice *stats)
+{
+    const int64_t row = work_block() * 4 + uniform(threadIdx.x / kWave);
+    if (row >= rows)
+        return;
+    float ref, S;
+    uint32_t tops[kMaxSlices / kWave];
+    join_row<T>(x, row, vocab, slices, out, stats, ref, S, tops);
+}
+
+// The largest v with at least k of the lanes' N values >= v; unless EXACT, the first v on the way with exactly k of them.
+template <int BITS, bool EXACT, int N>
+SDP4_DEV uint32_t kth_largest(const uint32_t (&value)[N], int used, int k)
+{
+    uint32_t v = 0;
+#pragma unroll 1
+    for (int b = BITS - 1; b >= 0; --b) {
+        const uint32_t mid = v | 1u << b;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < used)
+                n += __builtin_popcountll(__ballot(value[i] >= mid));
+        if (n >= k)
+            v = mid;
+        if (!EXACT && n == k)
+            break;
+    }
+    return v;
+}
+
+// Joins the slices and finds the alternatives: one wave per row and block, up to K alternatives.
+//
+// Call a lane's logits of one slice a group.  The row's k largest logits lie in the k groups with the best largest logit
+// (larger first, then earlier): each of these has one that is at least as good as any logit outside of them.  The same
+// holds one step up, for the k slices with the best largest logit, where there are so many.  A bisection over the bits
+// of the values, counting lanes, finds the k-th best slice (or group, with fewer slices); the groups from there up, k
+// and a few more, are listed in LDS, and a group's place is the number of better ones.  Of the k best groups' logits
+// (read again, k * NC chunks) those at least as good as the last one's largest are ranked in the same way.
+template <class T, int NC, int K>
+__global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
+                                                         TokenStats out, const Slice *stats,
+                                                         const typename GroupKey<T>::Word *keys)
+{
+    using Key = GroupKey<T>;
+    constexpr int W = kChunk<T>, N = kMaxSlices / kWave, VB = Key::kValueBits;
+    __shared__ uint16_t chosen[K];         // slices
+    __shared__ uint32_t groups[K];         // slice << 6 | lane of the k best
+    __shared__ uint64_t list[K * kWave];   // groups, or logits of k groups
+    __shared__ uint16_t where[K * kWave];  // of listed groups: place in `chosen` << 6 | lane
+    __shared__ uint32_t listed;
+    static_assert(NC * W <= kWave, "logits of a group");
+    const int lane = lane_id(), k = out.top_k;
+    const int64_t row = work_block();
+    if (row >= rows)
+        return;
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    if (lane == 0)
+        listed = 0;
+    float ref, S;
+    uint32_t tops[N];
+    join_row<T>(x, row, vocab, slices, out, stats, ref, S, tops);
+
+    // slices whose groups count, in order
+    int count = slices;
+    uint32_t tau = 0; // groups below it do not count
+    if (slices >= k) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            tops[i] >>= 32 - VB;
+        tau = kth_largest<VB, true>(tops, (slices + kWave - 1) / kWave, k);
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            above += __builtin_popcountll(__ballot(tops[i] > tau));
+        int equal = k - above; // of those at tau the first so many
+        count = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool tie = tops[i] == tau && i * kWave + lane < slices;
+            const uint64_t eq = __ballot(tie);
+            const bool take = tops[i] > tau || (tie && __builtin_popcountll(eq & below) < equal);
+            equal -= __builtin_popcountll(eq);
+            const uint64_t all = __ballot(take);
+            if (take)
+                chosen[count + __builtin_popcountll(all & below)] = (uint16_t)(i * kWave + lane);
+            count += __builtin_popcountll(all);
+        }
+    } else if (lane < count) {
+        chosen[lane] = (uint16_t)lane;
+    }
+    wave_lds_sync();
+
+    uint32_t value[K], pos[K];
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+        if (r < count) {
+            const typename Key::Word w = keys[(row * slices + chosen[r]) * kWave + lane];
+            value[r] = Key::value(w), pos[r] = Key::pos(w);
+        }
+    }
+    if (slices < k)
+        tau = kth_largest<VB, false>(value, count, k);
+    int above = 0;
+#pragma unroll
+    for (int r = 0; r < K; ++r)
+        if (r < count)
+            above += __builtin_popcountll(__ballot(value[r] > tau));
+    int equal = k - above, n = 0; // of the groups at tau the first `equal` may be needed: slices in order, positions in a slice
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+        if (r < count) {
+            const bool tie = value[r] == tau && equal > 0;
+            const int ties = __builtin_popcountll(__ballot(tie));
+            uint32_t limit = ~0u; // positions below it are taken
+            if (ties > equal && equal > 0) {
+                limit = 0;
+#pragma unroll 1
+                for (int b = 15; b >= 0; --b) {
+                    const uint32_t mid = limit | 1u << b;
+                    if (__builtin_popcountll(__ballot(tie && pos[r] < mid)) <= equal)
+                        limit = mid;
                 }
             }
+            const bool tie_taken = tie && pos[r] < limit;
+            equal -= __builtin_popcountll(__ballot(tie_taken));
+            const bool take = value[r] > tau || tie_taken;
+            const uint64_t all = __ballot(take);
+            if (take) {
+                const int at = n + __builtin_popcountll(all & below);
+                list[at] = (uint64_t)value[r] << 32 | (uint32_t)~(r << 16 | pos[r]);
+                where[at] = (uint16_t)(r << 6 | lane);
+            }
+            n += __builtin_popcountll(all);
+        }
+    }
+    wave_lds_sync();
+    // the k best of them, and the k-th: from its value on, and at its value up to its chunk, a logit counts
+    uint64_t kth = 0;
+    for (int a = lane; a < n; a += kWave) {
+        const uint64_t mine = list[a];
+        int rank = 0;
+        for (int o = 0; o < n; ++o)
+            rank += list[o] > mine;
+        if (rank < k)
+            groups[rank] = (uint32_t)chosen[where[a] >> 6] << 6 | (where[a] & 63u);
+        if (rank == k - 1)
+            kth = mine;
+    }
+    const uint64_t has = __ballot(kth != 0);
+    const int found = n < k ? n : k;
+    const int from = has ? __builtin_ctzll(has) : 0;
+    const uint32_t kth_value = __builtin_amdgcn_readlane((uint32_t)(kth >> 32), from);
+    const uint32_t kth_place = ~(uint32_t)__builtin_amdgcn_readlane((uint32_t)kth, from);
+    const float least = from_order_bits(Key::order(kth_value));
+    const int64_t last = has ? (int64_t)chosen[(kth_place >> 16) & (K - 1)] * (NC * kWave) + (kth_place & 0xFFFFu) : 0;
+    wave_lds_sync();
+
+    const T *p = x.p + row * x.stride;
+    const int64_t chunks = (vocab + W - 1) / W;
+    for (int c = lane; c < found * NC; c += kWave) {
+        const uint32_t g = groups[c / NC];
+        const int64_t chunk = (int64_t)(g >> 6) * (NC * kWave) + (c % NC) * kWave + (g & 63u);
+        if (chunk >= chunks)
+            continue;
+        const int64_t e = chunk * W;
+        float v[W];
+        load_row(p, e, vocab, v);
+        end_row(e, vocab, v, -__builtin_inff());
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            if (e + j < vocab && (v[j] > least || (v[j] == least && chunk <= last)))
+                list[atomicAdd(&listed, 1u)] = entry_of(v[j], (uint32_t)(e + j));
+    }
+    wave_lds_sync();
+    n = (int)uniform(listed);
+    const bool bad = !(S - S == 0.0f);
+    for (int a = lane; a < (n > k ? n : k); a += kWave) {
+        const uint64_t mine = a < n ? list[a] : 0;
+        int rank = a;
+        if (a < n) {
+            rank = 0;
+            for (int o = 0; o < n; ++o)
+                rank += list[o] > mine;
+        }
+        if (rank < k) {
+            const int64_t at = row * k + rank;
+            const float v = S == 0.0f ? -__builtin_inff() : (from_order_bits((uint32_t)(mine >> 32)) - ref) - kLn2 * log2_of(S);
+            out.top_logp[at] = bad ? __builtin_nanf("") : v;
+            out.top_ids[at] = bad ? -1 : (int64_t)entry_index(mine);
         }
     }
 }
@@ -404,7 +486,7 @@ __global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t
 // A = g_lse - g_logp - g_H H, B = -g_H ln 2.
 struct RowGrad {
     float ref, A, B, hit; // ref: lse, or 0 for a row without a finite logit
-    int64_t target;       // -1: none
+    int target;           // -W or less: none
 };
 
 SDP4_DEV RowGrad row_grad(float lse, float entropy, int64_t target, int64_t vocab, float g_logp, float g_entropy,
@@ -418,7 +500,7 @@ SDP4_DEV RowGrad row_grad(float lse, float entropy, int64_t target, int64_t voca
     r.A = g_lse - r.hit - g_entropy * entropy;
     r.B = -kLn2 * g_entropy;
     r.ref = empty ? 0.0f : lse;
-    r.target = target >= 0 && target < vocab && !empty ? target : -1;
+    r.target = target >= 0 && target < vocab && !empty ? (int)target : -1024;
     if (empty && target < vocab)
         r.A = r.B = 0.0f;
     if (!(lse == lse))
@@ -426,25 +508,25 @@ SDP4_DEV RowGrad row_grad(float lse, float entropy, int64_t target, int64_t voca
     return r;
 }
 
-// Gradient of the W elements of a chunk that starts at element e of the row; zeros from vocab on.
-template <int W, bool ENT, class X>
-SDP4_DEV void grad_chunk(const RowGrad &g, float A, X exponent, float delta, int64_t e, int64_t vocab, float (&v)[W])
+// Gradient of the W elements of a chunk that starts at element e of the row; zeros from vocab on (WHOLE: it ends before).
+template <int W, bool ENT, bool WHOLE, class X>
+SDP4_DEV void grad_chunk(const RowGrad &g, X exponent, float delta, int e, int vocab, float (&v)[W])
 {
 #pragma unroll
     for (int j = 0; j < W; ++j) {
         const float t = exponent(v[j]), p = exp2_of(t);
         if constexpr (ENT)
-            v[j] = p * __builtin_fmaf(g.B, fmaxf(t, -1000.0f) - delta, A);
+            v[j] = p * __builtin_fmaf(g.B, fmaxf(t, -1000.0f) - delta, g.A);
         else
-            v[j] = p * A;
+            v[j] = p * g.A;
     }
-    const int64_t at = g.target - e;
-    if (at >= 0 && at < W) {
+    const uint32_t at = (uint32_t)(g.target - e);
+    if (at < (uint32_t)W) {
 #pragma unroll
         for (int j = 0; j < W; ++j)
-            v[j] += at == j ? g.hit : 0.0f;
+            v[j] += at == (uint32_t)j ? g.hit : 0.0f;
     }
-    if (e + W > vocab) {
+    if (!WHOLE && e + W > vocab) {
 #pragma unroll
         for (int j = 0; j < W; ++j)
             v[j] = e + j < vocab ? v[j] : 0.0f;
@@ -453,12 +535,13 @@ SDP4_DEV void grad_chunk(const RowGrad &g, float A, X exponent, float delta, int
 
 // A wave takes U * 64 chunks of one row.
 template <class T, int U, bool ENT>
-__global__ __launch_bounds__(256) void k_logprob_grad(Rows<const T *> x, int64_t rows, int64_t vocab,
+__global__ __launch_bounds__(256) void k_logprob_grad(Rows<const T *> x, int64_t rows, int64_t vocab64,
                                                       const int64_t *targets, const float *lse, const float *entropy,
-                                                      TokenGrads g, Rows<T *> dx, int64_t width, Divisor tiles)
+                                                      TokenGrads g, Rows<T *> dx, int64_t width64, Divisor tiles)
 {
     constexpr int W = kChunk<T>;
-    const uint32_t wave = uniform(threadIdx.x / kWave), lane = lane_id();
+    const int vocab = (int)vocab64, width = (int)width64; // below 2^31 with the lanes beyond them
+    const uint32_t wave = uniform(threadIdx.x / kWave);
     const uint64_t w = (uint64_t)work_block() * 4 + wave;
     uint64_t tile;
     const int64_t row = (int64_t)divide(w, tiles, tile);
@@ -466,118 +549,114 @@ __global__ __launch_bounds__(256) void k_logprob_grad(Rows<const T *> x, int64_t
         return;
     const T *p = x.p + row * x.stride;
     T *q = dx.p + row * dx.stride;
-    const int64_t first = (int64_t)tile * (U * kWave) + lane;
+    const int64_t start = (int64_t)tile * (U * kWave * W);
+    const bool whole = start + U * kWave * W <= vocab;
+    const int64_t at = start + lane_id() * W;
     float v[U][W];
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int64_t e = (first + i * kWave) * W;
-        load_elems(p + e, vocab - e, v[i]);
+        for (int i = 0; i < U; ++i)
+            load_whole(p + start + (uint32_t)(lane_id() * W + i * (kWave * W)), v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int64_t e = at + i * (kWave * W);
+            load_row(p, e < vocab ? e : 0, vocab, v[i]);
+            end_row(e, vocab, v[i]);
+        }
     }
     const RowGrad rg = row_grad(lse[row], ENT ? entropy[row] : 0.0f, targets ? targets[row] : -1, vocab,
                                 g.logp ? g.logp[row] : 0.0f, ENT ? g.entropy[row] : 0.0f, g.lse ? g.lse[row] : 0.0f);
     with_exponent(rg.ref, 0.0f, [&](auto exponent, float delta) {
         const float f = exp2_of(-delta);
         RowGrad s = rg;
-        s.B *= f;
+        s.A *= f, s.B *= f;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int64_t e = (first + i * kWave) * W;
-            grad_chunk<W, ENT>(s, rg.A * f, exponent, delta, e, vocab, v[i]);
-            store_elems(q + e, width - e, v[i]);
+            const int64_t e = at + i * (kWave * W);
+            if (whole) {
+                grad_chunk<W, ENT, true>(s, exponent, delta, (int)e, vocab, v[i]);
+                store_elems(q + start + (uint32_t)(lane_id() * W + i * (kWave * W)), W, v[i]);
+            } else if (e < width) {
+                grad_chunk<W, ENT, false>(s, exponent, delta, (int)e, vocab, v[i]);
+                store_elems(q + e, width - e, v[i]);
+            }
         }
     });
 }
 
-// The loss and its gradient: a block holds a whole row in registers, so the logits are read once.
+// The loss and its gradient: a block holds a whole row in registers, so the logits are read once.  Each wave sums up its
+// own part, the parts are joined through LDS, and with the row's statistics every lane turns what it holds into the
+// gradient.
 template <class T, int WAVES, int NC, bool ENT>
-__global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, int64_t rows, int64_t vocab,
-                                                           TokenStats out, TokenGrads g, Rows<T *> dx, int64_t width)
+__global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, int64_t rows, int64_t vocab64,
+                                                           TokenStats out, TokenGrads g, Rows<T *> dx, int64_t width64)
 {
-    constexpr int W = kChunk<T>, NT = kWave * WAVES;
-    __shared__ float red[3][WAVES];
+    constexpr int W = kChunk<T>, STEP = kWave * WAVES * W;
+    __shared__ Slice red[WAVES];
     const int64_t row = work_block();
     if (row >= rows)
         return;
-    const uint32_t wave = threadIdx.x / kWave, lane = lane_id();
+    const int vocab = (int)vocab64, width = (int)width64; // below 2^20, and a row's registers
+    const int wave = (int)uniform(threadIdx.x / kWave), lane = lane_id();
     const T *p = x.p + row * x.stride;
     T *q = dx.p + row * dx.stride;
     const int64_t target = out.targets ? out.targets[row] : -1;
     const float g_logp = g.logp ? g.logp[row] : 0.0f, g_ent = ENT ? g.entropy[row] : 0.0f,
                 g_lse = g.lse ? g.lse[row] : 0.0f;
-    float tx = target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f;
+    const float tx = target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f;
+    // round i of the wave: 64 chunks from element start + i * STEP on
+    const int start = wave * (kWave * W), at = start + lane * W;
+    const int rounds = start < vocab ? (vocab - start + STEP - 1) / STEP : 0;
+    const int full = start + kWave * W <= vocab ? (vocab - start - kWave * W) / STEP + 1 : 0; // whole rounds
     u32x4 raw[NC];
-    float m = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int64_t e = ((int64_t)i * NT + threadIdx.x) * W;
-        float v[W];
-        if (e + W <= vocab) {
-            raw[i] = load_chunk<true>(p + e);
-        } else {
-            load_elems(p + e, vocab - e, v, -__builtin_inff());
+        if (i < full) {
+            raw[i] = load_chunk<true>(p + (uint32_t)(at + i * STEP));
+        } else if (i < rounds) {
+            float v[W];
+            const int e = at + i * STEP;
+            load_row(p, e < vocab ? e : 0, vocab, v);
+            end_row(e, vocab, v, -__builtin_inff());
             raw[i] = pack<T>(v);
         }
     }
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        float v[W];
-        unpack<T>(raw[i], v);
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            m = fmaxf(m, v[j]);
-    }
-    m = max_wave(m);
-    if (lane == 0)
-        red[0][wave] = m;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i)
-        m = fmaxf(m, red[0][i]);
-    float S = 0.0f, T2 = 0.0f;
-    with_exponent(m == -__builtin_inff() ? 0.0f : m, 0.0f, [&](auto exponent, float delta) {
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            float v[W];
-            unpack<T>(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float t = exponent(v[j]), e = exp2_of(t);
-                S += e;
-                T2 = __builtin_fmaf(e, fmaxf(t, -1000.0f), T2);
-            }
-        }
-        S = sum_lanes(S, kWave);
-        T2 = sum_lanes(T2, kWave);
+    Slice s{0.0f, 0.0f, 0.0f, 0.0f};
+    if (rounds)
+        slice_sums<T, NC>(raw, rounds, full == rounds, s.ref, s.S, s.T);
+    float ref = s.ref, S = s.S, T2 = s.T;
+    if constexpr (WAVES > 1) {
         if (lane == 0)
-            red[1][wave] = S, red[2][wave] = T2;
+            red[wave] = s;
         __syncthreads();
-        S = T2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i)
-            S += red[1][i], T2 += red[2][i];
-        const float f = exp2_of(-delta);
-        T2 = f * __builtin_fmaf(-delta, S, T2);
-        S *= f;
-    });
+        Slice part[1] = {lane < WAVES ? red[lane] : Slice{0.0f, 0.0f, 0.0f, 0.0f}};
+        join_sums<1>(part, ref, S, T2);
+    }
     if (threadIdx.x == 0)
-        finish_row(out, row, vocab, m, S, T2, tx, target);
+        finish_row(out, row, vocab, ref, S, T2, tx, target);
     const bool empty = S == 0.0f;
-    const float ln_s = kLn2 * log2_of(S);
-    const float lse = empty ? -__builtin_inff() : m + ln_s;
+    const float lg = empty ? 0.0f : log2_of(S), ln_s = kLn2 * lg;
+    const float lse = empty ? -__builtin_inff() : ref + ln_s;
     const float ent = ENT ? (empty ? 0.0f : fmaxf(ln_s - kLn2 * (T2 / S), 0.0f) + (S - S)) : 0.0f;
     const RowGrad rg = row_grad(lse, ent, target, vocab, g_logp, g_ent, g_lse);
-    // from m and log2 S rather than from their rounded sum
-    with_exponent(empty ? 0.0f : m, empty ? 0.0f : log2_of(S), [&](auto exponent, float delta) {
+    // from the reference and log2 S rather than from their rounded sum
+    with_exponent(empty ? 0.0f : ref, lg, [&](auto exponent, float delta) {
         const float f = exp2_of(-delta);
         RowGrad s = rg;
-        s.B *= f;
+        s.A *= f, s.B *= f;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int64_t e = ((int64_t)i * NT + threadIdx.x) * W;
-            if (e < width) {
+            const int e = at + i * STEP;
+            if (i < full) {
                 float v[W];
                 unpack<T>(raw[i], v);
-                grad_chunk<W, ENT>(s, rg.A * f, exponent, delta, e, vocab, v);
+                grad_chunk<W, ENT, true>(s, exponent, delta, e, vocab, v);
+                store_chunk<T>(q + (uint32_t)e, pack<T>(v));
+            } else if (e < width) {
+                float v[W];
+                unpack<T>(raw[i], v); // nothing of it counts from vocab on
+                grad_chunk<W, ENT, false>(s, exponent, delta, e, vocab, v);
                 store_elems(q + e, width - e, v);
             }
         }
@@ -590,51 +669,67 @@ Rows<T *> typed(Rows<P> r)
     return {static_cast<T *>(r.p), r.stride};
 }
 
-// How a row is cut into slices: NC chunks per lane, `slices` of `each` chunks.
+// How a row is cut into slices of 64 * nc chunks: the largest that still give 2048 waves, and no more than 64 if that
+// can be.
 struct Cut {
     int nc;
-    int64_t slices, each;
+    int64_t slices;
 };
-Cut cut_rows(int64_t rows, int64_t vocab, int chunk, int most)
-{
-    const int64_t chunks = (vocab + chunk - 1) / chunk;
-    int nc = 1;
-    const auto slices = [&](int n) { return (chunks + 64 * n - 1) / (64 * n); };
-    // the largest slices that still give 2048 waves, no more than kMaxSlices of them
-    while (nc < most && slices(nc) > 1 && (slices(nc) > kMaxSlices || rows * slices(2 * nc) >= 2048))
-        nc *= 2;
-    const int64_t each = (chunks + slices(nc) - 1) / slices(nc);
-    return {nc, (chunks + each - 1) / each, each};
-}
-
 template <class T>
-constexpr int kMostChunks = sizeof(T) == 2 ? 8 : 16;
-
-template <class T, bool TOP>
-auto slice_kernel(int nc)
+Cut cut_rows(int64_t rows, int64_t vocab)
 {
-    if constexpr (kMostChunks<T> == 16)
+    constexpr int most = sizeof(T) == 2 ? 8 : 16; // 4096 logits
+    const int64_t chunks = (vocab + kChunk<T> - 1) / kChunk<T>;
+    const auto slices = [&](int n) { return (chunks + 64 * n - 1) / (64 * n); };
+    int nc = 1;
+    while (nc < most && slices(nc) > 1 && (slices(nc) > kWave || rows * slices(2 * nc) >= 2048))
+        nc *= 2;
+    return {nc, slices(nc)};
+}
+static_assert(kMaxSlices * 4096 >= SDP4_MAX_VOCAB, "slices of a row");
+
+template <class T, class F>
+int with_chunks(int nc, F run)
+{
+    using std::integral_constant;
+    if constexpr (sizeof(T) == 4)
         if (nc == 16)
-            return k_logprob_slices<T, 16, TOP>;
-    return nc == 1   ? k_logprob_slices<T, 1, TOP>
-           : nc == 2 ? k_logprob_slices<T, 2, TOP>
-           : nc == 4 ? k_logprob_slices<T, 4, TOP>
-                     : k_logprob_slices<T, 8, TOP>;
+            return run(integral_constant<int, 16>{});
+    return nc == 1   ? run(integral_constant<int, 1>{})
+           : nc == 2 ? run(integral_constant<int, 2>{})
+           : nc == 4 ? run(integral_constant<int, 4>{})
+                     : run(integral_constant<int, 8>{});
 }
 
 template <class T>
 int logprob(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenStats &out, void *workspace, hipStream_t s)
 {
-    const Cut c = cut_rows(rows, vocab, kChunk<T>, kMostChunks<T>);
+    using Word = typename GroupKey<T>::Word;
+    const Cut c = cut_rows<T>(rows, vocab);
     Slice *stats = static_cast<Slice *>(workspace);
-    uint64_t *lists = reinterpret_cast<uint64_t *>(stats + (c.slices > 1 ? rows * c.slices : 0));
-    auto k = out.top_k ? slice_kernel<T, true>(c.nc) : slice_kernel<T, false>(c.nc);
-    const int rc = launch<4>(k, (rows * c.slices + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab,
-                             Divisor((uint64_t)c.slices), c.each, out, stats, lists);
-    if (rc || c.slices == 1)
-        return rc;
-    return launch<4>(k_logprob_join<T>, (rows + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab, (int)c.slices,
-                     out, stats, lists);
+    Word *keys = reinterpret_cast<Word *>(stats + rows * c.slices);
+    return with_chunks<T>(c.nc, [&](auto chunks) {
+        constexpr int NC = decltype(chunks)::value;
+        auto k = out.top_k ? k_logprob_slices<T, NC, true> : k_logprob_slices<T, NC, false>;
+        const int rc = launch<4>(k, (rows * c.slices + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab,
+                                 Divisor((uint64_t)c.slices), out, stats, keys);
+        if (rc || (c.slices == 1 && !out.top_k))
+            return rc;
+        if (out.top_k)
+            return launch<1>(out.top_k <= 8 ? k_logprob_join_top<T, NC, 8> : k_logprob_join_top<T, NC, kMaxTop>, rows,
+                             kUncapped, s, typed<const T>(x), rows, vocab, (int)c.slices, out, stats, keys);
+        return launch<4>(k_logprob_join<T>, (rows + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab,
+                         (int)c.slices, out, stats);
+    });
+}
+
+template <class T>
+int64_t workspace_of(int64_t rows, int64_t vocab, int top_k)
+{
+    const Cut c = cut_rows<T>(rows, vocab);
+    if (c.slices == 1 && !top_k)
+        return 0;
+    return rows * c.slices * (int64_t)(sizeof(Slice) + (top_k ? kWave * sizeof(typename GroupKey<T>::Word) : 0));
 }
 
 template <class T, bool ENT>
@@ -660,14 +755,21 @@ int token_loss(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenSta
         return launch<WV>(k_token_loss<T, WV, NC, ENT>, rows, kUncapped, s, typed<const T>(x), rows, vocab, out, g,
                           typed<T>(dx), width);
     };
+    using std::integral_constant;
     if (chunks <= 256)
-        return run(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+        return run(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+    if (chunks <= 1024)
+        return run(integral_constant<int, 4>{}, integral_constant<int, 4>{});
     if (chunks <= 2048)
-        return run(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
+        return run(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+    if (chunks <= 4096)
+        return run(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    if (chunks <= 6656)
+        return run(integral_constant<int, 8>{}, integral_constant<int, 13>{});
     if (chunks <= 8192)
-        return run(std::integral_constant<int, 16>{}, std::integral_constant<int, 8>{});
+        return run(integral_constant<int, 16>{}, integral_constant<int, 8>{});
     if (chunks <= 16384)
-        return run(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
+        return run(integral_constant<int, 16>{}, integral_constant<int, 16>{});
     const int rc = logprob<T>(x, rows, vocab, out, workspace, s);
     return rc ? rc : logprob_grad<T, ENT>(x, rows, vocab, out.targets, out.lse, out.entropy, g, dx, width, s);
 }
@@ -678,14 +780,8 @@ int64_t token_logprob_workspace(int64_t rows, int64_t vocab, int top_k)
 {
     if (rows <= 0 || vocab <= 0)
         return 0;
-    int64_t most = 0;
-    for (int two = 0; two < 2; ++two) { // either type
-        const Cut c = two ? cut_rows(rows, vocab, kChunk<bf16_t>, kMostChunks<bf16_t>)
-                          : cut_rows(rows, vocab, kChunk<float>, kMostChunks<float>);
-        const int64_t n = c.slices > 1 ? rows * c.slices * (int64_t)(sizeof(Slice) + sizeof(uint64_t) * top_k) : 0;
-        most = n > most ? n : most;
-    }
-    return most;
+    const int64_t a = workspace_of<bf16_t>(rows, vocab, top_k), b = workspace_of<float>(rows, vocab, top_k);
+    return a > b ? a : b; // for either type
 }
 
 int launch_token_logprob(int dtype, Rows<const void *> x, int64_t rows, int64_t vocab, const TokenStats &out,

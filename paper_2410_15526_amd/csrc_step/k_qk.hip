@@ -31,12 +31,14 @@ struct Side { // queries or keys
     T *out;
     int64_t dy_token, dy_head, x_token, x_head, out_token, out_head;
     Divisor heads;
+    uint32_t inv32;        // floor((2^32 - 1) / heads)
     int64_t items, blocks; // heads of all tokens, and the blocks that share them
     const T *weight;
     float *parts; // [blocks][dim] partial weight gradients
 };
 
-// One lane's unit of a head: where its two chunks lie, and which angles turn them.
+// One lane's unit of a head: where its two chunks lie, and which angles turn them.  Places that do not exist (`on`,
+// `on_b`) name existing ones: they are read like the others and what is read is not used.
 template <int W, bool INTER>
 struct Unit {
     int a, b;      // first elements of the chunks
@@ -46,33 +48,44 @@ struct Unit {
     SDP4_DEV Unit(const Layout &l, int u)
     {
         on = u < l.units;
+        u = on ? u : 0;
         if constexpr (INTER && W > 1) {
             a = 2 * W * u, b = a + W;
             turn_a = a < l.rot, turn_b = b < l.rot;
-            angle_a = a / 2, angle_b = b / 2;
+            angle_a = turn_a ? a / 2 : 0, angle_b = turn_b ? b / 2 : 0;
         } else {
             const bool turned = u < l.rot_units;
             const int v = turned ? u : u - l.rot_units;
             a = turned ? (INTER ? 2 * u : W * u) : l.rot + 2 * W * v;
             b = turned && !INTER ? a + l.half : a + W;
             turn_a = turn_b = turned;
-            angle_a = angle_b = W * u;
+            angle_a = angle_b = turned ? W * u : 0;
         }
         on_b = on && b < l.dim;
-        turn_a &= on, turn_b &= on_b;
+        b = b < l.dim ? b : a;
+        turn_b &= on_b;
     }
 };
 
 // W elements at an element address.
-template <class T, int W>
+template <class T, int W, bool NT>
 SDP4_DEV void load_w(const T *p, float (&v)[W])
 {
     if constexpr (W * sizeof(T) == 16) {
-        unpack<T>(load_chunk<true>(p), v);
+        unpack<T>(load_chunk<NT>(p), v);
     } else if constexpr (W * sizeof(T) == 8) {
-        const u32x2 c = __builtin_nontemporal_load(reinterpret_cast<const u32x2_b2 *>(p));
-        v[0] = __uint_as_float(c.x << 16), v[1] = __uint_as_float(c.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(c.y << 16), v[3] = __uint_as_float(c.y & 0xFFFF0000u);
+        auto q = reinterpret_cast<const half_at<T> *>(p);
+        const u32x2 c = NT ? (u32x2)__builtin_nontemporal_load(q) : (u32x2)*q;
+        if constexpr (W == 2) {
+            v[0] = __uint_as_float(c.x), v[1] = __uint_as_float(c.y);
+        } else {
+            v[0] = __uint_as_float(c.x << 16), v[1] = __uint_as_float(c.x & 0xFFFF0000u);
+            v[2] = __uint_as_float(c.y << 16), v[3] = __uint_as_float(c.y & 0xFFFF0000u);
+        }
+    } else if constexpr (sizeof(T) == 4 && W % 4 == 0) {
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k)
+            unpack<T>(load_chunk<NT>(p + 4 * k), *reinterpret_cast<float(*)[4]>(v + 4 * k));
     } else {
 #pragma unroll
         for (int j = 0; j < W; ++j)
@@ -82,86 +95,98 @@ SDP4_DEV void load_w(const T *p, float (&v)[W])
 template <class T, int W>
 SDP4_DEV void store_w(T *p, const float (&v)[W])
 {
-    if constexpr (W * sizeof(T) == 16) {
+    if constexpr (W * sizeof(T) == 16)
         store_chunk<T>(p, pack<T>(v));
-    } else if constexpr (W * sizeof(T) == 8) {
-        const u32x2 c = {bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
-        __builtin_nontemporal_store((u32x2_b2)c, reinterpret_cast<u32x2_b2 *>(p));
-    } else {
+    else if constexpr (W * sizeof(T) == 8)
+        store_half(p, v);
+    else
 #pragma unroll
         for (int j = 0; j < W; ++j)
             p[j] = from_f32<T>(v[j]);
-    }
-}
-// Table entries and weights, which other lanes and blocks read again.
-template <int W>
-SDP4_DEV void load_kept(const float *p, float (&v)[W])
-{
-    if constexpr (W % 4 == 0) {
-#pragma unroll
-        for (int k = 0; k < W / 4; ++k)
-            unpack<float>(load_chunk<false>(p + 4 * k), *reinterpret_cast<float(*)[4]>(v + 4 * k));
-    } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            v[j] = p[j];
-    }
-}
-template <class T, int W>
-SDP4_DEV void load_weight(const T *p, float (&v)[W])
-{
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-        v[j] = to_f32<T>(p[j]);
 }
 
-// Angles of a unit and their use.  BACK: by the opposite angle.
+// Two chunks of a lane's unit.
+template <int W>
+struct Two {
+    float a[W], b[W];
+    template <bool NT, class T, class U>
+    SDP4_DEV void load(const T *head, const U &u)
+    {
+        load_w<T, W, NT>(head + u.a, a);
+        load_w<T, W, NT>(head + u.b, b);
+    }
+    SDP4_DEV void fill(float v)
+    {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            a[j] = b[j] = v;
+    }
+    // what does not exist counts nothing in sums
+    template <class U>
+    SDP4_DEV void only(const U &u)
+    {
+        if (!u.on_b) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                a[j] = u.on ? a[j] : 0.0f, b[j] = 0.0f;
+        }
+    }
+    template <class T, class U>
+    SDP4_DEV void store(T *head, const U &u) const
+    {
+        if (u.on)
+            store_w<T, W>(head + u.a, a);
+        if (u.on_b)
+            store_w<T, W>(head + u.b, b);
+    }
+};
+
+// Angles of a unit and their use.
 template <int W, bool INTER>
 struct Angles {
     // half layout (and W = 1): W cosines and sines for both chunks; interleaved: W / 2 of either for each chunk
     float c[W], s[W];
-    SDP4_DEV void load(const Layout &l, const Unit<W, INTER> &u, const Rope &rope, int64_t token)
+    SDP4_DEV void load(const Layout &l, const Unit<W, INTER> &u, const Rope &rope, int64_t position)
     {
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            c[j] = 1.0f, s[j] = 0.0f;
-        if (!u.turn_a)
-            return;
-        const int64_t p = rope.positions ? rope.positions[token] : token;
-        if (p < 0 || p >= rope.rows) { // no such row: the result says so
+        const bool known = position >= 0 && position < rope.rows;
+        const float *row = rope.table + (known ? position : 0) * l.rot;
+        if constexpr (INTER && W > 1) {
+            constexpr int H = W / 2;
+            float(&c0)[H] = *reinterpret_cast<float(*)[H]>(c), (&c1)[H] = *reinterpret_cast<float(*)[H]>(c + H);
+            float(&s0)[H] = *reinterpret_cast<float(*)[H]>(s), (&s1)[H] = *reinterpret_cast<float(*)[H]>(s + H);
+            load_w<float, H, false>(row + u.angle_a, c0);
+            load_w<float, H, false>(row + l.half + u.angle_a, s0);
+            load_w<float, H, false>(row + u.angle_b, c1);
+            load_w<float, H, false>(row + l.half + u.angle_b, s1);
+        } else {
+            load_w<float, W, false>(row + u.angle_a, c);
+            load_w<float, W, false>(row + l.half + u.angle_a, s);
+        }
+        if (!known) { // no such row: the result says so
 #pragma unroll
             for (int j = 0; j < W; ++j)
                 c[j] = s[j] = __builtin_nanf("");
-            return;
-        }
-        const float *row = rope.table + p * l.rot;
-        if constexpr (INTER && W > 1) {
-            constexpr int H = W / 2;
-            load_kept<H>(row + u.angle_a, *reinterpret_cast<float(*)[H]>(c));
-            load_kept<H>(row + l.half + u.angle_a, *reinterpret_cast<float(*)[H]>(s));
-            if (u.turn_b) {
-                load_kept<H>(row + u.angle_b, *reinterpret_cast<float(*)[H]>(c + H));
-                load_kept<H>(row + l.half + u.angle_b, *reinterpret_cast<float(*)[H]>(s + H));
-            }
-        } else {
-            load_kept<W>(row + u.angle_a, c);
-            load_kept<W>(row + l.half + u.angle_a, s);
         }
     }
+    // BACK: by the opposite angle
     template <bool BACK>
-    SDP4_DEV void turn(const Unit<W, INTER> &u, float (&a)[W], float (&b)[W]) const
+    SDP4_DEV void turn(const Unit<W, INTER> &u, Two<W> &x) const
     {
+        if (!u.turn_a)
+            return;
         if constexpr (INTER && W > 1) {
 #pragma unroll
-            for (int j = 0; j < W / 2; ++j) {
-                one<BACK>(a[2 * j], a[2 * j + 1], c[j], s[j]);
-                if (u.turn_b)
-                    one<BACK>(b[2 * j], b[2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
+            for (int j = 0; j < W / 2; ++j)
+                one<BACK>(x.a[2 * j], x.a[2 * j + 1], c[j], s[j]);
+            if (u.turn_b) {
+#pragma unroll
+                for (int j = 0; j < W / 2; ++j)
+                    one<BACK>(x.b[2 * j], x.b[2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                one<BACK>(a[j], b[j], c[j], s[j]);
+                one<BACK>(x.a[j], x.b[j], c[j], s[j]);
         }
     }
     template <bool BACK>
@@ -173,6 +198,8 @@ struct Angles {
     }
 };
 
+SDP4_DEV int64_t position_of(const Rope &rope, int64_t token) { return rope.positions ? rope.positions[token] : token; }
+
 // 1 / sqrt(v) to the last place but rounding: one Newton step on the estimate.
 SDP4_DEV float rsqrt_of(float v)
 {
@@ -180,18 +207,6 @@ SDP4_DEV float rsqrt_of(float v)
     const float e = __builtin_fmaf(-v * y, y, 1.0f);
     const float z = __builtin_fmaf(0.5f * y, e, y);
     return e == e && __builtin_isfinite(y) ? z : y;
-}
-
-template <class T, int W>
-SDP4_DEV void load_unit(const T *head, bool on, bool on_b, int a, int b, float (&va)[W], float (&vb)[W])
-{
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-        va[j] = vb[j] = 0.0f;
-    if (on)
-        load_w<T, W>(head + a, va);
-    if (on_b)
-        load_w<T, W>(head + b, vb);
 }
 
 // Forward: one head per group of lanes; the first blocks take the queries, the others the keys.
@@ -202,65 +217,73 @@ __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, floa
     const bool keys = wb >= q.blocks;
     const Side<T> &s = keys ? k : q;
     const int lanes = 1 << l.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int64_t item = ((keys ? wb - q.blocks : wb) << (8 - l.lanes_log2)) + (threadIdx.x >> l.lanes_log2);
-    if (item >= s.items)
+    // the block's first head, and from there the lane group's: below 2^9 + heads, so 32 bits do
+    const int64_t first = (keys ? wb - q.blocks : wb) << (8 - l.lanes_log2);
+    uint64_t head0;
+    const int64_t token0 = (int64_t)divide((uint64_t)first, s.heads, head0);
+    const uint32_t group = threadIdx.x >> l.lanes_log2;
+    if (first + group >= s.items)
         return;
-    uint64_t head;
-    const int64_t token = (int64_t)divide((uint64_t)item, s.heads, head);
-    const T *x = s.x + token * s.x_token + (int64_t)head * s.x_head;
-    T *y = s.out + token * s.out_token + (int64_t)head * s.out_head;
-    float a[NU][W], b[NU][W];
+    uint32_t head = (uint32_t)head0 + group, ahead = __umulhi(head, s.inv32);
+    head -= ahead * (uint32_t)s.heads.d;
+    if (head >= (uint32_t)s.heads.d)
+        head -= (uint32_t)s.heads.d, ++ahead;
+    const int64_t token = token0 + ahead;
+    const T *x = s.x + token0 * s.x_token + (uint64_t)ahead * (uint64_t)s.x_token + (uint64_t)head * (uint64_t)s.x_head;
+    T *y = s.out + token0 * s.out_token + (uint64_t)ahead * (uint64_t)s.out_token + (uint64_t)head * (uint64_t)s.out_head;
+    Two<W> v[NU], w[NU];
+    Angles<W, INTER> turn[NU];
+    const int64_t position = l.rot ? position_of(rope, token) : 0;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         const Unit<W, INTER> u(l, lane + i * lanes);
-        load_unit<T, W>(x, u.on, u.on_b, u.a, u.b, a[i], b[i]);
+        v[i].template load<true>(x, u);
+        if constexpr (NORM) {
+            if (s.weight)
+                w[i].template load<false>(s.weight, u);
+        }
     }
-    float r = 1.0f;
+    if (l.rot) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i)
+            turn[i].load(l, Unit<W, INTER>(l, lane + i * lanes), rope, position);
+    }
     if constexpr (NORM) {
         float sq = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NU; ++i)
+        for (int i = 0; i < NU; ++i) {
+            v[i].only(Unit<W, INTER>(l, lane + i * lanes));
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                sq = __builtin_fmaf(a[i][j], a[i][j], sq);
-                sq = __builtin_fmaf(b[i][j], b[i][j], sq);
+                sq = __builtin_fmaf(v[i].a[j], v[i].a[j], sq);
+                sq = __builtin_fmaf(v[i].b[j], v[i].b[j], sq);
             }
-        r = rsqrt_of(__builtin_fmaf(sum_lanes(sq, lanes), l.inv_dim, eps));
+        }
+        const float r = rsqrt_of(__builtin_fmaf(sum_lanes(sq, lanes), l.inv_dim, eps));
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                v[i].a[j] *= r, v[i].b[j] *= r;
+            if (s.weight) {
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+                    v[i].a[j] *= w[i].a[j], v[i].b[j] *= w[i].b[j];
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         const Unit<W, INTER> u(l, lane + i * lanes);
-        if constexpr (NORM) {
-            float wa[W], wb_[W];
-#pragma unroll
-            for (int j = 0; j < W; ++j)
-                wa[j] = wb_[j] = 1.0f;
-            if (s.weight) {
-                if (u.on)
-                    load_weight<T, W>(s.weight + u.a, wa);
-                if (u.on_b)
-                    load_weight<T, W>(s.weight + u.b, wb_);
-            }
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                a[i][j] = a[i][j] * r * wa[j];
-                b[i][j] = b[i][j] * r * wb_[j];
-            }
-        }
-        if (u.turn_a) {
-            Angles<W, INTER> t;
-            t.load(l, u, rope, token);
-            t.template turn<false>(u, a[i], b[i]);
-        }
-        if (u.on)
-            store_w<T, W>(y + u.a, a[i]);
-        if (u.on_b)
-            store_w<T, W>(y + u.b, b[i]);
+        if (l.rot)
+            turn[i].template turn<false>(u, v[i]);
+        v[i].store(y, u);
     }
 }
 
-// Backward.  Each block takes every blocks-th group of heads of its side and adds up the weights' gradient in
-// registers; its lane groups and waves join at the end, and the block's sums go to the workspace.
+// Backward.  A block takes every blocks-th run of heads of its side; with DW it adds up the weights' gradient in
+// registers, its lane groups and waves join at the end, and the block's sums go to the workspace.  The next head's loads
+// are under way before the present one's stores: loads that follow stores wait for these.
 template <class T, int W, int NU, bool INTER, bool NORM, bool DW>
 __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k, float eps, Rope rope)
 {
@@ -271,54 +294,74 @@ __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k,
     const int64_t block = keys ? wb - q.blocks : wb;
     const int lanes = 1 << l.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> l.lanes_log2;
     const int groups = 256 >> l.lanes_log2;
-    float wa[NU][W], wv[NU][W], da[NU][W] = {}, db[NU][W] = {};
+    const uint32_t heads = (uint32_t)s.heads.d;
+    // first head of the lane group, and the step to its next: tokens and heads, where a carry makes one token more
+    uint64_t h0, hs;
+    int64_t item = block * groups + group;
+    const int64_t step = s.blocks * groups;
+    int64_t token = (int64_t)divide((uint64_t)item, s.heads, h0);
+    const int64_t token_step = (int64_t)divide((uint64_t)step, s.heads, hs);
+    uint32_t head = (uint32_t)h0;
+    const uint32_t head_step = (uint32_t)hs;
+    Two<W> w[NU], dw[NU], dy[NU], x[NU];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-        const Unit<W, INTER> u(l, lane + i * lanes);
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            wa[i][j] = wv[i][j] = 1.0f;
-        if (NORM && s.weight) {
-            if (u.on)
-                load_weight<T, W>(s.weight + u.a, wa[i]);
-            if (u.on_b)
-                load_weight<T, W>(s.weight + u.b, wv[i]);
-        }
+        dw[i].fill(0.0f);
+        if (NORM && s.weight)
+            w[i].template load<false>(s.weight, Unit<W, INTER>(l, lane + i * lanes));
+        else
+            w[i].fill(1.0f);
     }
-    for (int64_t item = block * groups + group; item < s.items; item += s.blocks * groups) {
-        uint64_t head;
-        const int64_t token = (int64_t)divide((uint64_t)item, s.heads, head);
-        const T *dy = s.dy + token * s.dy_token + (int64_t)head * s.dy_head;
-        const T *x = NORM ? s.x + token * s.x_token + (int64_t)head * s.x_head : nullptr;
-        T *dx = s.out + token * s.out_token + (int64_t)head * s.out_head;
-        float ga[NU][W], gb[NU][W], xa[NU][W], xb[NU][W];
+    int64_t position = 0;
+    auto fetch = [&] {
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const Unit<W, INTER> u(l, lane + i * lanes);
+            dy[i].template load<true>(s.dy + token * s.dy_token + (int64_t)head * s.dy_head, u);
+            if constexpr (NORM)
+                x[i].template load<true>(s.x + token * s.x_token + (int64_t)head * s.x_head, u);
+        }
+        if (l.rot)
+            position = position_of(rope, token);
+    };
+    if (item < s.items)
+        fetch();
+    for (; item < s.items; item += step) {
+        T *out = s.out + token * s.out_token + (int64_t)head * s.out_head;
+        Two<W> g[NU], xv[NU];
         float sq = 0.0f, dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const Unit<W, INTER> u(l, lane + i * lanes);
-            load_unit<T, W>(dy, u.on, u.on_b, u.a, u.b, ga[i], gb[i]);
-            if constexpr (NORM)
-                load_unit<T, W>(x, u.on, u.on_b, u.a, u.b, xa[i], xb[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const Unit<W, INTER> u(l, lane + i * lanes);
-            if (u.turn_a) {
+            g[i] = dy[i];
+            g[i].only(u);
+            if (l.rot) {
                 Angles<W, INTER> t;
-                t.load(l, u, rope, token);
-                t.template turn<true>(u, ga[i], gb[i]);
+                t.load(l, u, rope, position);
+                t.template turn<true>(u, g[i]);
             }
             if constexpr (NORM) {
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    sq = __builtin_fmaf(xa[i][j], xa[i][j], sq);
-                    sq = __builtin_fmaf(xb[i][j], xb[i][j], sq);
-                    dot = __builtin_fmaf(ga[i][j] * wa[i][j], xa[i][j], dot);
-                    dot = __builtin_fmaf(gb[i][j] * wv[i][j], xb[i][j], dot);
-                }
+                xv[i] = x[i];
+                xv[i].only(u);
             }
         }
+        if (DW || item + step < s.items) { // one head for each group of lanes otherwise
+            token += token_step, head += head_step;
+            if (head >= heads)
+                head -= heads, ++token;
+            if (item + step < s.items)
+                fetch();
+        }
         if constexpr (NORM) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    sq = __builtin_fmaf(xv[i].a[j], xv[i].a[j], sq);
+                    sq = __builtin_fmaf(xv[i].b[j], xv[i].b[j], sq);
+                    dot = __builtin_fmaf(g[i].a[j] * w[i].a[j], xv[i].a[j], dot);
+                    dot = __builtin_fmaf(g[i].b[j] * w[i].b[j], xv[i].b[j], dot);
+                }
             const float r = rsqrt_of(__builtin_fmaf(sum_lanes(sq, lanes), l.inv_dim, eps));
             const float m = sum_lanes(dot, lanes) * l.inv_dim * r * r; // mean(w g x r) r
 #pragma unroll
@@ -326,34 +369,28 @@ __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k,
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     if constexpr (DW) {
-                        da[i][j] = __builtin_fmaf(ga[i][j], xa[i][j] * r, da[i][j]);
-                        db[i][j] = __builtin_fmaf(gb[i][j], xb[i][j] * r, db[i][j]);
+                        dw[i].a[j] = __builtin_fmaf(g[i].a[j], xv[i].a[j] * r, dw[i].a[j]);
+                        dw[i].b[j] = __builtin_fmaf(g[i].b[j], xv[i].b[j] * r, dw[i].b[j]);
                     }
-                    ga[i][j] = r * __builtin_fmaf(-xa[i][j], m, ga[i][j] * wa[i][j]);
-                    gb[i][j] = r * __builtin_fmaf(-xb[i][j], m, gb[i][j] * wv[i][j]);
+                    g[i].a[j] = r * __builtin_fmaf(-xv[i].a[j], m, g[i].a[j] * w[i].a[j]);
+                    g[i].b[j] = r * __builtin_fmaf(-xv[i].b[j], m, g[i].b[j] * w[i].b[j]);
                 }
         }
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const Unit<W, INTER> u(l, lane + i * lanes);
-            if (u.on)
-                store_w<T, W>(dx + u.a, ga[i]);
-            if (u.on_b)
-                store_w<T, W>(dx + u.b, gb[i]);
-        }
+        for (int i = 0; i < NU; ++i)
+            g[i].store(out, Unit<W, INTER>(l, lane + i * lanes));
     }
     if constexpr (DW) {
         if (!s.parts)
             return;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const Unit<W, INTER> u(l, lane + i * lanes);
             if (i)
                 __syncthreads();
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                lds[(2 * j) * 256 + threadIdx.x] = da[i][j];
-                lds[(2 * j + 1) * 256 + threadIdx.x] = db[i][j];
+                lds[(2 * j) * 256 + threadIdx.x] = dw[i].a[j];
+                lds[(2 * j + 1) * 256 + threadIdx.x] = dw[i].b[j];
             }
             __syncthreads();
             // group 0's lanes hold the units: the threads of the block share out their 2 W sums
@@ -419,6 +456,7 @@ Side<T> side_of(const Heads *dy, const Heads &x, const Heads &out, int64_t token
 {
     Side<T> s{};
     s.heads = Divisor((uint64_t)(out.heads > 0 ? out.heads : 1));
+    s.inv32 = ~uint32_t(0) / (uint32_t)s.heads.d;
     s.items = tokens * out.heads;
     s.x = static_cast<const T *>(x.p), s.x_token = x.token_stride, s.x_head = x.head_stride;
     s.out = static_cast<T *>(out.p), s.out_token = out.token_stride, s.out_head = out.head_stride;
@@ -446,7 +484,7 @@ int with_layout(int w, int nu, bool inter, F run)
 }
 
 // Blocks of the backward pass of either side: about kGradBlocks for both, in proportion to their heads.
-constexpr int64_t kGradBlocks = 1024;
+constexpr int64_t kGradBlocks = 2048;
 int64_t grad_blocks(int64_t items, int64_t all, int groups)
 {
     if (items == 0)
@@ -523,12 +561,11 @@ int launch_qk_grad(int dtype, const Heads (&dy)[2], const Heads (&x)[2], const H
     });
     if (rc)
         return rc;
+    if (sums[0].parts && sums[1].parts)
+        return launch_sum_parts({{sums[0].parts, sums[0].blocks, dw[0]}, {sums[1].parts, sums[1].blocks, dw[1]}}, dim, dim, s);
     for (int i = 0; i < 2; ++i)
-        if (sums[i].parts) {
-            const int e = launch_sum_parts(sums[i].parts, sums[i].blocks, dim, dim, dw[i], s);
-            if (e)
-                return e;
-        }
+        if (sums[i].parts)
+            return launch_sum_parts({{sums[i].parts, sums[i].blocks, dw[i]}, {}}, dim, dim, s);
     return 0;
 }
 

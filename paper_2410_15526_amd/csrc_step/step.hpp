@@ -78,7 +78,12 @@ int64_t qk_grad_workspace(int64_t tokens, int q_heads, int k_heads, int dim);
 int launch_rope_table(const double *inv_freq, int half, int64_t start, int64_t rows, double scale, float *table,
                       hipStream_t s);
 
-// out[c] = the sum of parts[i * pitch + c] over i < nparts, for c < cols, in a fixed order
-int launch_sum_parts(const float *parts, int64_t nparts, int64_t pitch, int64_t cols, float *out, hipStream_t s);
+// out[c] = the sum of p[i * pitch + c] over i < count, for c < cols, in a fixed order; one or two such sums (out null: none).
+struct Parts {
+    const float *p = nullptr;
+    int64_t count = 0;
+    float *out = nullptr;
+};
+int launch_sum_parts(const Parts (&parts)[2], int64_t pitch, int64_t cols, hipStream_t s);
 
 } // namespace sdp4

@@ -73,6 +73,8 @@ typedef u32x2 u32x2_b2 __attribute__((aligned(2)));
 typedef u32x2 u32x2_b4 __attribute__((aligned(4)));
 template <class T>
 using chunk_at = std::conditional_t<sizeof(T) == 4, u32x4_b4, u32x4_b2>;
+template <class T>
+using half_at = std::conditional_t<sizeof(T) == 4, u32x2_b4, u32x2_b2>;
 
 // One chunk, streamed past the caches (NT) or kept in them.
 template <bool NT, class T>
@@ -115,19 +117,67 @@ SDP4_DEV u32x4 pack(const float (&v)[kChunk<T>])
         return u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])};
 }
 
-// N elements (a multiple of a chunk, or fewer than one) from element address p, of which `valid`
-// exist; the others read as `fill`.
-template <class T, int N>
-SDP4_DEV void load_elems(const T *p, int64_t valid, float (&v)[N], float fill = 0.0f)
+// Four bfloat16 elements, half a chunk.
+SDP4_DEV void load_half(const bf16_t *p, float (&v)[4])
 {
-    if (valid >= N) {
+    const u32x2 c = __builtin_nontemporal_load(reinterpret_cast<const u32x2_b2 *>(p));
+    v[0] = __uint_as_float(c.x << 16), v[1] = __uint_as_float(c.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(c.y << 16), v[3] = __uint_as_float(c.y & 0xFFFF0000u);
+}
+SDP4_DEV void store_half(bf16_t *p, const float (&v)[4])
+{
+    const u32x2 c = {bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
+    __builtin_nontemporal_store((u32x2_b2)c, reinterpret_cast<u32x2_b2 *>(p));
+}
+
+// N elements (whole chunks, or half a chunk of bfloat16) from element address p.
+template <class T, int N>
+SDP4_DEV void load_whole(const T *p, float (&v)[N])
+{
+    if constexpr (N < kChunk<T>) {
+        load_half(p, v);
+    } else {
 #pragma unroll
         for (int k = 0; k < N / kChunk<T>; ++k)
             unpack<T>(load_chunk<true>(p + k * kChunk<T>), *reinterpret_cast<float(*)[kChunk<T>]>(v + k * kChunk<T>));
+    }
+}
+
+// Elements c .. c + N - 1 of a row of `cols`, in two steps, so that the loads of several rows are in flight together:
+// where the row ends before, load_row reads its last N elements instead (what another lane may be replacing there is
+// not used) and end_row moves them to their places.  Places beyond the row get `fill`.
+template <class T, int N>
+SDP4_DEV void load_row(const T *row, int64_t c, int64_t cols, float (&v)[N])
+{
+    if (cols >= N) {
+        load_whole(row + (c + N <= cols ? c : cols - N), v);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            v[j] = j < valid ? to_f32<T>(p[j]) : fill;
+            v[j] = to_f32<T>(row[j < cols ? j : 0]);
+    }
+}
+template <int N>
+SDP4_DEV void end_row(int64_t c, int64_t cols, float (&v)[N], float fill = 0.0f)
+{
+    if (c + N <= cols)
+        return;
+    if (cols < N) { // load_row read from column 0, and c is 0 or beyond the row
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] = c + j < cols ? v[j] : fill;
+        return;
+    }
+    const int64_t by = c - (cols - N);
+    const int s = by < N ? (int)by : N;
+#pragma unroll
+    for (int b = N; b >= 1; b /= 2) {
+        const bool take = s & b;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float from = j + b < N ? v[j + b < N ? j + b : j] : fill;
+            v[j] = take ? from : v[j];
+        }
     }
 }
 
@@ -135,6 +185,8 @@ template <class T, int N>
 SDP4_DEV void store_elems(T *p, int64_t valid, const float (&v)[N])
 {
     if (valid >= N) {
+        if constexpr (N < kChunk<T>)
+            store_half(p, v);
 #pragma unroll
         for (int k = 0; k < N / kChunk<T>; ++k)
             store_chunk<T>(p + k * kChunk<T>, pack<T>(*reinterpret_cast<const float(*)[kChunk<T>]>(v + k * kChunk<T>)));
