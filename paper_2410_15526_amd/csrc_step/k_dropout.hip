@@ -149,7 +149,7 @@ __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, in
 {
     constexpr bool H = sizeof(In) == 4 || sizeof(Out) == 4;
     using L = Lanes<H>;
-    constexpr int N = L::N, C = L::COUNT;
+    constexpr int N = L::N, C = L::COUNT, U = 4 / C; // U rows of a lane in flight
     __shared__ float lds[256 * 8];
     const int lx = 1 << lx_log2, ly = 256 >> lx_log2;
     const int64_t part = work_block() / col_tiles, tile = work_block() - part * col_tiles;
@@ -172,40 +172,45 @@ __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, in
     const int drawn = wave + L::mine();
     uint64_t block = (uint64_t)((start + (drawn >> lx_log2)) * per_row + col0 + (drawn & (lx - 1)));
     const uint64_t block_step = (uint64_t)(ly * per_row);
-    float next[C][N];
+    Raw<In, N> next[U][C];
     auto fetch = [&](int64_t ahead) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int64_t at = r[i] + ahead < end ? r[i] + ahead : end - 1;
-            load_row(dy.p + at * dy.stride, c[i], d.cols, next[i]);
-        }
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                const int64_t at = r[i] + ahead + u * ly < end ? r[i] + ahead + u * ly : end - 1;
+                load_row(dy.p + at * dy.stride, c[i], d.cols, next[u][i]);
+            }
     };
     fetch(0);
-    for (int64_t r0 = start; r0 < end; r0 += ly) {
-        float v[C][N];
+    for (int64_t r0 = start; r0 < end; r0 += U * ly) {
+        float v[U][C][N];
 #pragma unroll
-        for (int i = 0; i < C; ++i)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                v[i][j] = next[i][j];
-        if (r0 + ly < end)
-            fetch(ly);
-        uint32_t words[C][N / 2];
-        if (d.drop)
-            L::draw(d, block, words);
-        block += block_step;
+            for (int i = 0; i < C; ++i)
+                next[u][i].get(v[u][i]);
+        if (r0 + U * ly < end)
+            fetch(U * ly);
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            if (r[i] < end && on[i]) {
-                end_row(c[i], d.cols, v[i]);
-                if (d.drop)
-                    apply_mask(words[i], d.drop, d.scale, v[i]);
+        for (int u = 0; u < U; ++u) {
+            uint32_t words[C][N / 2];
+            if (d.drop)
+                L::draw(d, block, words);
+            block += block_step;
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    acc[i][j] += v[i][j];
-                store_elems(dx.p + r[i] * dx.stride + c[i], d.cols - c[i], v[i]);
+            for (int i = 0; i < C; ++i) {
+                if (r[i] < end && on[i]) {
+                    end_row(c[i], d.cols, v[u][i]);
+                    if (d.drop)
+                        apply_mask(words[i], d.drop, d.scale, v[u][i]);
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        acc[i][j] += v[u][i][j];
+                    store_elems(dx.p + r[i] * dx.stride + c[i], d.cols - c[i], v[u][i]);
+                }
+                r[i] += ly;
             }
-            r[i] += ly;
         }
     }
 #pragma unroll
@@ -283,7 +288,10 @@ GradSplit grad_split(int64_t rows, int64_t cols)
         ++g.lx_log2;
     g.col_tiles = (g.per_row + (1 << g.lx_log2) - 1) >> g.lx_log2;
     const int64_t step = 256 >> g.lx_log2;          // rows a block takes at a time
-    int64_t want = (1024 + g.col_tiles - 1) / g.col_tiles;
+    #ifndef DGB
+#define DGB 1024
+#endif
+    int64_t want = (DGB + g.col_tiles - 1) / g.col_tiles;
     const int64_t most = (rows + 2 * step - 1) / (2 * step);
     want = want < most ? want : most;
     want = want < 1 ? 1 : want;

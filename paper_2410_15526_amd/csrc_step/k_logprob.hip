@@ -43,27 +43,28 @@ SDP4_DEV float from_order_bits(uint32_t k)
 SDP4_DEV uint64_t entry_of(float v, uint32_t index) { return (uint64_t)order_bits(v) << 32 | (0xFFFFFFFFu - index); }
 SDP4_DEV uint32_t entry_index(uint64_t e) { return 0xFFFFFFFFu - (uint32_t)e; }
 
-// A lane's largest logit in a slice and the position (of its chunk, in the slice) where it first stands.  Of bfloat16
-// order bits the upper 16 tell everything.
+// A lane's largest logit in a slice (its order bits; of bfloat16 the upper 16 tell everything), the round `at` in which it
+// first stands, and an upper bound of the largest logit of the lane's other rounds.
 template <class T>
-struct GroupKey;
-template <>
-struct GroupKey<bf16_t> {
-    using Word = uint32_t;
-    static constexpr int kValueBits = 16;
-    SDP4_DEV static Word make(uint32_t order, uint32_t pos) { return (order & 0xFFFF0000u) | pos; }
-    SDP4_DEV static uint32_t value(Word k) { return k >> 16; }
-    SDP4_DEV static uint32_t pos(Word k) { return k & 0xFFFFu; }
-    SDP4_DEV static uint32_t order(uint32_t value) { return value << 16 | (value & 0x8000u ? 0u : 0xFFFFu); }
-};
-template <>
-struct GroupKey<float> {
-    using Word = uint64_t;
-    static constexpr int kValueBits = 32;
-    SDP4_DEV static Word make(uint32_t order, uint32_t pos) { return (Word)order << 32 | pos; }
-    SDP4_DEV static uint32_t value(Word k) { return (uint32_t)(k >> 32); }
-    SDP4_DEV static uint32_t pos(Word k) { return (uint32_t)k; }
-    SDP4_DEV static uint32_t order(uint32_t value) { return value; }
+struct GroupKey {
+    static constexpr int kValueBits = sizeof(T) == 2 ? 16 : 32, kRestBits = sizeof(T) == 2 ? 12 : 28;
+    using Word = std::conditional_t<sizeof(T) == 2, uint32_t, uint64_t>;
+    SDP4_DEV static Word make(float top, uint32_t at, float rest)
+    {
+        return (Word)(order_bits(top) >> (32 - kValueBits)) << kValueBits | (Word)(order_bits(rest) >> (32 - kRestBits)) << 4 | at;
+    }
+    SDP4_DEV static uint32_t value(Word k) { return (uint32_t)(k >> kValueBits); }
+    SDP4_DEV static uint32_t at(Word k) { return (uint32_t)k & 15u; }
+    // order bits that no other logit of the group exceeds
+    SDP4_DEV static uint32_t rest(Word k)
+    {
+        const uint32_t r = (uint32_t)(k >> 4) << (32 - kRestBits);
+        return r | ((1u << (32 - kRestBits)) - 1);
+    }
+    SDP4_DEV static uint32_t order(uint32_t value)
+    {
+        return sizeof(T) == 2 ? value << 16 | (value & 0x8000u ? 0u : 0xFFFFu) : value;
+    }
 };
 
 SDP4_DEV float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
@@ -102,7 +103,7 @@ SDP4_DEV void finish_row(const TokenStats &out, int64_t row, int64_t vocab, floa
 }
 
 // Largest of a lane's values; NaN counts nothing.
-template <class T, int NC>
+template <class T>
 SDP4_DEV float chunk_max(const u32x4 &raw)
 {
     float v[kChunk<T>], m;
@@ -114,62 +115,110 @@ SDP4_DEV float chunk_max(const u32x4 &raw)
     return m;
 }
 
-// S and T of the wave's `rounds` chunks per lane, relative to the `ref` it chooses (uniform over the wave).
-//
-// The quick way (`whole`: every chunk holds logits only) takes the largest of the first round as reference, so that
-// every logit is seen once.  Where that does not do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is
-// not finite or far below the largest (T / S would cancel against log S), a type's lowest value, NaN -- the sums show
-// it, and the wave goes over its registers again with the true maximum and a lower bound on the exponent.
+// A wave's part of a row in registers: `full` chunks of each lane that hold logits only, and where the row ends in the
+// wave's next round, that round as `tail`, with -inf behind the end.
 template <class T, int NC>
-SDP4_DEV void slice_sums(const u32x4 (&raw)[NC], int rounds, bool whole, float &ref, float &S, float &T2)
+struct Held {
+    static constexpr int W = kChunk<T>;
+    u32x4 raw[NC], tail;
+    int full;
+    bool has_tail;
+
+    // Round i is the 64 chunks from element start + i * STEP of the row on; at most `most` rounds.
+    template <int STEP>
+    SDP4_DEV void load(const T *row, int start, int most, int vocab)
+    {
+        const int lane = lane_id();
+        full = start + kWave * W <= vocab ? (vocab - start - kWave * W) / STEP + 1 : 0;
+        full = full < most ? full : most;
+        has_tail = full < most && start + full * STEP < vocab;
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            if (i < full)
+                raw[i] = load_chunk<true>(row + (uint32_t)(start + i * STEP + lane * W));
+        tail = u32x4{0u, 0u, 0u, 0u};
+        if (has_tail) {
+            float v[W];
+            const int e = start + full * STEP + lane * W;
+            load_row(row, e < vocab ? e : 0, vocab, v);
+            end_row(e, vocab, v, -__builtin_inff());
+            tail = pack<T>(v);
+        }
+    }
+    SDP4_DEV bool any() const { return full > 0 || has_tail; }
+};
+
+// Sums of one chunk relative to `ref`; -inf counts nothing (2^-1000 is 0).
+template <class T>
+SDP4_DEV void add_guarded(const u32x4 &raw, float ref, float &S, float &T2)
+{
+    float v[kChunk<T>];
+    unpack<T>(raw, v);
+#pragma unroll
+    for (int j = 0; j < kChunk<T>; ++j) {
+        const float t = (v[j] - ref) * kLog2e, e = exp2_of(t);
+        S += e;
+        T2 = __builtin_fmaf(e, fmaxf(t, -1000.0f), T2);
+    }
+}
+
+// S and T of what the wave holds, relative to the `ref` it chooses (uniform over the wave), and with TOP the largest of
+// each chunk.
+//
+// The quick way takes the largest of the first round as reference, so that every logit is seen once.  Where that does not
+// do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is not finite or far below the largest (T / S would
+// cancel against log S), a type's lowest value, NaN -- the sums show it, and the wave goes over its registers again with
+// the true maximum and a lower bound on the exponent.
+template <bool TOP, class T, int NC>
+SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, float (&cm)[NC], float &tail_max)
 {
     constexpr int W = kChunk<T>;
-    if (whole) {
-        ref = max_wave(chunk_max<T, NC>(raw[0]));
-        const float c = ref * kLog2e;
-        S = T2 = 0.0f;
+    tail_max = h.has_tail ? chunk_max<T>(h.tail) : -__builtin_inff();
+    ref = max_wave(h.full ? chunk_max<T>(h.raw[0]) : tail_max);
+    const float c = ref * kLog2e;
+    S = T2 = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            if (i < rounds) {
-                float v[W];
-                unpack<T>(raw[i], v);
+    for (int i = 0; i < NC; ++i) {
+        if (i < h.full) {
+            float v[W];
+            unpack<T>(h.raw[i], v);
+            if constexpr (TOP) {
+                cm[i] = v[0];
 #pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const float t = __builtin_fmaf(v[j], kLog2e, -c), e = exp2_of(t);
-                    S += e;
-                    T2 = __builtin_fmaf(e, t, T2);
-                }
+                for (int j = 1; j < W; ++j)
+                    cm[i] = fmaxf(cm[i], v[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const float t = __builtin_fmaf(v[j], kLog2e, -c), e = exp2_of(t);
+                S += e;
+                T2 = __builtin_fmaf(e, t, T2);
             }
         }
-        S = sum_lanes(S, kWave);
-        T2 = sum_lanes(T2, kWave);
-        const float delta = __builtin_fmaf(ref, kLog2e, -c), f = exp2_of(-delta); // the rounding of c, taken out
-        T2 = f * __builtin_fmaf(-delta, S, T2);
-        S *= f;
-        if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < 1e38f)))
-            return;
     }
-    float m = -__builtin_inff();
+    const float delta = __builtin_fmaf(ref, kLog2e, -c), f = exp2_of(-delta); // the rounding of c, taken out
+    T2 = f * __builtin_fmaf(-delta, S, T2);
+    S *= f;
+    if (h.has_tail)
+        add_guarded<T>(h.tail, ref, S, T2);
+    S = sum_lanes(S, kWave);
+    T2 = sum_lanes(T2, kWave);
+    if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < 1e38f)))
+        return;
+    float m = tail_max;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-        if (i < rounds)
-            m = fmaxf(m, chunk_max<T, NC>(raw[i]));
+        if (i < h.full)
+            m = fmaxf(m, chunk_max<T>(h.raw[i]));
     m = max_wave(m);
     ref = m == -__builtin_inff() ? 0.0f : m;
     S = T2 = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        if (i < rounds) {
-            float v[W];
-            unpack<T>(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float t = (v[j] - ref) * kLog2e, e = exp2_of(t);
-                S += e;
-                T2 = __builtin_fmaf(e, fmaxf(t, -1000.0f), T2); // 2^-1000 is 0
-            }
-        }
-    }
+    for (int i = 0; i < NC; ++i)
+        if (i < h.full)
+            add_guarded<T>(h.raw[i], ref, S, T2);
+    if (h.has_tail)
+        add_guarded<T>(h.tail, ref, S, T2);
     S = sum_lanes(S, kWave);
     T2 = sum_lanes(T2, kWave);
 }
@@ -197,6 +246,35 @@ SDP4_DEV void join_sums(const Slice (&s)[N], float &ref, float &S, float &T2)
     T2 = sum_lanes(T2, kWave);
 }
 
+// What a slice leaves: its sums and, with TOP, its largest logit and the lane's key.
+template <bool TOP, class T, int NC>
+SDP4_DEV Slice take_slice(const Held<T, NC> &h, typename GroupKey<T>::Word &key)
+{
+    float ref, S, T2, cm[NC], tail_max;
+    slice_sums<TOP>(h, ref, S, T2, cm, tail_max);
+    float top = -__builtin_inff();
+    if constexpr (TOP) {
+        float rest = top;
+        uint32_t at = 0; // where nothing is larger than -inf, the first round
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            if (i < h.full) {
+                rest = fmaxf(rest, fminf(top, cm[i]));
+                at = cm[i] > top ? (uint32_t)i : at;
+                top = fmaxf(top, cm[i]);
+            }
+        }
+        if (h.has_tail) {
+            rest = fmaxf(rest, fminf(top, tail_max));
+            at = tail_max > top ? (uint32_t)h.full : at;
+            top = fmaxf(top, tail_max);
+        }
+        key = GroupKey<T>::make(top, at, rest);
+        top = max_wave(top);
+    }
+    return Slice{ref, S, T2, top};
+}
+
 // One slice per wave, four waves in a block: round i of a wave is 64 neighbouring chunks.
 template <class T, int NC, bool TOP>
 __global__ __launch_bounds__(256) void k_logprob_slices(Rows<const T *> x, int64_t rows, int64_t vocab,
@@ -211,52 +289,18 @@ __global__ __launch_bounds__(256) void k_logprob_slices(Rows<const T *> x, int64
     if (row >= rows)
         return;
     const T *p = x.p + row * x.stride;
-    const int64_t first = (int64_t)slice * (NC * kWave * W); // element of the row
-    const int left = (int)(vocab - first < NC * kWave * W ? vocab - first : NC * kWave * W);
-    const int rounds = (left + kWave * W - 1) / (kWave * W);
-    const bool whole = left == NC * kWave * W;
-    u32x4 raw[NC];
-    if (whole) {
-#pragma unroll
-        for (int i = 0; i < NC; ++i)
-            raw[i] = load_chunk<true>(p + first + (uint32_t)((i * kWave + lane) * W));
-    } else {
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            if (i < rounds) {
-                float v[W];
-                const int64_t e = first + (i * kWave + (int)lane) * W;
-                load_row(p, e < vocab ? e : 0, vocab, v);
-                end_row(e, vocab, v, -__builtin_inff());
-                raw[i] = pack<T>(v);
-            }
-        }
-    }
-    float ref, S, T2;
-    slice_sums<T, NC>(raw, rounds, whole, ref, S, T2);
-
-    float top = -__builtin_inff();
-    if constexpr (TOP) {
-        float cm[NC];
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            cm[i] = i < rounds ? chunk_max<T, NC>(raw[i]) : -__builtin_inff();
-            top = fmaxf(top, cm[i]);
-        }
-        uint32_t pos = lane;
-#pragma unroll
-        for (int i = NC - 1; i >= 0; --i)
-            if (cm[i] == top)
-                pos = (uint32_t)i * kWave + lane;
-        keys[w * kWave + lane] = GroupKey<T>::make(order_bits(top), pos);
-        top = max_wave(top);
-    }
+    Held<T, NC> h;
+    h.template load<kWave * W>(p, (int)slice * (NC * kWave * W), NC, (int)vocab);
+    typename GroupKey<T>::Word key;
+    const Slice s = take_slice<TOP>(h, key);
+    if constexpr (TOP)
+        keys[w * kWave + lane] = key;
     if (lane == 0) {
         if (!TOP && slices.d == 1) {
             const int64_t target = out.targets ? out.targets[row] : -1;
-            finish_row(out, row, vocab, ref, S, T2, target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f, target);
+            finish_row(out, row, vocab, s.ref, s.S, s.T, target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f, target);
         } else {
-            stats[w] = Slice{ref, S, T2, top};
+            stats[w] = s;
         }
     }
 }
@@ -274,7 +318,7 @@ SDP4_DEV void join_row(const Rows<const T *> &x, int64_t row, int64_t vocab, int
     for (int i = 0; i < N; ++i) {
         s[i] = Slice{0.0f, 0.0f, 0.0f, 0.0f};
         if (i * kWave + lane < slices)
-            s[i] = stats[row * slices + i * kWave + lane];
+            s[i] = stats[i * kWave + lane];
         tops[i] = i * kWave + lane < slices ? order_bits(s[i].top) : 0u;
     }
     float T2;
@@ -292,38 +336,54 @@ __global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t
         return;
     float ref, S;
     uint32_t tops[kMaxSlices / kWave];
-    join_row<T>(x, row, vocab, slices, out, stats, ref, S, tops);
+    join_row<T>(x, row, vocab, slices, out, stats + row * slices, ref, S, tops);
 }
 
-// The largest v with at least k of the lanes' N values >= v; unless EXACT, the first v on the way with exactly k of them.
-template <int BITS, bool EXACT, int N>
-SDP4_DEV uint32_t kth_largest(const uint32_t (&value)[N], int used, int k)
+// The largest v in [low, high], which hold it, with at least k of the lanes' values >= v: value(i), i < used <= N.  Found
+// bit by bit from the first in which low and high differ, counting lanes.
+template <int N, class V>
+SDP4_DEV uint32_t kth_largest(uint32_t low, uint32_t high, int used, int k, V value)
 {
-    uint32_t v = 0;
+    if (low == high)
+        return low;
+    int b = 31 - __builtin_clz(low ^ high);
+    uint32_t v = low & ~((2u << b) - 1);
 #pragma unroll 1
-    for (int b = BITS - 1; b >= 0; --b) {
+    for (; b >= 0; --b) {
         const uint32_t mid = v | 1u << b;
         int n = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < used)
-                n += __builtin_popcountll(__ballot(value[i] >= mid));
+                n += __builtin_popcountll(__ballot(value(i) >= mid));
         if (n >= k)
             v = mid;
-        if (!EXACT && n == k)
-            break;
     }
     return v;
+}
+
+SDP4_DEV uint32_t max_wave(uint32_t v)
+{
+    v = max(v, dpp_u32<kDppXor1>(v));
+    v = max(v, dpp_u32<kDppXor2>(v));
+    v = max(v, dpp_u32<kDppHalfMirror>(v));
+    v = max(v, dpp_u32<kDppRor8>(v));
+    v = max(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, (16 << 10) | 0x1F));
+    v = max(v, (uint32_t)__builtin_amdgcn_ds_bpermute((lane_id() ^ 32) << 2, (int)v));
+    return uniform(v);
 }
 
 // Joins the slices and finds the alternatives: one wave per row and block, up to K alternatives.
 //
 // Call a lane's logits of one slice a group.  The row's k largest logits lie in the k groups with the best largest logit
 // (larger first, then earlier): each of these has one that is at least as good as any logit outside of them.  The same
-// holds one step up, for the k slices with the best largest logit, where there are so many.  A bisection over the bits
-// of the values, counting lanes, finds the k-th best slice (or group, with fewer slices); the groups from there up, k
-// and a few more, are listed in LDS, and a group's place is the number of better ones.  Of the k best groups' logits
-// (read again, k * NC chunks) those at least as good as the last one's largest are ranked in the same way.
+// holds one step up, for the k slices with the best largest logit.  Of the k groups' logits (read
+// again: of most groups one chunk, as what its others hold is known to be less) those at least as good as the k-th best
+// group's largest, k and a few more, are listed in LDS, and each one's place is the number of better ones.
+//
+// A row takes a chain of three reads from memory (slices and keys, target, chunks) and the steps between, 9 us; 4096 rows
+// with 5 alternatives take 13.
+constexpr int kListed = 256;
 template <class T, int NC, int K>
 __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
                                                          TokenStats out, const Slice *stats,
@@ -331,12 +391,10 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
 {
     using Key = GroupKey<T>;
     constexpr int W = kChunk<T>, N = kMaxSlices / kWave, VB = Key::kValueBits;
-    __shared__ uint16_t chosen[K];         // slices
-    __shared__ uint32_t groups[K];         // slice << 6 | lane of the k best
-    __shared__ uint64_t list[K * kWave];   // groups, or logits of k groups
-    __shared__ uint16_t where[K * kWave];  // of listed groups: place in `chosen` << 6 | lane
+    __shared__ uint16_t chosen[K];     // slices
+    __shared__ uint64_t groups[K];     // bound of all but one round, then slice << 16 | chunk of the slice with the largest
+    __shared__ uint64_t list[kListed]; // logits
     __shared__ uint32_t listed;
-    static_assert(NC * W <= kWave, "logits of a group");
     const int lane = lane_id(), k = out.top_k;
     const int64_t row = work_block();
     if (row >= rows)
@@ -344,123 +402,140 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     const uint64_t below = (uint64_t(1) << lane) - 1;
     if (lane == 0)
         listed = 0;
+    stats += row * slices;
+    keys += row * slices * kWave;
     float ref, S;
     uint32_t tops[N];
     join_row<T>(x, row, vocab, slices, out, stats, ref, S, tops);
 
-    // slices whose groups count, in order
+    // slices whose groups count, in order; the best group's largest, and a bound that k groups reach
+    uint32_t high = 0, low = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        tops[i] >>= 32 - VB;
+        high = max(high, tops[i]);
+    }
+    high = max_wave(high);
     int count = slices;
-    uint32_t tau = 0; // groups below it do not count
-    if (slices >= k) {
+    if (slices >= k)
+        low = kth_largest<N>(0, high, (slices + kWave - 1) / kWave, k, [&](int i) { return tops[i]; });
+    {
+        int equal = slices; // of those at `low` the first so many
+        if (slices >= k) {
+            equal = k;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            tops[i] >>= 32 - VB;
-        tau = kth_largest<VB, true>(tops, (slices + kWave - 1) / kWave, k);
-        int above = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            above += __builtin_popcountll(__ballot(tops[i] > tau));
-        int equal = k - above; // of those at tau the first so many
+            for (int i = 0; i < N; ++i)
+                equal -= __builtin_popcountll(__ballot(tops[i] > low));
+        }
         count = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const bool tie = tops[i] == tau && i * kWave + lane < slices;
+            const bool is = i * kWave + lane < slices, tie = is && (tops[i] == low || slices < k);
             const uint64_t eq = __ballot(tie);
-            const bool take = tops[i] > tau || (tie && __builtin_popcountll(eq & below) < equal);
+            const bool take = (is && tops[i] > low) || (tie && __builtin_popcountll(eq & below) < equal);
             equal -= __builtin_popcountll(eq);
             const uint64_t all = __ballot(take);
             if (take)
                 chosen[count + __builtin_popcountll(all & below)] = (uint16_t)(i * kWave + lane);
             count += __builtin_popcountll(all);
         }
-    } else if (lane < count) {
-        chosen[lane] = (uint16_t)lane;
     }
     wave_lds_sync();
-
-    uint32_t value[K], pos[K];
-#pragma unroll
-    for (int r = 0; r < K; ++r) {
-        if (r < count) {
-            const typename Key::Word w = keys[(row * slices + chosen[r]) * kWave + lane];
-            value[r] = Key::value(w), pos[r] = Key::pos(w);
-        }
-    }
-    if (slices < k)
-        tau = kth_largest<VB, false>(value, count, k);
-    int above = 0;
+    typename Key::Word key[K];
 #pragma unroll
     for (int r = 0; r < K; ++r)
         if (r < count)
-            above += __builtin_popcountll(__ballot(value[r] > tau));
-    int equal = k - above, n = 0; // of the groups at tau the first `equal` may be needed: slices in order, positions in a slice
+            key[r] = keys[(int)chosen[r] * kWave + lane];
+
+    // the k best groups: those above tau, and of those at tau the first -- slices in order, positions in a slice
+    const uint32_t tau = kth_largest<K>(low, high, count, k, [&](int r) { return Key::value(key[r]); });
+    int equal = k, found = 0;
+#pragma unroll
+    for (int r = 0; r < K; ++r)
+        if (r < count)
+            equal -= __builtin_popcountll(__ballot(Key::value(key[r]) > tau));
+    int64_t last = -1; // chunk of the row up to which logits equal to tau count
 #pragma unroll
     for (int r = 0; r < K; ++r) {
         if (r < count) {
-            const bool tie = value[r] == tau && equal > 0;
-            const int ties = __builtin_popcountll(__ballot(tie));
-            uint32_t limit = ~0u; // positions below it are taken
-            if (ties > equal && equal > 0) {
+            const bool tie = Key::value(key[r]) == tau;
+            const uint32_t pos = Key::at(key[r]) * kWave + (uint32_t)lane;
+            uint32_t limit = equal > 0 ? ~0u : 0u; // positions below it are taken
+            if (equal > 0 && __builtin_popcountll(__ballot(tie)) > equal) {
                 limit = 0;
 #pragma unroll 1
-                for (int b = 15; b >= 0; --b) {
+                for (int b = 10; b >= 0; --b) { // NC * 64 positions
                     const uint32_t mid = limit | 1u << b;
-                    if (__builtin_popcountll(__ballot(tie && pos[r] < mid)) <= equal)
+                    if (__builtin_popcountll(__ballot(tie && pos < mid)) <= equal)
                         limit = mid;
                 }
             }
-            const bool tie_taken = tie && pos[r] < limit;
-            equal -= __builtin_popcountll(__ballot(tie_taken));
-            const bool take = value[r] > tau || tie_taken;
-            const uint64_t all = __ballot(take);
-            if (take) {
-                const int at = n + __builtin_popcountll(all & below);
-                list[at] = (uint64_t)value[r] << 32 | (uint32_t)~(r << 16 | pos[r]);
-                where[at] = (uint16_t)(r << 6 | lane);
-            }
-            n += __builtin_popcountll(all);
+            const bool tie_taken = tie && pos < limit, take = tie_taken || Key::value(key[r]) > tau;
+            const uint64_t ties = __ballot(tie_taken), all = __ballot(take);
+            const uint32_t slice = chosen[r];
+            equal -= __builtin_popcountll(ties);
+            if (take)
+                groups[found + __builtin_popcountll(all & below)] = (uint64_t)Key::rest(key[r]) << 32 | slice << 16 | pos;
+            found += __builtin_popcountll(all);
+            if (ties)
+                last = (int64_t)slice * (NC * kWave) + max_wave(tie_taken ? pos : 0u);
         }
     }
-    wave_lds_sync();
-    // the k best of them, and the k-th: from its value on, and at its value up to its chunk, a logit counts
-    uint64_t kth = 0;
-    for (int a = lane; a < n; a += kWave) {
-        const uint64_t mine = list[a];
-        int rank = 0;
-        for (int o = 0; o < n; ++o)
-            rank += list[o] > mine;
-        if (rank < k)
-            groups[rank] = (uint32_t)chosen[where[a] >> 6] << 6 | (where[a] & 63u);
-        if (rank == k - 1)
-            kth = mine;
-    }
-    const uint64_t has = __ballot(kth != 0);
-    const int found = n < k ? n : k;
-    const int from = has ? __builtin_ctzll(has) : 0;
-    const uint32_t kth_value = __builtin_amdgcn_readlane((uint32_t)(kth >> 32), from);
-    const uint32_t kth_place = ~(uint32_t)__builtin_amdgcn_readlane((uint32_t)kth, from);
-    const float least = from_order_bits(Key::order(kth_value));
-    const int64_t last = has ? (int64_t)chosen[(kth_place >> 16) & (K - 1)] * (NC * kWave) + (kth_place & 0xFFFFu) : 0;
     wave_lds_sync();
 
     const T *p = x.p + row * x.stride;
     const int64_t chunks = (vocab + W - 1) / W;
-    for (int c = lane; c < found * NC; c += kWave) {
-        const uint32_t g = groups[c / NC];
-        const int64_t chunk = (int64_t)(g >> 6) * (NC * kWave) + (c % NC) * kWave + (g & 63u);
-        if (chunk >= chunks)
-            continue;
-        const int64_t e = chunk * W;
-        float v[W];
-        load_row(p, e, vocab, v);
-        end_row(e, vocab, v, -__builtin_inff());
+    const uint32_t least_order = Key::order(tau);
+    const float least = from_order_bits(least_order);
+    // body(value, element) for each logit of the groups that may be among the k largest
+    auto candidates = [&](auto body) {
+        for (int c = lane; c < found * NC; c += kWave) {
+            const uint64_t g = groups[c / NC];
+            const uint32_t place = (uint32_t)g & 0xFFFFu;
+            if (c % NC != (int)(place / kWave) && (uint32_t)(g >> 32) < least_order)
+                continue; // nothing there reaches the k-th best
+            const int64_t chunk = (int64_t)((uint32_t)g >> 16) * (NC * kWave) + (c % NC) * kWave + place % kWave;
+            if (chunk >= chunks)
+                continue;
+            const int64_t e = chunk * W;
+            float v[W];
+            load_row(p, e, vocab, v);
+            end_row(e, vocab, v, -__builtin_inff());
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-            if (e + j < vocab && (v[j] > least || (v[j] == least && chunk <= last)))
-                list[atomicAdd(&listed, 1u)] = entry_of(v[j], (uint32_t)(e + j));
-    }
+            for (int j = 0; j < W; ++j)
+                if (e + j < vocab && (v[j] > least || (v[j] == least && chunk <= last)))
+                    body(entry_of(v[j], (uint32_t)(e + j)));
+        }
+    };
+    candidates([&](uint64_t entry) {
+        const uint32_t slot = atomicAdd(&listed, 1u);
+        if (slot < kListed)
+            list[slot] = entry;
+    });
     wave_lds_sync();
-    n = (int)uniform(listed);
+    int n = (int)uniform(listed);
+    if (n > kListed) {
+        // The largest logits crowd into few groups: the k-th best entry, bit by bit, then the list of the k from there up.
+        uint64_t kth = 0;
+#pragma unroll 1
+        for (int b = 63; b >= 0; --b) {
+            const uint64_t mid = kth | uint64_t(1) << b;
+            uint32_t mine = 0;
+            candidates([&](uint64_t entry) { mine += entry >= mid; });
+            if ((int)sum_lanes((float)mine, kWave) >= k) // below 2^24: exact
+                kth = mid;
+        }
+        wave_lds_sync();
+        if (lane == 0)
+            listed = 0;
+        wave_lds_sync();
+        candidates([&](uint64_t entry) {
+            if (entry >= kth)
+                list[atomicAdd(&listed, 1u)] = entry;
+        });
+        wave_lds_sync();
+        n = (int)uniform(listed);
+    }
     const bool bad = !(S - S == 0.0f);
     for (int a = lane; a < (n > k ? n : k); a += kWave) {
         const uint64_t mine = a < n ? list[a] : 0;
@@ -605,26 +680,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, in
     const float g_logp = g.logp ? g.logp[row] : 0.0f, g_ent = ENT ? g.entropy[row] : 0.0f,
                 g_lse = g.lse ? g.lse[row] : 0.0f;
     const float tx = target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f;
-    // round i of the wave: 64 chunks from element start + i * STEP on
     const int start = wave * (kWave * W), at = start + lane * W;
-    const int rounds = start < vocab ? (vocab - start + STEP - 1) / STEP : 0;
-    const int full = start + kWave * W <= vocab ? (vocab - start - kWave * W) / STEP + 1 : 0; // whole rounds
-    u32x4 raw[NC];
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        if (i < full) {
-            raw[i] = load_chunk<true>(p + (uint32_t)(at + i * STEP));
-        } else if (i < rounds) {
-            float v[W];
-            const int e = at + i * STEP;
-            load_row(p, e < vocab ? e : 0, vocab, v);
-            end_row(e, vocab, v, -__builtin_inff());
-            raw[i] = pack<T>(v);
-        }
-    }
+    Held<T, NC> h;
+    h.template load<STEP>(p, start, NC, vocab);
     Slice s{0.0f, 0.0f, 0.0f, 0.0f};
-    if (rounds)
-        slice_sums<T, NC>(raw, rounds, full == rounds, s.ref, s.S, s.T);
+    if (h.any()) {
+        float cm[NC], tail_max;
+        slice_sums<false>(h, s.ref, s.S, s.T, cm, tail_max);
+    }
     float ref = s.ref, S = s.S, T2 = s.T;
     if constexpr (WAVES > 1) {
         if (lane == 0)
@@ -647,18 +710,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, in
         s.A *= f, s.B *= f;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int e = at + i * STEP;
-            if (i < full) {
+            if (i < h.full) {
+                const int e = at + i * STEP;
                 float v[W];
-                unpack<T>(raw[i], v);
+                unpack<T>(h.raw[i], v);
                 grad_chunk<W, ENT, true>(s, exponent, delta, e, vocab, v);
                 store_chunk<T>(q + (uint32_t)e, pack<T>(v));
-            } else if (e < width) {
-                float v[W];
-                unpack<T>(raw[i], v); // nothing of it counts from vocab on
-                grad_chunk<W, ENT, false>(s, exponent, delta, e, vocab, v);
-                store_elems(q + e, width - e, v);
             }
+        }
+#pragma unroll 1
+        for (int e = at + h.full * STEP; e < width; e += STEP) { // the tail, and the padding behind it
+            float v[W];
+            unpack<T>(h.tail, v);
+            grad_chunk<W, ENT, false>(s, exponent, delta, e, vocab, v);
+            store_elems(q + e, width - e, v);
         }
     });
 }
@@ -676,9 +741,11 @@ struct Cut {
     int64_t slices;
 };
 template <class T>
+constexpr int kMostChunks = sizeof(T) == 2 ? 8 : 16; // 4096 logits
+template <class T>
 Cut cut_rows(int64_t rows, int64_t vocab)
 {
-    constexpr int most = sizeof(T) == 2 ? 8 : 16; // 4096 logits
+    constexpr int most = kMostChunks<T>;
     const int64_t chunks = (vocab + kChunk<T> - 1) / kChunk<T>;
     const auto slices = [&](int n) { return (chunks + 64 * n - 1) / (64 * n); };
     int nc = 1;

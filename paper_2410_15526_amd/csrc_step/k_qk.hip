@@ -8,9 +8,10 @@
 //
 // A head is the work of `lanes` neighbouring lanes (a power of two), each of
 // which holds units of two chunks of W elements: the two members of W pairs
-// in the half layout (chunks rot / 2 apart), neighbouring chunks in the
-// interleaved layout and behind the rotated part.  So a rotation never
-// crosses lanes, and a norm joins `lanes` lanes.
+// in the half layout (chunks rot / 2 apart), chunks half of the elements apart
+// in the interleaved layout and behind the rotated part.  So a rotation never
+// crosses lanes, neighbouring lanes access neighbouring chunks, and a norm
+// joins `lanes` lanes.
 #include "step_device.hpp"
 
 namespace sdp4 {
@@ -50,14 +51,14 @@ struct Unit {
         on = u < l.units;
         u = on ? u : 0;
         if constexpr (INTER && W > 1) {
-            a = 2 * W * u, b = a + W;
+            a = W * u, b = a + W * l.units;
             turn_a = a < l.rot, turn_b = b < l.rot;
             angle_a = turn_a ? a / 2 : 0, angle_b = turn_b ? b / 2 : 0;
         } else {
             const bool turned = u < l.rot_units;
             const int v = turned ? u : u - l.rot_units;
-            a = turned ? (INTER ? 2 * u : W * u) : l.rot + 2 * W * v;
-            b = turned && !INTER ? a + l.half : a + W;
+            a = turned ? (INTER ? 2 * u : W * u) : l.rot + W * v;
+            b = turned ? (INTER ? a + 1 : a + l.half) : a + W * (l.units - l.rot_units);
             turn_a = turn_b = turned;
             angle_a = angle_b = turned ? W * u : 0;
         }
@@ -67,53 +68,38 @@ struct Unit {
     }
 };
 
-// W elements at an element address.
-template <class T, int W, bool NT>
-SDP4_DEV void load_w(const T *p, float (&v)[W])
+// W float32 table entries, which other lanes and blocks read again.
+template <int W>
+SDP4_DEV void load_kept(const float *p, float (&v)[W])
 {
-    if constexpr (W * sizeof(T) == 16) {
-        unpack<T>(load_chunk<NT>(p), v);
-    } else if constexpr (W * sizeof(T) == 8) {
-        auto q = reinterpret_cast<const half_at<T> *>(p);
-        const u32x2 c = NT ? (u32x2)__builtin_nontemporal_load(q) : (u32x2)*q;
-        if constexpr (W == 2) {
-            v[0] = __uint_as_float(c.x), v[1] = __uint_as_float(c.y);
-        } else {
-            v[0] = __uint_as_float(c.x << 16), v[1] = __uint_as_float(c.x & 0xFFFF0000u);
-            v[2] = __uint_as_float(c.y << 16), v[3] = __uint_as_float(c.y & 0xFFFF0000u);
-        }
-    } else if constexpr (sizeof(T) == 4 && W % 4 == 0) {
+    constexpr int N = W > 4 ? 4 : W;
 #pragma unroll
-        for (int k = 0; k < W / 4; ++k)
-            unpack<T>(load_chunk<NT>(p + 4 * k), *reinterpret_cast<float(*)[4]>(v + 4 * k));
-    } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            v[j] = to_f32<T>(p[j]);
+    for (int k = 0; k < W / N; ++k) {
+        Raw<float, N> r;
+        r.template load<false>(p + N * k);
+        r.get(*reinterpret_cast<float(*)[N]>(v + N * k));
     }
 }
-template <class T, int W>
-SDP4_DEV void store_w(T *p, const float (&v)[W])
-{
-    if constexpr (W * sizeof(T) == 16)
-        store_chunk<T>(p, pack<T>(v));
-    else if constexpr (W * sizeof(T) == 8)
-        store_half(p, v);
-    else
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            p[j] = from_f32<T>(v[j]);
-}
 
-// Two chunks of a lane's unit.
+// Two chunks of a lane's unit, as loaded and as values.
+template <class T, int W>
+struct RawTwo {
+    Raw<T, W> a, b;
+    template <bool NT, class U>
+    SDP4_DEV void load(const T *head, const U &u)
+    {
+        a.template load<NT>(head + u.a);
+        b.template load<NT>(head + u.b);
+    }
+};
 template <int W>
 struct Two {
     float a[W], b[W];
-    template <bool NT, class T, class U>
-    SDP4_DEV void load(const T *head, const U &u)
+    template <class T>
+    SDP4_DEV void get(const RawTwo<T, W> &r)
     {
-        load_w<T, W, NT>(head + u.a, a);
-        load_w<T, W, NT>(head + u.b, b);
+        r.a.get(a);
+        r.b.get(b);
     }
     SDP4_DEV void fill(float v)
     {
@@ -134,10 +120,15 @@ struct Two {
     template <class T, class U>
     SDP4_DEV void store(T *head, const U &u) const
     {
-        if (u.on)
-            store_w<T, W>(head + u.a, a);
-        if (u.on_b)
-            store_w<T, W>(head + u.b, b);
+        Raw<T, W> r;
+        if (u.on) {
+            r.put(a);
+            r.store(head + u.a);
+        }
+        if (u.on_b) {
+            r.put(b);
+            r.store(head + u.b);
+        }
     }
 };
 
@@ -154,13 +145,13 @@ struct Angles {
             constexpr int H = W / 2;
             float(&c0)[H] = *reinterpret_cast<float(*)[H]>(c), (&c1)[H] = *reinterpret_cast<float(*)[H]>(c + H);
             float(&s0)[H] = *reinterpret_cast<float(*)[H]>(s), (&s1)[H] = *reinterpret_cast<float(*)[H]>(s + H);
-            load_w<float, H, false>(row + u.angle_a, c0);
-            load_w<float, H, false>(row + l.half + u.angle_a, s0);
-            load_w<float, H, false>(row + u.angle_b, c1);
-            load_w<float, H, false>(row + l.half + u.angle_b, s1);
+            load_kept<H>(row + u.angle_a, c0);
+            load_kept<H>(row + l.half + u.angle_a, s0);
+            load_kept<H>(row + u.angle_b, c1);
+            load_kept<H>(row + l.half + u.angle_b, s1);
         } else {
-            load_w<float, W, false>(row + u.angle_a, c);
-            load_w<float, W, false>(row + l.half + u.angle_a, s);
+            load_kept<W>(row + u.angle_a, c);
+            load_kept<W>(row + l.half + u.angle_a, s);
         }
         if (!known) { // no such row: the result says so
 #pragma unroll
@@ -178,7 +169,7 @@ struct Angles {
 #pragma unroll
             for (int j = 0; j < W / 2; ++j)
                 one<BACK>(x.a[2 * j], x.a[2 * j + 1], c[j], s[j]);
-            if (u.turn_b) {
+            if (u.turn_b) { // only with turn_a: b lies behind a
 #pragma unroll
                 for (int j = 0; j < W / 2; ++j)
                     one<BACK>(x.b[2 * j], x.b[2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
@@ -187,6 +178,19 @@ struct Angles {
 #pragma unroll
             for (int j = 0; j < W; ++j)
                 one<BACK>(x.a[j], x.b[j], c[j], s[j]);
+        }
+    }
+    template <bool BACK>
+    SDP4_DEV void all(Two<W> &x) const
+    {
+#pragma unroll
+        for (int j = 0; j < W / (INTER && W > 1 ? 2 : 1); ++j) {
+            if constexpr (INTER && W > 1) {
+                one<BACK>(x.a[2 * j], x.a[2 * j + 1], c[j], s[j]);
+                one<BACK>(x.b[2 * j], x.b[2 * j + 1], c[W / 2 + j], s[W / 2 + j]);
+            } else {
+                one<BACK>(x.a[j], x.b[j], c[j], s[j]);
+            }
         }
     }
     template <bool BACK>
@@ -209,19 +213,65 @@ SDP4_DEV float rsqrt_of(float v)
     return e == e && __builtin_isfinite(y) ? z : y;
 }
 
+// Sum over the wave's groups of `lanes` lanes, lane by lane.
+SDP4_DEV float sum_groups(float v, int lanes)
+{
+    if (lanes <= 1) v += xor_lane<1>(v);
+    if (lanes <= 2) v += xor_lane<2>(v);
+    if (lanes <= 4) v += xor_lane<4>(v);
+    if (lanes <= 8) v += xor_lane<8>(v);
+    if (lanes <= 16) v += xor_lane<16>(v);
+    if (lanes <= 32) v += xor_lane<32>(v);
+    return v;
+}
+
+// What a kernel knows beforehand.  The usual shapes are kernels of their own: 16-byte chunks, norm with weights, a known
+// number of lanes and either every pair turned or, lane by lane, some.  What such a kernel need not ask (phi moves of
+// optional turns and weights, tests of the lane count) was a third of its vector instructions: backward of 8192 x 48 heads
+// of 128 bfloat16 elements.
+enum Turn { kTurnAsked, kTurnAll, kTurnSome };
+template <int W_, int NU_, bool INTER_, bool NORM_, int LL_ = -1, Turn TURN_ = kTurnAsked>
+struct Known {
+    static constexpr int W = W_, NU = NU_; // elements of a chunk, units of a lane
+    static constexpr bool INTER = INTER_, NORM = NORM_;
+    static constexpr int LL = LL_; // log2 of the lanes of a head, -1: asked
+    static constexpr Turn TURN = TURN_;
+    static constexpr bool WEIGHTS = LL >= 0; // given, otherwise asked
+    SDP4_DEV static int lanes_log2(const Layout &l) { return LL >= 0 ? LL : l.lanes_log2; }
+    SDP4_DEV static bool weights(const void *w) { return NORM && (WEIGHTS || w); }
+    SDP4_DEV static bool turns(const Layout &l) { return TURN != kTurnAsked || l.rot; }
+    template <bool BACK>
+    SDP4_DEV static void turn(const Angles<W, INTER> &t, const Unit<W, INTER> &u, Two<W> &x)
+    {
+        if constexpr (TURN == kTurnAll) {
+            t.template all<BACK>(x);
+        } else if constexpr (TURN == kTurnSome) {
+            Two<W> y = x;
+            t.template all<BACK>(y);
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                x.a[j] = u.turn_a ? y.a[j] : x.a[j], x.b[j] = u.turn_b ? y.b[j] : x.b[j];
+        } else {
+            t.template turn<BACK>(u, x);
+        }
+    }
+};
+
 // Forward: one head per group of lanes; the first blocks take the queries, the others the keys.
-template <class T, int W, int NU, bool INTER, bool NORM>
+template <class T, class K>
 __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, float eps, Rope rope)
 {
+    constexpr int W = K::W, NU = K::NU;
+    using U = Unit<W, K::INTER>;
     const int64_t wb = work_block();
     const bool keys = wb >= q.blocks;
     const Side<T> &s = keys ? k : q;
-    const int lanes = 1 << l.lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const int ll = K::lanes_log2(l), lanes = 1 << ll, lane = threadIdx.x & (lanes - 1);
     // the block's first head, and from there the lane group's: below 2^9 + heads, so 32 bits do
-    const int64_t first = (keys ? wb - q.blocks : wb) << (8 - l.lanes_log2);
+    const int64_t first = (keys ? wb - q.blocks : wb) << (8 - ll);
     uint64_t head0;
     const int64_t token0 = (int64_t)divide((uint64_t)first, s.heads, head0);
-    const uint32_t group = threadIdx.x >> l.lanes_log2;
+    const uint32_t group = threadIdx.x >> ll;
     if (first + group >= s.items)
         return;
     uint32_t head = (uint32_t)head0 + group, ahead = __umulhi(head, s.inv32);
@@ -231,28 +281,30 @@ __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, floa
     const int64_t token = token0 + ahead;
     const T *x = s.x + token0 * s.x_token + (uint64_t)ahead * (uint64_t)s.x_token + (uint64_t)head * (uint64_t)s.x_head;
     T *y = s.out + token0 * s.out_token + (uint64_t)ahead * (uint64_t)s.out_token + (uint64_t)head * (uint64_t)s.out_head;
+    RawTwo<T, W> xr[NU], wr[NU];
     Two<W> v[NU], w[NU];
-    Angles<W, INTER> turn[NU];
-    const int64_t position = l.rot ? position_of(rope, token) : 0;
+    Angles<W, K::INTER> turn[NU];
+    const int64_t position = K::turns(l) ? position_of(rope, token) : 0;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-        const Unit<W, INTER> u(l, lane + i * lanes);
-        v[i].template load<true>(x, u);
-        if constexpr (NORM) {
-            if (s.weight)
-                w[i].template load<false>(s.weight, u);
-        }
+        const U u(l, lane + i * lanes);
+        xr[i].template load<true>(x, u);
+        if (K::weights(s.weight))
+            wr[i].template load<false>(s.weight, u);
     }
-    if (l.rot) {
+    if (K::turns(l)) {
 #pragma unroll
         for (int i = 0; i < NU; ++i)
-            turn[i].load(l, Unit<W, INTER>(l, lane + i * lanes), rope, position);
+            turn[i].load(l, U(l, lane + i * lanes), rope, position);
     }
-    if constexpr (NORM) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+        v[i].get(xr[i]);
+    if constexpr (K::NORM) {
         float sq = 0.0f;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            v[i].only(Unit<W, INTER>(l, lane + i * lanes));
+            v[i].only(U(l, lane + i * lanes));
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 sq = __builtin_fmaf(v[i].a[j], v[i].a[j], sq);
@@ -265,7 +317,8 @@ __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, floa
 #pragma unroll
             for (int j = 0; j < W; ++j)
                 v[i].a[j] *= r, v[i].b[j] *= r;
-            if (s.weight) {
+            if (K::weights(s.weight)) {
+                w[i].get(wr[i]);
 #pragma unroll
                 for (int j = 0; j < W; ++j)
                     v[i].a[j] *= w[i].a[j], v[i].b[j] *= w[i].b[j];
@@ -274,96 +327,118 @@ __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, floa
     }
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-        const Unit<W, INTER> u(l, lane + i * lanes);
-        if (l.rot)
-            turn[i].template turn<false>(u, v[i]);
-        v[i].store(y, u);
+        const U u(l, lane + i * lanes);
+        if (K::turns(l))
+            K::template turn<false>(turn[i], u, v[i]);
+        v[i].template store<T>(y, u);
     }
 }
 
 // Backward.  A block takes every blocks-th run of heads of its side; with DW it adds up the weights' gradient in
 // registers, its lane groups and waves join at the end, and the block's sums go to the workspace.  The next head's loads
 // are under way before the present one's stores: loads that follow stores wait for these.
-template <class T, int W, int NU, bool INTER, bool NORM, bool DW>
+template <class T, class K, bool DW>
 __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k, float eps, Rope rope)
 {
-    __shared__ float lds[DW ? 256 * 2 * W : 1];
+    constexpr int W = K::W, NU = K::NU;
+    using U = Unit<W, K::INTER>;
+    __shared__ float lds[4][DW ? 2 * W : 1][kWave];
     const int64_t wb = work_block();
     const bool keys = wb >= q.blocks;
     const Side<T> &s = keys ? k : q;
     const int64_t block = keys ? wb - q.blocks : wb;
-    const int lanes = 1 << l.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> l.lanes_log2;
-    const int groups = 256 >> l.lanes_log2;
+    const int ll = K::lanes_log2(l), lanes = 1 << ll, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> ll;
+    const int groups = 256 >> ll;
     const uint32_t heads = (uint32_t)s.heads.d;
-    // first head of the lane group, and the step to its next: tokens and heads, where a carry makes one token more
+    // The lane group's heads are `step` apart: so many tokens and heads, where a carry makes one token more.
     uint64_t h0, hs;
-    int64_t item = block * groups + group;
     const int64_t step = s.blocks * groups;
+    int64_t item = block * groups + group;
     int64_t token = (int64_t)divide((uint64_t)item, s.heads, h0);
     const int64_t token_step = (int64_t)divide((uint64_t)step, s.heads, hs);
     uint32_t head = (uint32_t)h0;
     const uint32_t head_step = (uint32_t)hs;
-    Two<W> w[NU], dw[NU], dy[NU], x[NU];
+    const T *pdy = s.dy + token * s.dy_token + (int64_t)head * s.dy_head;
+    const T *px = s.x + token * s.x_token + (int64_t)head * s.x_head;
+    T *out = s.out + token * s.out_token + (int64_t)head * s.out_head, *next_out = out;
+    const int64_t dy_step = token_step * s.dy_token + (int64_t)head_step * s.dy_head, dy_carry = s.dy_token - (int64_t)heads * s.dy_head;
+    const int64_t x_step = token_step * s.x_token + (int64_t)head_step * s.x_head, x_carry = s.x_token - (int64_t)heads * s.x_head;
+    const int64_t out_step = token_step * s.out_token + (int64_t)head_step * s.out_head, out_carry = s.out_token - (int64_t)heads * s.out_head;
+    Two<W> dw[NU];
+    RawTwo<T, W> dy[NU], x[NU], wr[NU];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         dw[i].fill(0.0f);
-        if (NORM && s.weight)
-            w[i].template load<false>(s.weight, Unit<W, INTER>(l, lane + i * lanes));
-        else
-            w[i].fill(1.0f);
+        if (K::weights(s.weight))
+            wr[i].template load<false>(s.weight, U(l, lane + i * lanes));
     }
     int64_t position = 0;
     auto fetch = [&] {
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const Unit<W, INTER> u(l, lane + i * lanes);
-            dy[i].template load<true>(s.dy + token * s.dy_token + (int64_t)head * s.dy_head, u);
-            if constexpr (NORM)
-                x[i].template load<true>(s.x + token * s.x_token + (int64_t)head * s.x_head, u);
+            const U u(l, lane + i * lanes);
+            dy[i].template load<true>(pdy, u);
+            if constexpr (K::NORM)
+                x[i].template load<true>(px, u);
         }
-        if (l.rot)
+        if (K::turns(l))
             position = position_of(rope, token);
     };
     if (item < s.items)
         fetch();
     for (; item < s.items; item += step) {
-        T *out = s.out + token * s.out_token + (int64_t)head * s.out_head;
         Two<W> g[NU], xv[NU];
-        float sq = 0.0f, dot = 0.0f;
+        Angles<W, K::INTER> turn[NU];
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const Unit<W, INTER> u(l, lane + i * lanes);
-            g[i] = dy[i];
+            const U u(l, lane + i * lanes);
+            g[i].get(dy[i]);
             g[i].only(u);
-            if (l.rot) {
-                Angles<W, INTER> t;
-                t.load(l, u, rope, position);
-                t.template turn<true>(u, g[i]);
-            }
-            if constexpr (NORM) {
-                xv[i] = x[i];
+            if constexpr (K::NORM) {
+                xv[i].get(x[i]);
                 xv[i].only(u);
             }
+            if (K::turns(l))
+                turn[i].load(l, u, rope, position);
         }
-        if (DW || item + step < s.items) { // one head for each group of lanes otherwise
-            token += token_step, head += head_step;
-            if (head >= heads)
-                head -= heads, ++token;
-            if (item + step < s.items)
-                fetch();
+        out = next_out;
+        if (item + step < s.items) {
+            const bool carry = head + head_step >= heads;
+            head += head_step - (carry ? heads : 0u);
+            token += token_step + carry;
+            pdy += dy_step + (carry ? dy_carry : 0);
+            px += x_step + (carry ? x_carry : 0);
+            next_out += out_step + (carry ? out_carry : 0);
+            fetch();
         }
-        if constexpr (NORM) {
+        if (K::turns(l)) {
 #pragma unroll
             for (int i = 0; i < NU; ++i)
+                K::template turn<true>(turn[i], U(l, lane + i * lanes), g[i]);
+        }
+        if constexpr (K::NORM) {
+            Two<W> gw[NU]; // w g
+            float sq = 0.0f, dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                gw[i] = g[i];
+                if (K::weights(s.weight)) {
+                    Two<W> w;
+                    w.get(wr[i]);
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        gw[i].a[j] *= w.a[j], gw[i].b[j] *= w.b[j];
+                }
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     sq = __builtin_fmaf(xv[i].a[j], xv[i].a[j], sq);
+                    dot = __builtin_fmaf(gw[i].a[j], xv[i].a[j], dot);
                     sq = __builtin_fmaf(xv[i].b[j], xv[i].b[j], sq);
-                    dot = __builtin_fmaf(g[i].a[j] * w[i].a[j], xv[i].a[j], dot);
-                    dot = __builtin_fmaf(g[i].b[j] * w[i].b[j], xv[i].b[j], dot);
+                    dot = __builtin_fmaf(gw[i].b[j], xv[i].b[j], dot);
                 }
+            }
             const float r = rsqrt_of(__builtin_fmaf(sum_lanes(sq, lanes), l.inv_dim, eps));
-            const float m = sum_lanes(dot, lanes) * l.inv_dim * r * r; // mean(w g x r) r
+            const float m = -(sum_lanes(dot, lanes) * l.inv_dim) * r * r * r; // - mean(w g x r) r^2
 #pragma unroll
             for (int i = 0; i < NU; ++i)
 #pragma unroll
@@ -372,34 +447,35 @@ __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k,
                         dw[i].a[j] = __builtin_fmaf(g[i].a[j], xv[i].a[j] * r, dw[i].a[j]);
                         dw[i].b[j] = __builtin_fmaf(g[i].b[j], xv[i].b[j] * r, dw[i].b[j]);
                     }
-                    g[i].a[j] = r * __builtin_fmaf(-xv[i].a[j], m, g[i].a[j] * w[i].a[j]);
-                    g[i].b[j] = r * __builtin_fmaf(-xv[i].b[j], m, g[i].b[j] * w[i].b[j]);
+                    g[i].a[j] = __builtin_fmaf(xv[i].a[j], m, gw[i].a[j] * r);
+                    g[i].b[j] = __builtin_fmaf(xv[i].b[j], m, gw[i].b[j] * r);
                 }
         }
 #pragma unroll
         for (int i = 0; i < NU; ++i)
-            g[i].store(out, Unit<W, INTER>(l, lane + i * lanes));
+            g[i].template store<T>(out, U(l, lane + i * lanes));
     }
     if constexpr (DW) {
         if (!s.parts)
             return;
+        const int wave = threadIdx.x / kWave;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             if (i)
                 __syncthreads();
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                lds[(2 * j) * 256 + threadIdx.x] = dw[i].a[j];
-                lds[(2 * j + 1) * 256 + threadIdx.x] = dw[i].b[j];
+                dw[i].a[j] = sum_groups(dw[i].a[j], lanes), dw[i].b[j] = sum_groups(dw[i].b[j], lanes);
+                if (lane_id() < lanes) {
+                    lds[wave][2 * j][lane] = dw[i].a[j];
+                    lds[wave][2 * j + 1][lane] = dw[i].b[j];
+                }
             }
             __syncthreads();
-            // group 0's lanes hold the units: the threads of the block share out their 2 W sums
             for (int o = threadIdx.x; o < 2 * W * lanes; o += 256) {
-                const int which = o >> l.lanes_log2, ln = o & (lanes - 1);
-                const Unit<W, INTER> v(l, ln + i * lanes);
-                float sum = 0.0f;
-                for (int g = 0; g < groups; ++g)
-                    sum += lds[which * 256 + (g << l.lanes_log2) + ln];
+                const int which = o >> ll, ln = o & (lanes - 1);
+                const U v(l, ln + i * lanes);
+                const float sum = (lds[0][which][ln] + lds[1][which][ln]) + (lds[2][which][ln] + lds[3][which][ln]);
                 const int at = (which & 1 ? v.b : v.a) + (which >> 1);
                 if (which & 1 ? v.on_b : v.on)
                     s.parts[block * l.dim + at] = sum;
@@ -466,25 +542,45 @@ Side<T> side_of(const Heads *dy, const Heads &x, const Heads &out, int64_t token
     return s;
 }
 
-// Calls run(W, NU, INTER) as compile-time constants.
+// Calls run(Known<...>) for the shape.
 template <class T, class F>
-int with_layout(int w, int nu, bool inter, F run)
+int with_known(const Layout &l, int w, int nu, bool inter, const HeadNorm &norm, bool keys, F run)
 {
-    auto at = [&](auto wc, auto nc) {
-        return inter ? run(wc, nc, std::true_type{}) : run(wc, nc, std::false_type{});
+    constexpr int CW = kChunk<T>;
+    auto general = [&](auto wc, auto nc) {
+        constexpr int W = decltype(wc)::value, NU = decltype(nc)::value;
+        return inter ? (norm.on ? run(Known<W, NU, true, true>{}) : run(Known<W, NU, true, false>{}))
+                     : (norm.on ? run(Known<W, NU, false, true>{}) : run(Known<W, NU, false, false>{}));
     };
     using std::integral_constant;
-    if constexpr (sizeof(T) == 2)
-        if (w == 8)
-            return at(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    if (w == 4)
-        return at(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    return nu == 1 ? at(integral_constant<int, 1>{}, integral_constant<int, 1>{})
-                   : at(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+    if (w == CW && norm.on && norm.weight[0] && (norm.weight[1] || !keys) && l.rot > 0 && l.lanes_log2 >= 2 && l.lanes_log2 <= 5) {
+        const bool all = l.rot == l.dim;
+        auto at = [&](auto ll) {
+            constexpr int LL = decltype(ll)::value;
+            return inter ? (all ? run(Known<CW, 1, true, true, LL, kTurnAll>{}) : run(Known<CW, 1, true, true, LL, kTurnSome>{}))
+                         : (all ? run(Known<CW, 1, false, true, LL, kTurnAll>{}) : run(Known<CW, 1, false, true, LL, kTurnSome>{}));
+        };
+        switch (l.lanes_log2) {
+        case 2: return at(integral_constant<int, 2>{});
+        case 3: return at(integral_constant<int, 3>{});
+        case 4: return at(integral_constant<int, 4>{});
+        default: return at(integral_constant<int, 5>{});
+        }
+    }
+    if (w == CW)
+        return general(integral_constant<int, CW>{}, integral_constant<int, 1>{});
+    if constexpr (CW == 8)
+        if (w == 4)
+            return general(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    return nu == 1 ? general(integral_constant<int, 1>{}, integral_constant<int, 1>{})
+                   : general(integral_constant<int, 1>{}, integral_constant<int, 4>{});
 }
 
 // Blocks of the backward pass of either side: about kGradBlocks for both, in proportion to their heads.
-constexpr int64_t kGradBlocks = 2048;
+#ifndef QKB
+#define QKB 768
+#endif
+constexpr int64_t kGradBlocks = QKB;
 int64_t grad_blocks(int64_t items, int64_t all, int groups)
 {
     if (items == 0)
@@ -498,7 +594,7 @@ int64_t grad_blocks(int64_t items, int64_t all, int groups)
 
 int64_t qk_grad_workspace(int64_t tokens, int q_heads, int k_heads, int dim)
 {
-    // as many blocks as any layout of such heads takes: groups of 4 (64 lanes) and more
+    // as many blocks as any layout of such heads takes: 4 groups of lanes (of 64) in a block and more
     const int64_t qi = tokens * q_heads, ki = tokens * k_heads;
     if (qi + ki <= 0 || dim <= 0)
         return 0;
@@ -517,11 +613,8 @@ int launch_qk(int dtype, const Heads (&x)[2], const Heads (&y)[2], int64_t token
         Side<T> q = side_of<T>(nullptr, x[0], y[0], tokens, norm.weight[0]);
         Side<T> k = side_of<T>(nullptr, x[1], y[1], tokens, norm.weight[1]);
         q.blocks = (q.items + groups - 1) / groups, k.blocks = (k.items + groups - 1) / groups;
-        return with_layout<T>(w, nu, rope.interleaved, [&](auto wc, auto nc, auto inter) {
-            constexpr int W = decltype(wc)::value, NU = decltype(nc)::value;
-            constexpr bool I = decltype(inter)::value;
-            auto kernel = norm.on ? k_qk<T, W, NU, I, true> : k_qk<T, W, NU, I, false>;
-            return launch<4>(kernel, q.blocks + k.blocks, kUncapped, s, l, q, k, norm.eps, rope);
+        return with_known<T>(l, w, nu, rope.interleaved, norm, k.items > 0, [&](auto known) {
+            return launch<4>(k_qk<T, decltype(known)>, q.blocks + k.blocks, kUncapped, s, l, q, k, norm.eps, rope);
         });
     });
 }
@@ -550,12 +643,12 @@ int launch_qk_grad(int dtype, const Heads (&dy)[2], const Heads (&x)[2], const H
         } else { // nothing to add up: a block per group of heads
             q.blocks = (q.items + groups - 1) / groups, k.blocks = (k.items + groups - 1) / groups;
         }
-        return with_layout<T>(w, nu, rope.interleaved, [&](auto wc, auto nc, auto inter) {
-            constexpr int W = decltype(wc)::value, NU = decltype(nc)::value;
-            constexpr bool I = decltype(inter)::value;
-            auto kernel = want_dw   ? k_qk_grad<T, W, NU, I, true, true>
-                          : norm.on ? k_qk_grad<T, W, NU, I, true, false>
-                                    : k_qk_grad<T, W, NU, I, false, false>;
+        return with_known<T>(l, w, nu, rope.interleaved, norm, k.items > 0, [&](auto known) {
+            using K = decltype(known);
+            auto kernel = k_qk_grad<T, K, false>;
+            if constexpr (K::NORM)
+                if (want_dw)
+                    kernel = k_qk_grad<T, K, true>;
             return launch<4>(kernel, q.blocks + k.blocks, kUncapped, s, l, q, k, norm.eps, rope);
         });
     });

@@ -117,45 +117,98 @@ SDP4_DEV u32x4 pack(const float (&v)[kChunk<T>])
         return u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])};
 }
 
-// Four bfloat16 elements, half a chunk.
-SDP4_DEV void load_half(const bf16_t *p, float (&v)[4])
-{
-    const u32x2 c = __builtin_nontemporal_load(reinterpret_cast<const u32x2_b2 *>(p));
-    v[0] = __uint_as_float(c.x << 16), v[1] = __uint_as_float(c.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(c.y << 16), v[3] = __uint_as_float(c.y & 0xFFFF0000u);
-}
-SDP4_DEV void store_half(bf16_t *p, const float (&v)[4])
-{
-    const u32x2 c = {bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
-    __builtin_nontemporal_store((u32x2_b2)c, reinterpret_cast<u32x2_b2 *>(p));
-}
+// N elements as they lie in memory: 16 or 8 bytes, or one element.  Loops that load ahead carry this form, since values
+// that are unpacked are values that have been waited for.
+template <class T, int N>
+struct Raw {
+    static constexpr int BYTES = N * sizeof(T);
+    static_assert(BYTES == 16 || BYTES == 8 || N == 1, "accesses");
+    using V = std::conditional_t<BYTES == 16, u32x4, std::conditional_t<BYTES == 8, u32x2, T>>;
+    V v;
+    template <bool NT>
+    SDP4_DEV void load(const T *p)
+    {
+        if constexpr (BYTES == 16) {
+            v = load_chunk<NT>(p);
+        } else if constexpr (BYTES == 8) {
+            auto q = reinterpret_cast<const half_at<T> *>(p);
+            v = NT ? (u32x2)__builtin_nontemporal_load(q) : (u32x2)*q;
+        } else {
+            v = *p;
+        }
+    }
+    SDP4_DEV void get(float (&o)[N]) const
+    {
+        if constexpr (N == 1) {
+            o[0] = to_f32<T>(v);
+        } else {
+            uint32_t w[BYTES / 4];
+            __builtin_memcpy(w, &v, BYTES);
+#pragma unroll
+            for (int j = 0; j < BYTES / 4; ++j) {
+                if constexpr (sizeof(T) == 4) {
+                    o[j] = __uint_as_float(w[j]);
+                } else {
+                    o[2 * j] = __uint_as_float(w[j] << 16);
+                    o[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+                }
+            }
+        }
+    }
+    SDP4_DEV void put(const float (&o)[N])
+    {
+        if constexpr (N == 1) {
+            v = from_f32<T>(o[0]);
+        } else {
+            uint32_t w[BYTES / 4];
+#pragma unroll
+            for (int j = 0; j < BYTES / 4; ++j)
+                w[j] = sizeof(T) == 4 ? __float_as_uint(o[j]) : bf16x2_rne(o[2 * j * (sizeof(T) == 2)], o[(2 * j + 1) * (sizeof(T) == 2)]);
+            __builtin_memcpy(&v, w, BYTES);
+        }
+    }
+    SDP4_DEV void store(T *p) const
+    {
+        if constexpr (BYTES == 16)
+            store_chunk<T>(p, v);
+        else if constexpr (BYTES == 8)
+            __builtin_nontemporal_store((half_at<T>)v, reinterpret_cast<half_at<T> *>(p));
+        else
+            *p = v;
+    }
+};
 
-// N elements (whole chunks, or half a chunk of bfloat16) from element address p.
+// N elements from element address p.
 template <class T, int N>
 SDP4_DEV void load_whole(const T *p, float (&v)[N])
 {
-    if constexpr (N < kChunk<T>) {
-        load_half(p, v);
-    } else {
-#pragma unroll
-        for (int k = 0; k < N / kChunk<T>; ++k)
-            unpack<T>(load_chunk<true>(p + k * kChunk<T>), *reinterpret_cast<float(*)[kChunk<T>]>(v + k * kChunk<T>));
-    }
+    Raw<T, N> r;
+    r.template load<true>(p);
+    r.get(v);
 }
 
 // Elements c .. c + N - 1 of a row of `cols`, in two steps, so that the loads of several rows are in flight together:
 // where the row ends before, load_row reads its last N elements instead (what another lane may be replacing there is
 // not used) and end_row moves them to their places.  Places beyond the row get `fill`.
 template <class T, int N>
-SDP4_DEV void load_row(const T *row, int64_t c, int64_t cols, float (&v)[N])
+SDP4_DEV void load_row(const T *row, int64_t c, int64_t cols, Raw<T, N> &r)
 {
     if (cols >= N) {
-        load_whole(row + (c + N <= cols ? c : cols - N), v);
+        r.template load<true>(row + (c + N <= cols ? c : cols - N));
     } else {
+        float v[N];
 #pragma unroll
         for (int j = 0; j < N; ++j)
             v[j] = to_f32<T>(row[j < cols ? j : 0]);
+        r.put(v);
     }
+}
+template <class T, int N>
+SDP4_DEV void load_row(const T *row, int64_t c, int64_t cols, float (&v)[N])
+{
+    Raw<T, N> r;
+    load_row(row, c, cols, r);
+    r.get(v);
 }
 template <int N>
 SDP4_DEV void end_row(int64_t c, int64_t cols, float (&v)[N], float fill = 0.0f)
@@ -185,11 +238,9 @@ template <class T, int N>
 SDP4_DEV void store_elems(T *p, int64_t valid, const float (&v)[N])
 {
     if (valid >= N) {
-        if constexpr (N < kChunk<T>)
-            store_half(p, v);
-#pragma unroll
-        for (int k = 0; k < N / kChunk<T>; ++k)
-            store_chunk<T>(p + k * kChunk<T>, pack<T>(*reinterpret_cast<const float(*)[kChunk<T>]>(v + k * kChunk<T>)));
+        Raw<T, N> r;
+        r.put(v);
+        r.store(p);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
