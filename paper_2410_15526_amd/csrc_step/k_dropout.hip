@@ -138,78 +138,107 @@ __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row,
     }
 }
 
-// Backward with column sums.  A block takes 2^lx_log2 neighbouring 8-element columns and a range of rows; a lane adds up its
-// columns in registers, the block's lanes of one column join through LDS, and the sums of the row ranges go to the
-// workspace, from where k_sum_parts adds them in order: no atomics, one result.  The loop has the next rows' loads under
-// way before it stores the present ones: loads that follow stores wait for these.
+// Backward with column sums.  A block takes 2^lx_log2 neighbouring 8-element columns and every parts-th batch of rows; a
+// lane adds up its columns in registers, the block's lanes of one column join through LDS, and the blocks' sums go to the
+// workspace, from where k_sum_parts adds them in order: no atomics, one result.
+//
+// Batches in turn rather than a range of rows for each block, so that the chip's accesses move through memory on one
+// front.  The loop over whole batches has no test in it and steps its addresses, and it has the next batch's loads under
+// way before it stores the present one, since loads that follow stores wait for these.
 template <class In, class Out>
 __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, int64_t per_row, int64_t col_tiles,
-                                                      int64_t rows_each, Rows<const In *> dy, Rows<Out *> dx,
+                                                      int64_t nparts, Rows<const In *> dy, Rows<Out *> dx,
                                                       float *parts)
 {
     constexpr bool H = sizeof(In) == 4 || sizeof(Out) == 4;
     using L = Lanes<H>;
-    constexpr int N = L::N, C = L::COUNT, U = 4 / C; // U rows of a lane in flight
+    constexpr int N = L::N, C = L::COUNT, U = 4 / C; // U rows of a lane in a batch
     __shared__ float lds[256 * 8];
     const int lx = 1 << lx_log2, ly = 256 >> lx_log2;
     const int64_t part = work_block() / col_tiles, tile = work_block() - part * col_tiles;
-    const int64_t start = part * rows_each, end = start + rows_each < d.rows ? start + rows_each : d.rows;
+    const int64_t batch = U * ly, stride = nparts * batch; // rows of a batch, and to the block's next
     // the block's 256 (column, row) places, 64 to a wave: place -> column place % lx, row place / lx
     const int wave = uniform(threadIdx.x / kWave) * kWave;
     const int64_t col0 = tile * lx;
-    int64_t c[C];       // first element of the lane's columns
-    int64_t r[C];       // its next row
-    bool on[C];
     float acc[C][N] = {};
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int place = wave + L::block(i), k = place & (lx - 1);
-        on[i] = col0 + k < per_row;
-        c[i] = on[i] ? 8 * (col0 + k) + L::start() : 0;
-        r[i] = start + (place >> lx_log2);
-    }
-    // the generator's block of the lane's first row, and the step from row to row
+    int64_t r0 = part * batch;
+    // the generator's block of the lane's first row, and the steps from row to row
     const int drawn = wave + L::mine();
-    uint64_t block = (uint64_t)((start + (drawn >> lx_log2)) * per_row + col0 + (drawn & (lx - 1)));
-    const uint64_t block_step = (uint64_t)(ly * per_row);
-    Raw<In, N> next[U][C];
-    auto fetch = [&](int64_t ahead) {
+    uint64_t block = (uint64_t)((r0 + (drawn >> lx_log2)) * per_row + col0 + (drawn & (lx - 1)));
+    const uint64_t row_step = (uint64_t)(ly * per_row), batch_step = (uint64_t)(stride * per_row);
+    if (8 * (col0 + lx) <= d.cols && r0 + batch <= d.rows) {
+        const In *src[C];
+        Out *dst[C];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int i = 0; i < C; ++i) {
+            const int place = wave + L::block(i);
+            const int64_t c = 8 * (col0 + (place & (lx - 1))) + L::start(), r = r0 + (place >> lx_log2);
+            src[i] = dy.p + r * dy.stride + c, dst[i] = dx.p + r * dx.stride + c;
+        }
+        const int64_t in_row = ly * dy.stride, out_row = ly * dx.stride, in_step = stride * dy.stride, out_step = stride * dx.stride;
+        Raw<In, N> next[U][C];
+        auto fetch = [&] {
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int64_t at = r[i] + ahead + u * ly < end ? r[i] + ahead + u * ly : end - 1;
-                load_row(dy.p + at * dy.stride, c[i], d.cols, next[u][i]);
-            }
-    };
-    fetch(0);
-    for (int64_t r0 = start; r0 < end; r0 += U * ly) {
-        float v[U][C][N];
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+                for (int i = 0; i < C; ++i)
+                    next[u][i].template load<true>(src[i] + u * in_row);
 #pragma unroll
             for (int i = 0; i < C; ++i)
-                next[u][i].get(v[u][i]);
-        if (r0 + U * ly < end)
-            fetch(U * ly);
+                src[i] += in_step;
+        };
+        fetch();
+        for (; r0 + batch <= d.rows; r0 += stride) {
+            float v[U][C][N];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            uint32_t words[C][N / 2];
-            if (d.drop)
-                L::draw(d, block, words);
-            block += block_step;
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                if (r[i] < end && on[i]) {
-                    end_row(c[i], d.cols, v[u][i]);
-                    if (d.drop)
-                        apply_mask(words[i], d.drop, d.scale, v[u][i]);
+                for (int i = 0; i < C; ++i)
+                    next[u][i].get(v[u][i]);
+            if (r0 + stride + batch <= d.rows)
+                fetch();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                uint32_t words[C][N / 2] = {};
+                if (d.drop)
+                    L::draw(d, block + u * row_step, words);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    apply_mask(words[i], d.drop, d.scale, v[u][i]);
 #pragma unroll
                     for (int j = 0; j < N; ++j)
                         acc[i][j] += v[u][i][j];
-                    store_elems(dx.p + r[i] * dx.stride + c[i], d.cols - c[i], v[u][i]);
+                    Raw<Out, N> o;
+                    o.put(v[u][i]);
+                    o.store(dst[i] + u * out_row);
                 }
-                r[i] += ly;
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                dst[i] += out_step;
+            block += batch_step;
+        }
+    }
+    for (; r0 < d.rows; r0 += stride, block += batch_step) { // rows and columns that need looking after
+#pragma unroll 1
+        for (int u = 0; u < U; ++u) {
+            uint32_t words[C][N / 2] = {};
+            if (d.drop)
+                L::draw(d, block + u * row_step, words);
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                const int place = wave + L::block(i);
+                const int64_t r = r0 + u * ly + (place >> lx_log2), k = col0 + (place & (lx - 1)), c = 8 * k + L::start();
+                if (r < d.rows && k < per_row) {
+                    float v[N];
+                    load_row(dy.p + r * dy.stride, c, d.cols, v);
+                    end_row(c, d.cols, v);
+                    apply_mask(words[i], d.drop, d.scale, v);
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        acc[i][j] += v[j];
+                    store_elems(dx.p + r * dx.stride + c, d.cols - c, v);
+                }
             }
         }
     }
@@ -224,7 +253,7 @@ __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, in
         float sum = 0.0f;
         for (int i = 0; i < ly; ++i)
             sum += lds[j * 256 + (i << lx_log2) + l];
-        if (8 * col0 + o < 8 * per_row)
+        if (8 * col0 + o < (nparts == 1 ? d.cols : 8 * per_row)) // one part: the sums themselves
             parts[part * 8 * per_row + 8 * col0 + o] = sum;
     }
 }
@@ -274,11 +303,13 @@ Rows<T *> typed(Rows<P> r)
     return {static_cast<T *>(r.p), r.stride};
 }
 
-// The split of the backward pass: 8-element columns side by side in a block, and row ranges.
+// The split of the backward pass: 8-element columns side by side in a block, and the blocks that share a column's rows --
+// about kGradBlocks in all, with 8 rows of a lane for each.
 struct GradSplit {
     int lx_log2;
-    int64_t per_row, col_tiles, rows_each, parts;
+    int64_t per_row, col_tiles, parts;
 };
+constexpr int64_t kGradBlocks = 1280;
 GradSplit grad_split(int64_t rows, int64_t cols)
 {
     GradSplit g;
@@ -287,16 +318,9 @@ GradSplit grad_split(int64_t rows, int64_t cols)
     while (g.lx_log2 < 6 && (int64_t(1) << g.lx_log2) < g.per_row)
         ++g.lx_log2;
     g.col_tiles = (g.per_row + (1 << g.lx_log2) - 1) >> g.lx_log2;
-    const int64_t step = 256 >> g.lx_log2;          // rows a block takes at a time
-    #ifndef DGB
-#define DGB 1024
-#endif
-    int64_t want = (DGB + g.col_tiles - 1) / g.col_tiles;
-    const int64_t most = (rows + 2 * step - 1) / (2 * step);
-    want = want < most ? want : most;
-    want = want < 1 ? 1 : want;
-    g.rows_each = ((rows + want - 1) / want + step - 1) / step * step;
-    g.parts = (rows + g.rows_each - 1) / g.rows_each;
+    const int64_t want = (kGradBlocks + g.col_tiles - 1) / g.col_tiles;
+    const int64_t rows_each = 4 * (256 >> g.lx_log2), most = (rows + rows_each - 1) / rows_each;
+    g.parts = want < most ? want : most;
     return g;
 }
 
@@ -336,10 +360,10 @@ int launch_dropout_grad(const Dropout &d, int in, Rows<const void *> dy, int out
             using In = decltype(in_tag);
             using Out = decltype(out_tag);
             return launch<4>(k_dropout_grad<In, Out>, g.col_tiles * g.parts, kUncapped, s, d, g.lx_log2, g.per_row,
-                             g.col_tiles, g.rows_each, typed<const In>(dy), typed<Out>(dx), workspace);
+                             g.col_tiles, g.parts, typed<const In>(dy), typed<Out>(dx), g.parts == 1 ? dbias : workspace);
         });
     });
-    return rc ? rc : launch_sum_parts({{workspace, g.parts, dbias}, {}}, 8 * g.per_row, d.cols, s);
+    return rc || g.parts == 1 ? rc : launch_sum_parts({{workspace, g.parts, dbias}, {}}, 8 * g.per_row, d.cols, s);
 }
 
 int launch_sum_parts(const Parts (&parts)[2], int64_t pitch, int64_t cols, hipStream_t s)

@@ -394,14 +394,12 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     __shared__ uint16_t chosen[K];     // slices
     __shared__ uint64_t groups[K];     // bound of all but one round, then slice << 16 | chunk of the slice with the largest
     __shared__ uint64_t list[kListed]; // logits
-    __shared__ uint32_t listed;
+    __shared__ uint32_t reads[K * NC]; // chunks of the row
     const int lane = lane_id(), k = out.top_k;
     const int64_t row = work_block();
     if (row >= rows)
         return;
     const uint64_t below = (uint64_t(1) << lane) - 1;
-    if (lane == 0)
-        listed = 0;
     stats += row * slices;
     keys += row * slices * kWave;
     float ref, S;
@@ -483,59 +481,64 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     }
     wave_lds_sync();
 
+    // chunks of these groups that reach the k-th best: most often one of each
     const T *p = x.p + row * x.stride;
-    const int64_t chunks = (vocab + W - 1) / W;
-    const uint32_t least_order = Key::order(tau);
+    const uint32_t least_order = Key::order(tau), chunks = (uint32_t)((vocab + W - 1) / W);
     const float least = from_order_bits(least_order);
-    // body(value, element) for each logit of the groups that may be among the k largest
-    auto candidates = [&](auto body) {
-        for (int c = lane; c < found * NC; c += kWave) {
-            const uint64_t g = groups[c / NC];
-            const uint32_t place = (uint32_t)g & 0xFFFFu;
-            if (c % NC != (int)(place / kWave) && (uint32_t)(g >> 32) < least_order)
-                continue; // nothing there reaches the k-th best
-            const int64_t chunk = (int64_t)((uint32_t)g >> 16) * (NC * kWave) + (c % NC) * kWave + place % kWave;
-            if (chunk >= chunks)
-                continue;
-            const int64_t e = chunk * W;
-            float v[W];
-            load_row(p, e, vocab, v);
-            end_row(e, vocab, v, -__builtin_inff());
-#pragma unroll
-            for (int j = 0; j < W; ++j)
-                if (e + j < vocab && (v[j] > least || (v[j] == least && chunk <= last)))
-                    body(entry_of(v[j], (uint32_t)(e + j)));
-        }
-    };
-    candidates([&](uint64_t entry) {
-        const uint32_t slot = atomicAdd(&listed, 1u);
-        if (slot < kListed)
-            list[slot] = entry;
-    });
-    wave_lds_sync();
-    int n = (int)uniform(listed);
-    if (n > kListed) {
-        // The largest logits crowd into few groups: the k-th best entry, bit by bit, then the list of the k from there up.
-        uint64_t kth = 0;
-#pragma unroll 1
-        for (int b = 63; b >= 0; --b) {
-            const uint64_t mid = kth | uint64_t(1) << b;
-            uint32_t mine = 0;
-            candidates([&](uint64_t entry) { mine += entry >= mid; });
-            if ((int)sum_lanes((float)mine, kWave) >= k) // below 2^24: exact
-                kth = mid;
-        }
-        wave_lds_sync();
-        if (lane == 0)
-            listed = 0;
-        wave_lds_sync();
-        candidates([&](uint64_t entry) {
-            if (entry >= kth)
-                list[atomicAdd(&listed, 1u)] = entry;
-        });
-        wave_lds_sync();
-        n = (int)uniform(listed);
+    int n_read = 0;
+    for (int c0 = 0; c0 < found * NC; c0 += kWave) {
+        const int c = c0 + lane;
+        const uint64_t g = groups[c < found * NC ? c / NC : 0];
+        const uint32_t place = (uint32_t)g & 0xFFFFu, chunk = ((uint32_t)g >> 16) * (NC * kWave) + (c % NC) * kWave + place % kWave;
+        const bool wanted = c < found * NC && chunk < chunks && (c % NC == (int)(place / kWave) || (uint32_t)(g >> 32) >= least_order);
+        const uint64_t all = __ballot(wanted);
+        if (wanted)
+            reads[n_read + __builtin_popcountll(all & below)] = chunk;
+        n_read += __builtin_popcountll(all);
     }
+    wave_lds_sync();
+    // Their logits from the k-th best on, an element a lane.  Should the list not hold them (the largest logits crowd into
+    // few groups), passes that count find the k-th best entry bit by bit, and the last one lists the k from there up.
+    constexpr int F = 4; // loads in flight
+    uint64_t kth = 0;
+    int n, bit = 64;
+#pragma unroll 1
+    for (;;) {
+        const uint64_t from = bit >= 0 && bit < 64 ? kth | uint64_t(1) << bit : kth;
+        n = 0;
+#pragma unroll 1
+        for (int e0 = 0; e0 < n_read * W; e0 += F * kWave) {
+            float v[F];
+            uint32_t chunk[F], at[F];
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const int e = e0 + f * kWave + lane;
+                chunk[f] = reads[e < n_read * W ? e / W : 0];
+                at[f] = e < n_read * W ? chunk[f] * W + e % W : (uint32_t)vocab;
+                v[f] = to_f32<T>(p[at[f] < vocab ? at[f] : 0]);
+            }
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const uint64_t entry = entry_of(v[f], at[f]);
+                const bool is = at[f] < vocab && (v[f] > least || (v[f] == least && (int64_t)chunk[f] <= last)) && entry >= from;
+                const uint64_t all = __ballot(is);
+                const int slot = n + __builtin_popcountll(all & below);
+                if (is && slot < kListed)
+                    list[slot] = entry;
+                n += __builtin_popcountll(all);
+            }
+        }
+        if (bit == 64) {
+            if (n <= kListed)
+                break;
+        } else if (bit >= 0) {
+            kth = n >= k ? from : kth;
+        } else {
+            break;
+        }
+        --bit;
+    }
+    wave_lds_sync();
     const bool bad = !(S - S == 0.0f);
     for (int a = lane; a < (n > k ? n : k); a += kWave) {
         const uint64_t mine = a < n ? list[a] : 0;
