@@ -162,18 +162,30 @@ SDP4_DEV void add_guarded(const u32x4 &raw, float ref, float &S, float &T2)
     }
 }
 
-// S and T of what the wave holds, relative to the `ref` it chooses (uniform over the wave), and with TOP the largest of
-// each chunk.
+// A lane's largest logit, the round it first stands in, and the largest of its other rounds.
+struct LaneTop {
+    float top, rest;
+    uint32_t at;
+    SDP4_DEV void add(float m, int round)
+    {
+        rest = fmaxf(rest, fminf(top, m));
+        at = m > top ? (uint32_t)round : at;
+        top = fmaxf(top, m);
+    }
+};
+
+// S and T of what the wave holds, relative to the `ref` it chooses (uniform over the wave), and with TOP each lane's top.
 //
 // The quick way takes the largest of the first round as reference, so that every logit is seen once.  Where that does not
 // do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is not finite or far below the largest (T / S would
 // cancel against log S), a type's lowest value, NaN -- the sums show it, and the wave goes over its registers again with
 // the true maximum and a lower bound on the exponent.
 template <bool TOP, class T, int NC>
-SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, float (&cm)[NC], float &tail_max)
+SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, LaneTop &lt)
 {
     constexpr int W = kChunk<T>;
-    tail_max = h.has_tail ? chunk_max<T>(h.tail) : -__builtin_inff();
+    lt = LaneTop{-__builtin_inff(), -__builtin_inff(), 0u}; // where nothing is larger than -inf, the first round
+    const float tail_max = h.has_tail ? chunk_max<T>(h.tail) : -__builtin_inff();
     ref = max_wave(h.full ? chunk_max<T>(h.raw[0]) : tail_max);
     const float c = ref * kLog2e;
     S = T2 = 0.0f;
@@ -183,10 +195,11 @@ SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, 
             float v[W];
             unpack<T>(h.raw[i], v);
             if constexpr (TOP) {
-                cm[i] = v[0];
+                float m = v[0];
 #pragma unroll
                 for (int j = 1; j < W; ++j)
-                    cm[i] = fmaxf(cm[i], v[j]);
+                    m = fmaxf(m, v[j]);
+                lt.add(m, i);
             }
 #pragma unroll
             for (int j = 0; j < W; ++j) {
@@ -199,8 +212,11 @@ SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, 
     const float delta = __builtin_fmaf(ref, kLog2e, -c), f = exp2_of(-delta); // the rounding of c, taken out
     T2 = f * __builtin_fmaf(-delta, S, T2);
     S *= f;
-    if (h.has_tail)
+    if (h.has_tail) {
         add_guarded<T>(h.tail, ref, S, T2);
+        if constexpr (TOP)
+            lt.add(tail_max, h.full);
+    }
     S = sum_lanes(S, kWave);
     T2 = sum_lanes(T2, kWave);
     if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < 1e38f)))
@@ -250,27 +266,13 @@ SDP4_DEV void join_sums(const Slice (&s)[N], float &ref, float &S, float &T2)
 template <bool TOP, class T, int NC>
 SDP4_DEV Slice take_slice(const Held<T, NC> &h, typename GroupKey<T>::Word &key)
 {
-    float ref, S, T2, cm[NC], tail_max;
-    slice_sums<TOP>(h, ref, S, T2, cm, tail_max);
+    float ref, S, T2;
+    LaneTop lt;
+    slice_sums<TOP>(h, ref, S, T2, lt);
     float top = -__builtin_inff();
     if constexpr (TOP) {
-        float rest = top;
-        uint32_t at = 0; // where nothing is larger than -inf, the first round
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            if (i < h.full) {
-                rest = fmaxf(rest, fminf(top, cm[i]));
-                at = cm[i] > top ? (uint32_t)i : at;
-                top = fmaxf(top, cm[i]);
-            }
-        }
-        if (h.has_tail) {
-            rest = fmaxf(rest, fminf(top, tail_max));
-            at = tail_max > top ? (uint32_t)h.full : at;
-            top = fmaxf(top, tail_max);
-        }
-        key = GroupKey<T>::make(top, at, rest);
-        top = max_wave(top);
+        key = GroupKey<T>::make(lt.top, lt.at, lt.rest);
+        top = max_wave(lt.top);
     }
     return Slice{ref, S, T2, top};
 }
@@ -688,8 +690,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, in
     h.template load<STEP>(p, start, NC, vocab);
     Slice s{0.0f, 0.0f, 0.0f, 0.0f};
     if (h.any()) {
-        float cm[NC], tail_max;
-        slice_sums<false>(h, s.ref, s.S, s.T, cm, tail_max);
+        LaneTop unused;
+        slice_sums<false>(h, s.ref, s.S, s.T, unused);
     }
     float ref = s.ref, S = s.S, T2 = s.T;
     if constexpr (WAVES > 1) {
@@ -831,13 +833,15 @@ int token_loss(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenSta
     if (chunks <= 1024)
         return run(integral_constant<int, 4>{}, integral_constant<int, 4>{});
     if (chunks <= 2048)
-        return run(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+        return run(integral_constant<int, 8>{}, integral_constant<int, 4>{});
     if (chunks <= 4096)
-        return run(integral_constant<int, 8>{}, integral_constant<int, 8>{});
-    if (chunks <= 6656)
-        return run(integral_constant<int, 8>{}, integral_constant<int, 13>{});
-    if (chunks <= 8192)
-        return run(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+        return run(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    if (chunks <= 7168)
+        return run(integral_constant<int, 16>{}, integral_constant<int, 7>{});
+    if (chunks <= 10240)
+        return run(integral_constant<int, 16>{}, integral_constant<int, 10>{});
+    if (chunks <= 13312)
+        return run(integral_constant<int, 16>{}, integral_constant<int, 13>{});
     if (chunks <= 16384)
         return run(integral_constant<int, 16>{}, integral_constant<int, 16>{});
     const int rc = logprob<T>(x, rows, vocab, out, workspace, s);
