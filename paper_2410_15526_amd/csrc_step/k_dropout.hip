@@ -63,8 +63,9 @@ struct Lanes {
 // 512 elements per wave, four waves in a block, rows one after the other.  A wave whose blocks are all whole and in one
 // row addresses them as a scalar base plus a lane offset; the others find each lane's row.
 template <class In, class Out, bool BIAS, bool RES>
-__global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row, int64_t total, Rows<const In *> x,
-                                                     const In *bias, Rows<const Out *> res, Rows<Out *> y)
+__global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row, uint32_t inv32, int64_t total,
+                                                     Rows<const In *> x, const In *bias, Rows<const Out *> res,
+                                                     Rows<Out *> y)
 {
     using L = Lanes<sizeof(In) == 4 || sizeof(Out) == 4>;
     constexpr int N = L::N, C = L::COUNT;
@@ -111,16 +112,23 @@ __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row,
         }
         return;
     }
-    int64_t r[C], c[C];
+    const In *xw = x.p + (int64_t)r0 * x.stride;
+    const Out *rw = res.p + (int64_t)r0 * res.stride;
+    Out *yw = y.p + (int64_t)r0 * y.stride;
+    const uint32_t left = (uint64_t)total - first < kWave ? (uint32_t)((uint64_t)total - first) : kWave; // blocks of the wave
+    uint32_t ahead[C]; // rows from the wave's first
+    int32_t c[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        uint64_t t = first + L::block(i), k;
-        t = t < (uint64_t)total ? t : (uint64_t)total - 1;
-        r[i] = (int64_t)divide(t, per_row, k);
-        c[i] = 8 * (int64_t)k + L::start();
-        load_row(x.p + r[i] * x.stride, c[i], d.cols, v[i]);
+        const uint32_t b0 = L::block(i);
+        uint32_t k = (uint32_t)k0 + (b0 < left ? b0 : left - 1), q = __umulhi(k, inv32);
+        k -= q * (uint32_t)per_row.d;
+        if (k >= (uint32_t)per_row.d)
+            k -= (uint32_t)per_row.d, ++q;
+        ahead[i] = q, c[i] = (int32_t)(8 * k) + L::start();
+        load_row(xw + (uint64_t)q * (uint64_t)x.stride, c[i], d.cols, v[i]);
         if constexpr (RES)
-            load_row(res.p + r[i] * res.stride, c[i], d.cols, a[i]);
+            load_row(rw + (uint64_t)q * (uint64_t)res.stride, c[i], d.cols, a[i]);
         if constexpr (BIAS)
             load_row(bias, c[i], d.cols, b[i]);
     }
@@ -134,7 +142,7 @@ __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row,
         if constexpr (BIAS)
             end_row(c[i], d.cols, b[i]);
         finish(i);
-        store_elems(y.p + r[i] * y.stride + c[i], first + L::block(i) < (uint64_t)total ? d.cols - c[i] : 0, v[i]);
+        store_elems(yw + (uint64_t)ahead[i] * (uint64_t)y.stride + c[i], (uint32_t)L::block(i) < left ? d.cols - c[i] : 0, v[i]);
     }
 }
 
@@ -344,7 +352,8 @@ int launch_dropout_add(const Dropout &d, int in, Rows<const void *> x, const voi
             using Out = decltype(out_tag);
             auto k = bias ? (residual.p ? k_dropout_add<In, Out, true, true> : k_dropout_add<In, Out, true, false>)
                           : (residual.p ? k_dropout_add<In, Out, false, true> : k_dropout_add<In, Out, false, false>);
-            return launch<4>(k, (total + 255) / 256, kUncapped, s, d, Divisor((uint64_t)per_row), total,
+            return launch<4>(k, (total + 255) / 256, kUncapped, s, d, Divisor((uint64_t)per_row),
+                             ~uint32_t(0) / (uint32_t)per_row, total,
                              typed<const In>(x), static_cast<const In *>(bias), typed<const Out>(residual),
                              typed<Out>(y));
         });
