@@ -334,27 +334,32 @@ __global__ __launch_bounds__(256) void k_logprob_slices(Rows<const T *> x, int64
     }
 }
 
-// The statistics of a row's slices, joined.  Returns the largest of each of the lane's slices.
+// What a wave reads of a row's slices, slice i * 64 + lane each, and of its target.
 template <class T, int N>
-SDP4_DEV void join_row(const Rows<const T *> &x, int64_t row, int64_t vocab, int slices, const TokenStats &out,
-                       const Slice *stats, float &ref, float &S, uint32_t (&tops)[N])
-{
-    const int lane = lane_id();
-    const int64_t target = out.targets ? out.targets[row] : -1;
-    const float tx = target >= 0 && target < vocab ? to_f32<T>(x.p[row * x.stride + target]) : 0.0f;
+struct RowSlices {
     Slice s[N];
+    int64_t target;
+    float target_x;
+    SDP4_DEV void load(const T *p, int64_t row, int64_t vocab, int slices, const TokenStats &out, const Slice *stats)
+    {
+        const int lane = lane_id();
+        target = out.targets ? out.targets[row] : -1;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] = Slice{0.0f, 0.0f, 0.0f, 0.0f};
-        if (i * kWave + lane < slices)
-            s[i] = stats[i * kWave + lane];
-        tops[i] = i * kWave + lane < slices ? order_bits(s[i].top) : 0u;
+        for (int i = 0; i < N; ++i) {
+            s[i] = Slice{0.0f, 0.0f, 0.0f, -__builtin_inff()};
+            if (i * kWave + lane < slices)
+                s[i] = stats[i * kWave + lane];
+        }
+        target_x = target >= 0 && target < vocab ? to_f32<T>(p[target]) : 0.0f;
     }
-    float T2;
-    join_sums<N>(s, ref, S, T2);
-    if (lane == 0)
-        finish_row(out, row, vocab, ref, S, T2, tx, target);
-}
+    SDP4_DEV void finish(int64_t row, int64_t vocab, const TokenStats &out, float &ref, float &S) const
+    {
+        float T2;
+        join_sums<N>(s, ref, S, T2);
+        if (lane_id() == 0)
+            finish_row(out, row, vocab, ref, S, T2, target_x, target);
+    }
+};
 
 template <class T>
 __global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
@@ -363,9 +368,10 @@ __global__ __launch_bounds__(256) void k_logprob_join(Rows<const T *> x, int64_t
     const int64_t row = work_block() * 4 + uniform(threadIdx.x / kWave);
     if (row >= rows)
         return;
+    RowSlices<T, kMaxSlices / kWave> r;
     float ref, S;
-    uint32_t tops[kMaxSlices / kWave];
-    join_row<T>(x, row, vocab, slices, out, stats + row * slices, ref, S, tops);
+    r.load(x.p + row * x.stride, row, vocab, slices, out, stats + row * slices);
+    r.finish(row, vocab, out, ref, S);
 }
 
 // The largest v in [low, high], which hold it, with at least k of the lanes' values >= v: value(i), i < used <= N.  Found
@@ -431,15 +437,15 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     const uint64_t below = (uint64_t(1) << lane) - 1;
     stats += row * slices;
     keys += row * slices * kWave;
-    float ref, S;
-    uint32_t tops[N];
-    join_row<T>(x, row, vocab, slices, out, stats, ref, S, tops);
+    const T *p = x.p + row * x.stride;
+    RowSlices<T, N> rs;
+    rs.load(p, row, vocab, slices, out, stats);
 
     // slices whose groups count, in order; the best group's largest, and a bound that k groups reach
-    uint32_t high = 0, low = 0;
+    uint32_t tops[N], high = 0, low = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        tops[i] >>= 32 - VB;
+        tops[i] = i * kWave + lane < slices ? order_bits(rs.s[i].top) >> (32 - VB) : 0u;
         high = max(high, tops[i]);
     }
     high = max_wave(high);
@@ -473,6 +479,8 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     for (int r = 0; r < K; ++r)
         if (r < count)
             key[r] = keys[(int)chosen[r] * kWave + lane];
+    float ref, S;
+    rs.finish(row, vocab, out, ref, S); // while the keys come
 
     // the k best groups: those above tau, and of those at tau the first -- slices in order, positions in a slice
     const uint32_t tau = kth_largest<K>(low, high, count, k, [&](int r) { return Key::value(key[r]); });
@@ -511,7 +519,6 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
     wave_lds_sync();
 
     // chunks of these groups that reach the k-th best: most often one of each
-    const T *p = x.p + row * x.stride;
     const uint32_t least_order = Key::order(tau), chunks = (uint32_t)((vocab + W - 1) / W);
     const float least = from_order_bits(least_order);
     int n_read = 0;
