@@ -266,42 +266,49 @@ __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, in
     }
 }
 
-// Sums over parts: a block of 16 waves takes 16 columns, 64 threads share the parts of each.  Few columns and many parts
-// make this a matter of latency: a thread has 16 loads in flight, and one barrier joins the waves.
-constexpr int kSumColumns = 16;
-__global__ __launch_bounds__(1024) void k_sum_parts(Parts first, Parts second, int64_t blocks_each, int64_t pitch, int64_t cols)
+// Sums over parts: a block of 8 waves takes 16 columns, 32 threads share the parts of each.  Few columns and many parts
+// make this a matter of latency: a thread has 16 loads in flight, each an offset from one scalar base (64-bit products
+// for the addresses took longer than the loads), and one barrier joins the waves.
+constexpr int kSumColumns = 16, kSumThreads = 512, kSumShare = kSumThreads / kSumColumns;
+template <class Offset> // uint32_t where the parts lie within 4 GB
+__global__ __launch_bounds__(kSumThreads) void k_sum_parts(Parts first, Parts second, int64_t blocks_each, int64_t pitch, int64_t cols)
 {
-    __shared__ float lds[16][kSumColumns];
+    __shared__ float lds[kSumThreads / kWave][kSumColumns];
     const int64_t wb = work_block();
     const Parts s = wb < blocks_each ? first : second;
     if (!s.out)
         return;
     const int col = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns;
-    const int64_t c = (wb < blocks_each ? wb : wb - blocks_each) * kSumColumns + col;
+    const int64_t c0 = (wb < blocks_each ? wb : wb - blocks_each) * kSumColumns;
+    const bool on = c0 + col < cols;
+    const char *base = reinterpret_cast<const char *>(s.p + c0);
+    const Offset step = (Offset)(kSumShare * sizeof(float)) * (Offset)pitch;
+    Offset at = ((Offset)share * (Offset)pitch + (on ? col : 0)) * (Offset)sizeof(float);
     float sum = 0.0f;
-    if (c < cols) {
-        const float *p = s.p + c;
-        for (int64_t i = share; i < s.count; i += 64 * 16) {
-            float v[16];
+    for (int i = share; i < (int)s.count; i += 16 * kSumShare) {
+        float v[16];
+        Offset o = at;
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                v[j] = p[(i + 64 * j < s.count ? i + 64 * j : i) * pitch];
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                sum += i + 64 * j < s.count ? v[j] : 0.0f;
+        for (int j = 0; j < 16; ++j) {
+            v[j] = *reinterpret_cast<const float *>(base + o);
+            o = i + (j + 1) * kSumShare < (int)s.count ? o + step : at; // beyond the last part: the first again, not used
         }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            sum += i + j * kSumShare < (int)s.count ? v[j] : 0.0f;
+        at += 16 * step;
     }
     sum += xor_lane<16>(sum);
     sum += xor_lane<32>(sum);
     if (lane_id() < kSumColumns)
         lds[threadIdx.x / kWave][col] = sum;
     __syncthreads();
-    if (threadIdx.x < kSumColumns && c < cols) {
+    if (threadIdx.x < kSumColumns && on) {
         float total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 16; ++w)
+        for (int w = 0; w < kSumThreads / kWave; ++w)
             total += lds[w][col];
-        s.out[c] = total;
+        s.out[c0 + col] = total;
     }
 }
 
@@ -378,7 +385,9 @@ int launch_dropout_grad(const Dropout &d, int in, Rows<const void *> dy, int out
 int launch_sum_parts(const Parts (&parts)[2], int64_t pitch, int64_t cols, hipStream_t s)
 {
     const int64_t each = (cols + kSumColumns - 1) / kSumColumns;
-    return launch<16>(k_sum_parts, parts[1].out ? 2 * each : each, kUncapped, s, parts[0], parts[1], each, pitch, cols);
+    const int64_t most = parts[0].count > parts[1].count ? parts[0].count : parts[1].count;
+    auto k = (most + 17 * kSumShare) * pitch < (int64_t(1) << 30) ? k_sum_parts<uint32_t> : k_sum_parts<uint64_t>;
+    return launch<kSumThreads / kWave>(k, parts[1].out ? 2 * each : each, kUncapped, s, parts[0], parts[1], each, pitch, cols);
 }
 
 } // namespace sdp4
