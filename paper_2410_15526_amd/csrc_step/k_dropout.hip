@@ -7,6 +7,9 @@
 // backward pass draws it again.  Rows start at multiples of the width
 // rounded up to 8, which keeps the eight elements of an evaluation in one
 // row: they are the work of one lane.
+//
+// HBM bounds all of it; the generator's 20 products for eight elements keep the vector units 40 % busy in the forward
+// pass (p = 0, without them, takes the same time).
 #include "step_device.hpp"
 
 namespace sdp4 {
@@ -60,7 +63,8 @@ struct Lanes {
     }
 };
 
-// 512 elements per wave, four waves in a block, rows one after the other.  A wave whose blocks are all whole and in one
+// 512 elements per wave, four waves in a block, rows one after the other: 8192 x 5120 bfloat16 40.7 us, 6.2 TB/s (float32
+// 79, 6.4, and 105 in a form in which a lane read its 32 bytes together).  A wave whose blocks are all whole and in one
 // row addresses them as a scalar base plus a lane offset; the others find each lane's row.
 template <class In, class Out, bool BIAS, bool RES>
 __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row, uint32_t inv32, int64_t total,
@@ -152,7 +156,9 @@ __global__ __launch_bounds__(256) void k_dropout_add(Dropout d, Divisor per_row,
 //
 // Batches in turn rather than a range of rows for each block, so that the chip's accesses move through memory on one
 // front.  The loop over whole batches has no test in it and steps its addresses, and it has the next batch's loads under
-// way before it stores the present one, since loads that follow stores wait for these.
+// way before it stores the present one, since loads that follow stores wait for these.  4095 x 2048 float32 12.8 us, 5.4
+// TB/s with its partial sums, and 4.5 for the sums over the parts, which is a launch and one trip to memory; 8192 x 5120
+// bfloat16 34.6 in all.
 template <class In, class Out>
 __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, int64_t per_row, int64_t col_tiles,
                                                       int64_t nparts, Rows<const In *> dy, Rows<Out *> dx,
@@ -324,6 +330,8 @@ struct GradSplit {
     int lx_log2;
     int64_t per_row, col_tiles, parts;
 };
+// 768 / 1024 / 1280 / 1536 blocks: 8192 x 5120 bfloat16 39.8 / 38.7 / 36.8 / 37.9 us, float32 70.6 / 68.1 / 63.3 / 66.5
+// (4095 x 2048 float32, which has fewer batches than that, 17.9 / 18.7 / 18.7 / 18.6).
 constexpr int64_t kGradBlocks = 1280;
 GradSplit grad_split(int64_t rows, int64_t cols)
 {

@@ -12,9 +12,10 @@
 // finished by its wave.  For the alternatives each lane also leaves the largest of its 64 logits, and the second launch
 // finds from these which few groups of 64 can hold the row's largest and reads only those again.
 //
-// What bounds it: with bfloat16 logits the vector units as much as HBM -- 3.5 T logits a second at the rate of reads
-// leave 11 issue slots for each, of which the exponential alone takes 4.  So the sums run without a pass for the maximum:
-// any logit of the slice serves as the reference, as long as the sum is finite at the end.
+// What bounds it: HBM (4096 x 50001 bfloat16 without alternatives 65 us, 6.3 TB/s, float32 122, 6.7), and with bfloat16
+// nearly the vector units too: at the rate of reads 3.5 T logits a second leave 11 issue slots for each, and the kernel
+// takes 10 where it looks for alternatives, 70 us.  So the sums run without a pass for the maximum (the form with one took
+// 78 us without alternatives): any logit of the slice serves as the reference, as long as the sum is finite at the end.
 #include "step_device.hpp"
 
 namespace sdp4 {
@@ -418,8 +419,10 @@ SDP4_DEV uint32_t max_wave(uint32_t v)
 // again: of most groups one chunk, as what its others hold is known to be less) those at least as good as the k-th best
 // group's largest, k and a few more, are listed in LDS, and each one's place is the number of better ones.
 //
-// A row takes a chain of three reads from memory (slices and keys, target, chunks) and the steps between, 9 us; 4096 rows
-// with 5 alternatives take 13.
+// A row is a chain of reads from memory (slices, keys, chunks) with some 600 dependent vector instructions of one wave
+// between them: 8 us for few rows, 13 for 4096 with 5 alternatives.  (Alternatives chosen in the slices themselves and
+// joined here took 118 us in all for 4096 x 50001 and k = 5, 186 for 20, against 82 and 95.  A block for each row with its
+// waves as the slices saves this launch and loses more by waves that wait: 94, without alternatives 83 against 65.)
 constexpr int kListed = 256;
 template <class T, int NC, int K, int N>
 __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int64_t rows, int64_t vocab, int slices,
@@ -649,7 +652,7 @@ SDP4_DEV void grad_chunk(const RowGrad &g, X exponent, float delta, int e, int v
     }
 }
 
-// A wave takes U * 64 chunks of one row.
+// A wave takes U * 64 chunks of one row: 2048 x 32768 float32 with all three gradients 86 us, 6.2 TB/s, nearly a copy's rate.
 template <class T, int U, bool ENT>
 __global__ __launch_bounds__(256) void k_logprob_grad(Rows<const T *> x, int64_t rows, int64_t vocab64,
                                                       const int64_t *targets, const float *lse, const float *entropy,
@@ -703,7 +706,8 @@ __global__ __launch_bounds__(256) void k_logprob_grad(Rows<const T *> x, int64_t
 
 // The loss and its gradient: a block holds a whole row in registers, so the logits are read once.  Each wave sums up its
 // own part, the parts are joined through LDS, and with the row's statistics every lane turns what it holds into the
-// gradient.
+// gradient.  8192 x 50000 bfloat16 272 us, 6.0 TB/s, vector units 65 % busy.  Shapes, when they were chosen: 16 waves
+// with 7 chunks a lane 279 us, 8 with 13 298, 4 with 25 306.
 template <class T, int WAVES, int NC, bool ENT>
 __global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, int64_t rows, int64_t vocab64,
                                                            TokenStats out, TokenGrads g, Rows<T *> dx, int64_t width64)
@@ -782,8 +786,10 @@ Rows<T *> typed(Rows<P> r)
     return {static_cast<T *>(r.p), r.stride};
 }
 
-// How a row is cut into slices of 64 * nc chunks: the largest that still give 2048 waves, and no more than 64 if that
-// can be.
+// How a row is cut into slices of 64 * nc chunks: the largest that still give 2048 waves, two to a SIMD, and no more than
+// 64 if that can be, which the join reads in one go.  1024 and 4096 waves take the same time within 3 % for 4 to 2048 rows
+// of 131072 and 32000.  Slices of 2048 logits at most instead of 4096: 4096 x 50001 with 5 alternatives 88 us against 81,
+// float32 157 against 151.
 struct Cut {
     int nc;
     int64_t slices;
@@ -830,6 +836,8 @@ int logprob(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenStats 
                                  Divisor((uint64_t)c.slices), out, stats, keys);
         if (rc || (c.slices == 1 && !out.top_k))
             return rc;
+        // The join holds keys for as many slices and alternatives as it is built for.  With 256 slices and 32 alternatives
+        // for every call: 4 x 131072 with 8 13.4 us against 10.6, 8192 x 6000 with 5 45 against 34.
         constexpr int most = kMaxSlices / kWave;
         const bool few = c.slices <= kWave;
         if (out.top_k) {
@@ -856,12 +864,10 @@ int logprob_grad(Rows<const void *> x, int64_t rows, int64_t vocab, const int64_
                  const float *entropy, const TokenGrads &g, Rows<void *> dx, int64_t width, hipStream_t s)
 {
     const int64_t chunks = (width + kChunk<T> - 1) / kChunk<T>;
-    auto run = [&](auto k, int u) {
-        const int64_t tiles = (chunks + 64 * u - 1) / (64 * u);
-        return launch<4>(k, (rows * tiles + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab, targets, lse,
-                         entropy, g, typed<T>(dx), width, Divisor((uint64_t)tiles));
-    };
-    return run(k_logprob_grad<T, 2, ENT>, 2);
+    constexpr int U = 2; // 1 / 2 / 4: 2048 x 32768 float32 86.6 / 86.3 / 88.8 us, 4096 x 32768 bfloat16 85.4 / 84.6 / 83.9
+    const int64_t tiles = (chunks + 64 * U - 1) / (64 * U);
+    return launch<4>(k_logprob_grad<T, U, ENT>, (rows * tiles + 3) / 4, kUncapped, s, typed<const T>(x), rows, vocab, targets,
+                     lse, entropy, g, typed<T>(dx), width, Divisor((uint64_t)tiles));
 }
 
 template <class T, bool ENT>
@@ -876,6 +882,10 @@ int token_loss(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenSta
         return launch<WV>(k_token_loss<T, WV, NC, ENT>, rows, kUncapped, s, typed<const T>(x), rows, vocab, out, g,
                           typed<T>(dx), width);
     };
+    // The fewest waves, then the fewest chunks a lane, that hold the row; longer rows take two launches.  Those where one
+    // would do: 8192 x 1000 14.5 us against 10.1, 4096 x 50000 bfloat16 197 against 150, 4096 x 131072 507 against 405,
+    // float32 4096 x 50000 394 against 299.  (Few long rows leave units empty here, but a loss is taken of many:
+    // 64 x 131072 14.5 against 16.4.)
     using std::integral_constant;
     if (chunks <= 256)
         return run(integral_constant<int, 1>{}, integral_constant<int, 4>{});
