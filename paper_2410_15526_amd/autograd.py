@@ -3,11 +3,13 @@
 Each function allocates its outputs (and a workspace where the call needs
 one) and calls the entry points of :mod:`paper_2410_15526_amd.sdp4`; a
 program that keeps its buffers calls those directly.  Broadcast or transposed
-arguments are copied; what else must hold of them is checked there.
+arguments are copied; what else must hold of them is checked there.  The
+gradients have no gradients themselves: torch raises where one is asked for.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import sdp4
 
@@ -34,6 +36,7 @@ class _DropoutAdd(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         p, seed, offset, dtype, bias_dtype, with_residual = ctx.args
         dy = _laid_out(dy)
@@ -63,6 +66,7 @@ class _QkNormRope(torch.autograd.Function):
         return q_out, k_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, table, positions = ctx.saved_tensors
         eps, interleaved = ctx.args
@@ -97,6 +101,7 @@ class _TokenLogprob(torch.autograd.Function):
         return tuple(out)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_logp, g_lse, g_entropy):
         logits, targets, lse, entropy = ctx.saved_tensors
         d = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
@@ -115,6 +120,7 @@ def token_loss(logits, targets, weights, vocab: int | None = None):
     computed together (the logits are read once): for
     ``logits.backward(gradient)``.  Returns (loss, gradient)."""
     with torch.no_grad():
+        logits = _laid_out(logits)
         rows, width = logits.shape
         logp, lse, entropy = (torch.empty(rows, device=logits.device) for _ in range(3))
         d = torch.empty(rows, width, dtype=logits.dtype, device=logits.device)

@@ -126,3 +126,33 @@ def test_rope_table_rules():
     mid = (turns > 1) & (turns < 32)
     assert bool(mid.any()) and bool((got[mid] < inv[mid]).all()) and bool((got[mid] > inv[mid] / 8).all())
     assert torch.allclose(autograd.rope_table(3, 8, scale=0.5)[0, :4], torch.full((4,), 0.5, device="cuda"))
+
+
+def test_loss_of_transposed_logits():
+    import torch
+
+    from paper_2410_15526_amd import autograd
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randn(70, 9, device="cuda", generator=g)
+    t = torch.randint(0, 64, (9,), device="cuda", generator=g)
+    w = torch.rand(9, 2, device="cuda", generator=g)[:, 0]
+    got, want = (autograd.token_loss(x, t, w, 64) for x in (z.T, z.T.contiguous()))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("name", ["dropout_add", "token_logprob", "qk_norm_rope"])
+def test_gradients_of_gradients_are_refused(name):
+    import torch
+
+    from paper_2410_15526_amd import autograd
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(6, 4, 16, device="cuda", generator=g).requires_grad_()
+    if name == "dropout_add":
+        y = autograd.dropout_add(x.view(24, 16), None, None, 0.5, 1, 0)
+    elif name == "token_logprob":
+        y = autograd.token_logprob(x.view(24, 16), torch.zeros(24, dtype=torch.int64, device="cuda"))[1]
+    else:
+        y = autograd.qk_norm_rope(x, x, None, None, 1e-6, None, None)[0]
+    dx, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (dx.square().sum() + x.sum()).backward()
