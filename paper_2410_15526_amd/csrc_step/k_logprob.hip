@@ -14,7 +14,7 @@
 //
 // What bounds it: HBM (4096 x 50001 bfloat16 without alternatives 65 us, 6.3 TB/s, float32 122, 6.7), and with bfloat16
 // nearly the vector units too: at the rate of reads 3.5 T logits a second leave 11 issue slots for each, and the kernel
-// takes 10 where it looks for alternatives, 70 us.  So the sums run without a pass for the maximum (the form with one took
+// takes 10 where it looks for alternatives, 71 us.  So the sums run without a pass for the maximum (the form with one took
 // 78 us without alternatives): any logit of the slice serves as the reference, as long as the sum is finite at the end.
 #include "step_device.hpp"
 
@@ -419,8 +419,8 @@ SDP4_DEV uint32_t max_wave(uint32_t v)
 // again: of most groups one chunk, as what its others hold is known to be less) those at least as good as the k-th best
 // group's largest, k and a few more, are listed in LDS, and each one's place is the number of better ones.
 //
-// A row is a chain of reads from memory (slices, keys, chunks) with some 600 dependent vector instructions of one wave
-// between them: 8 us for few rows, 13 for 4096 with 5 alternatives.  (Alternatives chosen in the slices themselves and
+// A row is a chain of reads from memory (slices, keys, chunks) with some 560 dependent vector instructions of one wave
+// between them: 8 us for few rows, 11 for 4096 with 5 alternatives.  (Alternatives chosen in the slices themselves and
 // joined here took 118 us in all for 4096 x 50001 and k = 5, 186 for 20, against 82 and 95.  A block for each row with its
 // waves as the slices saves this launch and loses more by waves that wait: 94, without alternatives 83 against 65.)
 constexpr int kListed = 256;
