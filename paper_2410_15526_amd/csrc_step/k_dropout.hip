@@ -233,25 +233,50 @@ __global__ __launch_bounds__(256) void k_dropout_grad(Dropout d, int lx_log2, in
             block += batch_step;
         }
     }
-    for (; r0 < d.rows; r0 += stride, block += batch_step) { // rows and columns that need looking after
+    // Rows and columns that need looking after: the same loop with tests, places beyond the array reading others.  Batch after
+    // batch in flight here too, since these blocks end last: 8192 x 5119 bfloat16 48.8 / 42.4 us, 4095 x 2047 float32 20.3 /
+    // 17.9, 4095 x 2048 17.8 / 16.8.
+    if (r0 < d.rows) {
+        Raw<In, N> next[U][C];
+        auto fetch = [&](int64_t from) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    const int place = wave + L::block(i);
+                    const int64_t r = from + u * ly + (place >> lx_log2), k = col0 + (place & (lx - 1));
+                    load_row(dy.p + (r < d.rows ? r : d.rows - 1) * dy.stride, k < per_row ? 8 * k + L::start() : 0, d.cols,
+                             next[u][i]);
+                }
+        };
+        fetch(r0);
 #pragma unroll 1
-        for (int u = 0; u < U; ++u) {
-            uint32_t words[C][N / 2] = {};
-            if (d.drop)
-                L::draw(d, block + u * row_step, words);
+        for (; r0 < d.rows; r0 += stride, block += batch_step) {
+            float v[U][C][N];
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int place = wave + L::block(i);
-                const int64_t r = r0 + u * ly + (place >> lx_log2), k = col0 + (place & (lx - 1)), c = 8 * k + L::start();
-                if (r < d.rows && k < per_row) {
-                    float v[N];
-                    load_row(dy.p + r * dy.stride, c, d.cols, v);
-                    end_row(c, d.cols, v);
-                    apply_mask(words[i], d.drop, d.scale, v);
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        acc[i][j] += v[j];
-                    store_elems(dx.p + r * dx.stride + c, d.cols - c, v);
+                for (int i = 0; i < C; ++i)
+                    next[u][i].get(v[u][i]);
+            if (r0 + stride < d.rows)
+                fetch(r0 + stride);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                uint32_t words[C][N / 2] = {};
+                if (d.drop)
+                    L::draw(d, block + u * row_step, words);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    const int place = wave + L::block(i);
+                    const int64_t r = r0 + u * ly + (place >> lx_log2), k = col0 + (place & (lx - 1)), c = 8 * k + L::start();
+                    if (r < d.rows && k < per_row) {
+                        end_row(c, d.cols, v[u][i]);
+                        apply_mask(words[i], d.drop, d.scale, v[u][i]);
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            acc[i][j] += v[u][i][j];
+                        store_elems(dx.p + r * dx.stride + c, d.cols - c, v[u][i]);
+                    }
                 }
             }
         }
