@@ -71,13 +71,18 @@ struct GroupKey {
 SDP4_DEV float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
 SDP4_DEV float log2_of(float s) { return __builtin_amdgcn_logf(s); }
 
+// Largest reference for t = (x - ref) log2 e as one fma x log2 e - c with c = ref log2 e rounded: every t is off by that
+// rounding, at most 2^-4 up to here, which is known and taken out.  It grows with ref, past the exponents of float32 from 3e9
+// on.  Larger references take a subtraction and a product, which loses nothing: what is near such a reference differs from it
+// exactly, and the rest has no share.
+constexpr float kOneFma = 0x1p20f;
+
 // Calls body(exponent, delta) with t(x) = (x - ref) log2 e - lg: one fma, whose constant's rounding error the caller
-// takes out again by `delta` (t is too large by it), or, for magnitudes whose product with log2 e overflows (rows of a
-// type's lowest value), a subtraction and an fma.
+// takes out again by `delta` (t is too large by it), or, for larger references, a subtraction and an fma.
 template <class F>
 SDP4_DEV void with_exponent(float ref, float lg, F body)
 {
-    if (__builtin_fabsf(ref) < 1e38f) {
+    if (__builtin_fabsf(ref) < kOneFma) {
         const float c = __builtin_fmaf(ref, kLog2e, lg);
         body([=](float x) { return __builtin_fmaf(x, kLog2e, -c); }, __builtin_fmaf(ref, kLog2e, -c) + lg);
     } else {

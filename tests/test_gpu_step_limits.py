@@ -1,0 +1,101 @@
+"""The training-step operators on the GPU where values, lengths or layouts go
+to the limits of what the library's header allows, against 64-bit forms."""
+import numpy as np
+import pytest
+
+from paper_2410_15526_amd import sdp4
+from tests import _step as ref
+from tests._gpu import say, torch
+from tests.test_gpu_step import close, dt, f64, normal, scratch
+
+pytestmark = pytest.mark.gpu
+
+
+def rng(seed):
+    return torch().Generator(device="cuda").manual_seed(seed)
+
+
+def empties(rows, n=3):
+    return [torch().full((rows,), 7.0, device="cuda") for _ in range(n)]
+
+
+# ---------------------------------------------------------------------------
+# logits of large magnitude
+# ---------------------------------------------------------------------------
+def grad_from(x, targets, lse, ent, g_logp, g_ent, g_lse, dtype):
+    """(dlogits, bound) from a given float32 logsumexp: p = exp(x - lse), whatever these sum up to.  t = (x - lse) log2 e is
+    off by at most 3 U of itself (difference, log2 e, product) and once more U where its share in the entropy's term is
+    taken; the exponential by 2 U; the factors and their sum by 8 U of their magnitudes; bfloat16 by its final rounding."""
+    d = x - lse[:, None]
+    p = np.exp(d)
+    dd = np.where(p > 0, d, 0.0)
+    z = np.zeros(len(x))
+    gl, ga, ge = (z if g is None else g for g in (g_lse, g_logp, g_ent))
+    ga = np.where(targets < 0, 0.0, ga)
+    v = p * ((gl - ga)[:, None] - ge[:, None] * (dd + ent[:, None]))
+    mag = p * ((np.abs(gl) + np.abs(ga) + np.abs(ge * ent))[:, None] + np.abs(ge[:, None] * dd))
+    bound = mag * ref.U * (4 * np.abs(dd) + 12)
+    hit = np.nonzero(targets >= 0)[0]
+    v[hit, targets[hit]] += ga[hit]
+    bound[hit, targets[hit]] += 2 * ref.U * np.abs(ga[hit])
+    return v, bound + ref.rounding(dtype) * np.abs(v) + 1000 * ref.TINY
+
+
+LARGE = [1e5, 3e6, -2e8, 1.3e9, 5e9, -1e10, 1e20, -1e30, 1e38, -1e38]
+
+
+def large_rows(g, vocab, dtype):
+    """Rows of one large value; a large value among ordinary ones; half a row of masks at -1e30; ordinary rows."""
+    t = torch()
+    x = normal(g, 2 * len(LARGE) + 4, vocab, dtype=dtype, scale=2.0)
+    for i, v in enumerate(LARGE):
+        x[i] = v
+        x[len(LARGE) + i, vocab // 2] = v
+    x[-4, ::2] = -1e30
+    x[-3, :vocab // 2] = -1e10
+    x[-2] = x[-2] + 1e6
+    tg = t.randint(0, vocab, (len(x),), device="cuda", generator=g)
+    tg[2], tg[-1] = -100, vocab // 2
+    return x, tg
+
+
+@pytest.mark.parametrize("entropy", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [9, 700, 20003, 140001])
+def test_token_gradients_of_large_logits(vocab, dtype, entropy):
+    t = torch()
+    say("large logits", vocab, dtype, entropy)
+    g = rng(100 + vocab)
+    x, tg = large_rows(g, vocab, dtype)
+    rows = len(x)
+    gs = [normal(g, rows, scale=0.5), normal(g, rows, scale=0.5) if entropy else None, normal(g, rows, scale=0.5)]
+    xs, tn, gn = f64(x), tg.cpu().numpy(), [None if a is None else f64(a) for a in gs]
+    logp, lse, ent = ref.token_stats(xs, tn)
+    l32, e32 = (t.from_numpy(a).float().cuda() for a in (lse, ent))
+    d = t.full((rows, vocab), float("nan"), dtype=dt(dtype), device="cuda")
+    sdp4.sdp4_token_logprob_grad(x, tg, l32, e32, *gs, d)
+    want, bound = grad_from(xs, tn, f64(l32), f64(e32), *gn, dtype)
+    close(d, want, bound, "dlogits")
+    d = t.full((rows, vocab), float("nan"), dtype=dt(dtype), device="cuda")
+    lp, ls, en = empties(rows)
+    sdp4.sdp4_token_loss(x, tg, *gs, lp, ls, en, d, scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab)))
+    bl, be, bn = ref.stats_bounds(xs, logp, ent)
+    close(ls, lse, be, "lse")
+    close(lp, logp, bl, "logp")
+    close(en, ent, bn, "entropy")
+    if vocab > (131072 if dtype == "bf16" else 65536):     # two launches: p from the rounded logsumexp
+        want, bound = grad_from(xs, tn, f64(ls), f64(en), *gn, dtype)
+    else:
+        want, bound = ref.token_grad(xs, tn, ent, *gn, vocab, dtype, lse_given=False)
+    close(d, want, bound, "dlogits of the loss")
+
+
+def test_gradient_of_a_row_that_is_left_out():
+    """No upstream gradient and no target: zeros, whatever finite values the row holds."""
+    t = torch()
+    for dtype in ("f32", "bf16"):
+        x = t.tensor([[-1e10], [-1e30], [7e9], [1e38]], device="cuda").expand(4, 640).to(dt(dtype)).contiguous()
+        tg, z = t.full((4,), -100, device="cuda"), t.zeros(4, device="cuda")
+        d = t.full_like(x, float("nan"))
+        sdp4.sdp4_token_loss(x, tg, z, z, z, *empties(4), d, scratch(sdp4.sdp4_token_logprob_workspace(4, 640)))
+        assert bool((d == 0).all()), dtype
