@@ -206,9 +206,9 @@ struct LaneTop {
 // S and T of what the wave holds, relative to the `ref` it chooses (uniform over the wave), and with TOP each lane's top.
 //
 // The quick way takes the largest of the first round as reference, so that every logit is seen once.  Where that does not
-// do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is not finite or far below the largest (T / S would
-// cancel against log S), a type's lowest value, NaN -- the sums show it, and the wave goes over its registers again with
-// the true maximum and a lower bound on the exponent.
+// do -- a logit of -inf, whose 0 * -inf spoils T, a reference that is large (its exponents carry the rounding of c), not
+// finite or far below the largest (T / S would cancel against log S), a type's lowest value, NaN -- the sums or the reference
+// show it, and the wave goes over its registers again with the true maximum and a lower bound on the exponent.
 template <bool TOP, class T, int NC>
 SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, LaneTop &lt)
 {
@@ -250,7 +250,7 @@ SDP4_DEV void slice_sums(const Held<T, NC> &h, float &ref, float &S, float &T2, 
         take_out(h.copy(), ref, S, T2);
     S = sum_lanes(S, kWave);
     T2 = sum_lanes(T2, kWave);
-    if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < 1e38f)))
+    if (uniform((uint32_t)(S > 0.0f && S < 0x1p24f && T2 - T2 == 0.0f && __builtin_fabsf(ref) < kOneFma)))
         return;
     float m = tail_max;
 #pragma unroll

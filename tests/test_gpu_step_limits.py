@@ -99,3 +99,29 @@ def test_gradient_of_a_row_that_is_left_out():
         d = t.full_like(x, float("nan"))
         sdp4.sdp4_token_loss(x, tg, z, z, z, *empties(4), d, scratch(sdp4.sdp4_token_logprob_workspace(4, 640)))
         assert bool((d == 0).all()), dtype
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(40, 250), (2100, 1000), (40, 20003)])
+def test_statistics_of_large_logits(rows, vocab, dtype):
+    """Rows of equal logits: lse = x + log vocab, entropy log vocab, each logp -log vocab, as for small ones.  The sum of n
+    ones is off by (its 64 additions in a lane at most, 6 over the lanes and those over slices, the exponent's constants 4)
+    U; the logarithm and its factor by 4 U of itself."""
+    t = torch()
+    x = t.logspace(2, 38, rows, device="cuda", dtype=t.float64)
+    x[1::2] *= -1
+    x = x.to(dt(dtype))[:, None].expand(rows, vocab).contiguous()
+    tg = t.arange(rows, device="cuda") % vocab
+    b = ref.U * (64 + 6 + 16 + 4 + 4 * np.log(vocab))
+    d = t.empty_like(x)
+    for loss in (False, True):
+        lp, ls, en = empties(rows)
+        ws = scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab))
+        if loss:
+            sdp4.sdp4_token_loss(x, tg, None, None, None, lp, ls, en, d, ws)
+        else:
+            sdp4.sdp4_token_logprob(x, tg, 0, lp, ls, en, workspace=ws)
+        close(lp, np.full(rows, -np.log(vocab)), b, ("logp", loss))
+        close(en, np.full(rows, np.log(vocab)), b, ("entropy", loss))
+        x0 = f64(x[:, 0])
+        close(ls, x0 + np.log(vocab), b + 2 * ref.U * np.abs(x0), ("lse", loss))
