@@ -363,7 +363,8 @@ int64_t sdp4_dropout_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes
  * and its top_k largest logits (ties: the lower index first) as token ids
  * and log probabilities.  Logits of -inf have probability 0; a row of
  * nothing else has lse = logp = -inf and entropy 0; a NaN or +inf in a row
- * makes its lse, logp, entropy and top_logp NaN and its top_ids -1.
+ * makes its lse, logp, entropy and top_logp NaN and its top_ids -1.  Other
+ * log probabilities are never above 0 and entropies never below.
  *
  *   logits   [rows][vocab] dtype, row stride `stride`; what lies between
  *            vocab and stride is not read

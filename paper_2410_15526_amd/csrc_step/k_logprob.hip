@@ -90,6 +90,14 @@ SDP4_DEV void with_exponent(float ref, float lg, F body)
     }
 }
 
+// Log probability of logit x.  Its terms' roundings may leave that of a certain token above 0, and no caller expects that;
+// NaN stays.
+SDP4_DEV float log_prob(float x, float ref, float ln_s)
+{
+    const float v = (x - ref) - ln_s;
+    return v > 0.0f ? 0.0f : v;
+}
+
 // The outputs of one row from its whole statistics.
 SDP4_DEV void finish_row(const TokenStats &out, int64_t row, int64_t vocab, float m, float S, float T, float target_x,
                          int64_t target)
@@ -103,7 +111,7 @@ SDP4_DEV void finish_row(const TokenStats &out, int64_t row, int64_t vocab, floa
     if (out.logp) {
         float v = target < 0 ? 0.0f : __builtin_nanf("");
         if (target >= 0 && target < vocab)
-            v = empty ? -__builtin_inff() : (target_x - m) - ln_s;
+            v = empty ? -__builtin_inff() : log_prob(target_x, m, ln_s);
         out.logp[row] = v;
     }
 }
@@ -596,7 +604,7 @@ __global__ __launch_bounds__(64) void k_logprob_join_top(Rows<const T *> x, int6
         }
         if (rank < k) {
             const int64_t at = row * k + rank;
-            const float v = S == 0.0f ? -__builtin_inff() : (from_order_bits((uint32_t)(mine >> 32)) - ref) - kLn2 * log2_of(S);
+            const float v = S == 0.0f ? -__builtin_inff() : log_prob(from_order_bits((uint32_t)(mine >> 32)), ref, kLn2 * log2_of(S));
             out.top_logp[at] = bad ? __builtin_nanf("") : v;
             out.top_ids[at] = bad ? -1 : (int64_t)entry_index(mine);
         }

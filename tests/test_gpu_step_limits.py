@@ -125,3 +125,37 @@ def test_statistics_of_large_logits(rows, vocab, dtype):
         close(en, np.full(rows, np.log(vocab)), b, ("entropy", loss))
         x0 = f64(x[:, 0])
         close(ls, x0 + np.log(vocab), b + 2 * ref.U * np.abs(x0), ("lse", loss))
+
+
+# ---------------------------------------------------------------------------
+# confident rows
+# ---------------------------------------------------------------------------
+def peaked(g, rows, vocab, dtype):
+    """Logits around 0 with one that stands 0 to 40 above them, anywhere in the row; targets there."""
+    t = torch()
+    x = normal(g, rows, vocab, dtype="f32", scale=0.3)
+    tg = t.randint(0, vocab, (rows,), device="cuda", generator=g)
+    high = t.linspace(0, 40, rows, device="cuda")
+    x.scatter_(1, tg[:, None], high[:, None])
+    return x.to(dt(dtype)), tg
+
+
+PEAKED = [(2100, 320), (2100, 1000), (2100, 4096), (300, 9001), (64, 70001)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", PEAKED)
+def test_log_probabilities_are_not_positive(rows, vocab, dtype):
+    t = torch()
+    say("signs", rows, vocab, dtype)
+    x, tg = peaked(rng(vocab), rows, vocab, dtype)
+    for k in (0, 3):
+        lp, ls, en = empties(rows)
+        tl, ti = t.full((rows, k), 7.0, device="cuda"), t.zeros(rows, k, dtype=t.int64, device="cuda")
+        sdp4.sdp4_token_logprob(x, tg, k, lp, ls, en, tl, ti, scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab, k)))
+        assert float(lp.max()) <= 0 and float(en.min()) >= 0
+        assert not k or float(tl.max()) <= 0
+    lp, ls, en = empties(rows)
+    sdp4.sdp4_token_loss(x, tg, None, None, None, lp, ls, en, t.empty_like(x),
+                         scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab)))
+    assert float(lp.max()) <= 0 and float(en.min()) >= 0
