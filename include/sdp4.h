@@ -364,7 +364,10 @@ int64_t sdp4_dropout_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes
  * and log probabilities.  Logits of -inf have probability 0; a row of
  * nothing else has lse = logp = -inf and entropy 0; a NaN or +inf in a row
  * makes its lse, logp, entropy and top_logp NaN and its top_ids -1.  Other
- * log probabilities are never above 0 and entropies never below.
+ * log probabilities are never above 0 and entropies never below.  Beside the
+ * rounding of the result both carry that of a float32 sum of exponentials, an
+ * absolute error of a few 1e-6 at most (2.3e-6 was the largest seen), which
+ * counts where -logp is as small.
  *
  *   logits   [rows][vocab] dtype, row stride `stride`; what lies between
  *            vocab and stride is not read

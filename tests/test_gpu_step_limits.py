@@ -159,3 +159,35 @@ def test_log_probabilities_are_not_positive(rows, vocab, dtype):
     sdp4.sdp4_token_loss(x, tg, None, None, None, lp, ls, en, t.empty_like(x),
                          scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab)))
     assert float(lp.max()) <= 0 and float(en.min()) >= 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", PEAKED)
+def test_confident_rows_keep_their_precision(rows, vocab, dtype):
+    """Errors relative to -logp and to the entropy H, wherever in its row the largest logit stands.
+
+    With sums of 2^t relative to a reference whose mean exponent (weighted by probability) is at most 4, the weighted |t|
+    is at most 4 + 2 H / ln 2 and the sum's logarithm at most 4 ln 2 + H.  A sum is then off by U times (a lane's additions +
+    6 over the lanes + the joins' 16 + 4 for exponential and constants + 2 ln 2 |t|), logp by that and 3 U (-logp + 2 H +
+    4 ln 2); the entropy twice by the sums' error, its second sum in proportion to |t|."""
+    t = torch()
+    say("confident rows", rows, vocab, dtype)
+    x, tg = peaked(rng(vocab), rows, vocab, dtype)
+    xs, tn = f64(x), tg.cpu().numpy()
+    logp, lse, ent = ref.token_stats(xs, tn)
+    slices = -(-vocab // 4096)
+    adds = min(64, -(-vocab // 64)) + 6 + (16 if slices > 1 else 0) + 4
+    rel = ref.U * (adds + 8 * np.log(2) + 4 * ent)
+    b_logp = rel + 3 * ref.U * (-logp + 2 * ent + 4 * np.log(2))
+    b_ent = rel + ref.U * (adds + 4) * (4 * np.log(2) + 2 * ent) + 3 * ref.U * (2 * ent + 4 * np.log(2))
+    for loss in (False, True):
+        lp, ls, en = empties(rows)
+        ws = scratch(sdp4.sdp4_token_logprob_workspace(rows, vocab))
+        if loss:
+            sdp4.sdp4_token_loss(x, tg, None, None, None, lp, ls, en, t.empty_like(x), ws)
+        else:
+            sdp4.sdp4_token_logprob(x, tg, 0, lp, ls, en, workspace=ws)
+        print("logp", np.abs(f64(lp) - logp).max(), "entropy", np.abs(f64(en) - ent).max(), flush=True)
+        close(lp, logp, b_logp, ("logp", loss))
+        close(en, ent, b_ent, ("entropy", loss))
+        close(ls, lse, b_logp + 2 * ref.U * np.abs(lse), ("lse", loss))
