@@ -376,7 +376,8 @@ int64_t sdp4_dropout_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes
  *            >= vocab is a mistake (logp = NaN)
  *   logp, lse, entropy   [rows] out, each may be NULL (logp needs targets)
  *   top_k    0 .. min(vocab, SDP4_MAX_TOP); top_logp, top_ids [rows][top_k] out
- *   workspace  sdp4_token_logprob_workspace(rows, vocab, top_k) bytes
+ *   workspace  sdp4_token_logprob_workspace(rows, vocab, top_k) bytes, which
+ *            serve any smaller number of rows too
  */
 int sdp4_token_logprob(const void *logits, int dtype, int64_t stride, int64_t rows, int64_t vocab,
                        const int64_t *targets, int top_k, float *logp, float *lse, float *entropy, float *top_logp,

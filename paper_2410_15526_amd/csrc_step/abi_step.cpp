@@ -284,7 +284,7 @@ int sdp4_token_logprob(const void *logits, int dtype, int64_t stride, int64_t ro
         return SDP4_EINVAL;
     if (!aligned(logp, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4) || !aligned(top_ids, 8))
         return SDP4_EALIGN;
-    const int64_t need = sdp4::token_logprob_workspace(rows, vocab, top_k);
+    const int64_t need = sdp4::token_logprob_workspace(rows, vocab, top_k, false);
     rc = check_workspace(workspace, workspace_bytes, need);
     if (rc != SDP4_OK)
         return rc;
@@ -308,7 +308,7 @@ int64_t sdp4_token_logprob_workspace(int64_t rows, int64_t vocab, int top_k)
 {
     if (!valid_shape(rows, vocab) || vocab < 1 || vocab > SDP4_MAX_VOCAB || top_k < 0 || top_k > SDP4_MAX_TOP)
         return -1;
-    return sdp4::token_logprob_workspace(rows, vocab, top_k);
+    return sdp4::token_logprob_workspace(rows, vocab, top_k, true);
 }
 
 int sdp4_token_logprob_grad(const void *logits, int dtype, int64_t stride, int64_t rows, int64_t vocab,
@@ -351,7 +351,7 @@ int sdp4_token_loss(const void *logits, int dtype, int64_t stride, int64_t rows,
         return SDP4_EINVAL;
     if (!aligned(logp, 4) || !aligned(lse, 4) || !aligned(entropy, 4))
         return SDP4_EALIGN;
-    const int64_t need = sdp4::token_logprob_workspace(rows, vocab, 0);
+    const int64_t need = sdp4::token_logprob_workspace(rows, vocab, 0, false);
     rc = check_workspace(workspace, workspace_bytes, need);
     if (rc != SDP4_OK)
         return rc;

@@ -816,6 +816,7 @@ Rows<T *> typed(Rows<P> r)
 // 64 if that can be, which the join reads in one go.  1024 and 4096 waves take the same time within 3 % for 4 to 2048 rows
 // of 131072 and 32000.  Slices of 2048 logits at most instead of 4096: 4096 x 50001 with 5 alternatives 88 us against 81,
 // float32 157 against 151.
+constexpr int64_t kSliceWaves = 2048;
 struct Cut {
     int nc;
     int64_t slices;
@@ -829,7 +830,7 @@ Cut cut_rows(int64_t rows, int64_t vocab)
     const int64_t chunks = (vocab + kChunk<T> - 1) / kChunk<T>;
     const auto slices = [&](int n) { return (chunks + 64 * n - 1) / (64 * n); };
     int nc = 1;
-    while (nc < most && slices(nc) > 1 && (slices(nc) > kWave || rows * slices(2 * nc) >= 2048))
+    while (nc < most && slices(nc) > 1 && (slices(nc) > kWave || rows * slices(2 * nc) >= kSliceWaves))
         nc *= 2;
     return {nc, slices(nc)};
 }
@@ -876,13 +877,23 @@ int logprob(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenStats 
     });
 }
 
+// Workspace of `rows` rows, or with `fewer` the most that they or any smaller number of them take: fewer rows are cut into
+// more slices, so the largest need may be that of the last number of rows before larger slices.
 template <class T>
-int64_t workspace_of(int64_t rows, int64_t vocab, int top_k)
+int64_t workspace_of(int64_t rows, int64_t vocab, int top_k, bool fewer)
 {
-    const Cut c = cut_rows<T>(rows, vocab);
-    if (c.slices == 1 && !top_k)
-        return 0;
-    return rows * c.slices * (int64_t)(sizeof(Slice) + (top_k ? kWave * sizeof(typename GroupKey<T>::Word) : 0));
+    const auto need = [&](int64_t r) {
+        const Cut c = cut_rows<T>(r, vocab);
+        return c.slices == 1 && !top_k ? 0 : r * c.slices;
+    };
+    int64_t most = need(rows);
+    const int64_t chunks = (vocab + kChunk<T> - 1) / kChunk<T>;
+    for (int nc = 2; fewer && nc <= kMostChunks<T>; nc *= 2) {
+        const int64_t slices = (chunks + 64 * nc - 1) / (64 * nc), last = (kSliceWaves - 1) / slices;
+        if (last > 0 && last < rows && need(last) > most)
+            most = need(last);
+    }
+    return most * (int64_t)(sizeof(Slice) + (top_k ? kWave * sizeof(typename GroupKey<T>::Word) : 0));
 }
 
 // May some row start at an odd element address?
@@ -940,11 +951,11 @@ int token_loss(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenSta
 
 } // namespace
 
-int64_t token_logprob_workspace(int64_t rows, int64_t vocab, int top_k)
+int64_t token_logprob_workspace(int64_t rows, int64_t vocab, int top_k, bool fewer)
 {
     if (rows <= 0 || vocab <= 0)
         return 0;
-    const int64_t a = workspace_of<bf16_t>(rows, vocab, top_k), b = workspace_of<float>(rows, vocab, top_k);
+    const int64_t a = workspace_of<bf16_t>(rows, vocab, top_k, fewer), b = workspace_of<float>(rows, vocab, top_k, fewer);
     return a > b ? a : b; // for either type
 }
 

@@ -48,7 +48,8 @@ int launch_token_logprob_grad(int dtype, Rows<const void *> x, int64_t rows, int
                               int64_t width, hipStream_t s);
 int launch_token_loss(int dtype, Rows<const void *> x, int64_t rows, int64_t vocab, const TokenStats &out,
                       const TokenGrads &g, Rows<void *> dx, int64_t width, void *workspace, hipStream_t s);
-int64_t token_logprob_workspace(int64_t rows, int64_t vocab, int top_k);
+// `fewer`: the most that so many rows or fewer take.
+int64_t token_logprob_workspace(int64_t rows, int64_t vocab, int top_k, bool fewer);
 
 struct Heads {
     void *p = nullptr;

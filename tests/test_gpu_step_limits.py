@@ -191,3 +191,17 @@ def test_confident_rows_keep_their_precision(rows, vocab, dtype):
         close(lp, logp, b_logp, ("logp", loss))
         close(en, ent, b_ent, ("entropy", loss))
         close(ls, lse, b_logp + 2 * ref.U * np.abs(lse), ("lse", loss))
+
+
+@pytest.mark.parametrize("vocab", [700, 4096, 9001])
+def test_a_workspace_serves_shorter_batches(vocab):
+    """A buffer for the whole batch does for its last, shorter part."""
+    t = torch()
+    for k in (0, 3):
+        x = normal(rng(5), 2500, vocab, dtype="bf16")
+        ws = t.empty(sdp4.sdp4_token_logprob_workspace(2500, vocab, k), dtype=t.uint8, device="cuda")
+        for rows in (2500, 513, 100, 1):
+            tl, ti = t.empty(rows, k, device="cuda"), t.empty(rows, k, dtype=t.int64, device="cuda")
+            sdp4.sdp4_token_logprob(x[:rows], None, k, None, *empties(rows, 2), tl, ti, ws)
+            if k == 0:
+                sdp4.sdp4_token_loss(x[:rows], None, None, None, None, None, *empties(rows, 2), t.empty_like(x[:rows]), ws)

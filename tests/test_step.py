@@ -224,3 +224,14 @@ def test_workspace_helpers():
     assert L.sdp4_token_logprob_workspace(4, (1 << 20) + 1, 0) == -1 and L.sdp4_token_logprob_workspace(1, 1 << 20, 32) > 0
     assert L.sdp4_qk_grad_workspace(-1, 1, 1, 64) == -1 and L.sdp4_qk_grad_workspace(8, 1, 1, 0) == -1
     assert L.sdp4_qk_grad_workspace(0, 4, 4, 64) == 0 and L.sdp4_qk_grad_workspace(8192, 40, 8, 128) > 0
+
+
+@pytest.mark.cpu_only
+def test_token_workspace_serves_fewer_rows():
+    """What the helper names never falls with more rows, whatever the rows' split."""
+    f = sdp4.lib().sdp4_token_logprob_workspace
+    for vocab in (1, 300, 513, 1000, 2049, 4096, 4097, 9001, 50001, 131072, 300007, 1 << 20):
+        for k in (0, 3):
+            sizes = [f(rows, vocab, min(k, vocab)) for rows in range(1, 4200)]
+            assert sizes == sorted(sizes), (vocab, k)
+            assert f(100000, vocab, min(k, vocab)) >= sizes[-1]
