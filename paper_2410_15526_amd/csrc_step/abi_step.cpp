@@ -135,6 +135,21 @@ Area area_of(const sdp4_heads &h, int64_t tokens, int dim, int dtype)
         return {h.data, tokens, ((h.heads - 1) * h.head_stride + dim) * s, h.token_stride * s};
     return {h.data, h.heads, ((tokens - 1) * h.token_stride + dim) * s, h.head_stride * s};
 }
+// May two sets of heads share a byte?  Sets with one inner stride that divides both outer ones (each head's query and key
+// side by side) are told apart by where their heads lie within it, the others as rows.
+bool heads_overlap(const sdp4_heads &a, const sdp4_heads &b, int64_t tokens, int dim, int dtype)
+{
+    if (!overlap(area_of(a, tokens, dim, dtype), area_of(b, tokens, dim, dtype)))
+        return false;
+    const auto inner = [](const sdp4_heads &h) { return h.token_stride < h.head_stride ? h.token_stride : h.head_stride; };
+    const int64_t in = inner(a);
+    if (in != inner(b) || a.token_stride % in || a.head_stride % in || b.token_stride % in || b.head_stride % in)
+        return true;
+    const auto a0 = reinterpret_cast<std::uintptr_t>(a.data), b0 = reinterpret_cast<std::uintptr_t>(b.data);
+    const std::uintptr_t pitch = (std::uintptr_t)(in * size_of(dtype)), width = (std::uintptr_t)(dim * size_of(dtype));
+    const std::uintptr_t d = b0 >= a0 ? (b0 - a0) % pitch : (pitch - (a0 - b0) % pitch) % pitch;
+    return d < width || d + width > pitch;
+}
 bool same_heads(const sdp4_heads &a, const sdp4_heads &b, int64_t tokens)
 {
     return a.data == b.data && (tokens <= 1 || a.token_stride == b.token_stride) &&
@@ -396,9 +411,9 @@ int sdp4_qk_norm_rope(const sdp4_heads *q, const sdp4_heads *k, const sdp4_qk_pa
     for (int i = 0; i < sides; ++i) {
         const Area o = area_of(oh[i], tokens, dim, params->dtype);
         for (int j = 0; j < sides; ++j) {
-            if (!(i == j && same_heads(ih[j], oh[i], tokens)) && overlap(o, area_of(ih[j], tokens, dim, params->dtype)))
+            if (!(i == j && same_heads(ih[j], oh[i], tokens)) && heads_overlap(oh[i], ih[j], tokens, dim, params->dtype))
                 return SDP4_EINVAL;
-            if (j < i && overlap(o, area_of(oh[j], tokens, dim, params->dtype)))
+            if (j < i && heads_overlap(oh[i], oh[j], tokens, dim, params->dtype))
                 return SDP4_EINVAL;
         }
         if (clash(o, {}, {flat(params->q_weight, s * dim), flat(params->k_weight, s * dim),
@@ -462,11 +477,11 @@ int sdp4_qk_norm_rope_grad(const sdp4_heads *dq_out, const sdp4_heads *dk_out, c
         const Area o = area_of(oh[i], tokens, dim, params->dtype);
         for (int j = 0; j < sides; ++j) {
             const Area g = area_of(gh[j], tokens, dim, params->dtype), x = area_of(xh[j], tokens, dim, params->dtype);
-            if (!(i == j && same_heads(gh[j], oh[i], tokens)) && overlap(o, g))
+            if (!(i == j && same_heads(gh[j], oh[i], tokens)) && heads_overlap(oh[i], gh[j], tokens, dim, params->dtype))
                 return SDP4_EINVAL;
-            if (norm && !(i == j && same_heads(xh[j], oh[i], tokens)) && overlap(o, x))
+            if (norm && !(i == j && same_heads(xh[j], oh[i], tokens)) && heads_overlap(oh[i], xh[j], tokens, dim, params->dtype))
                 return SDP4_EINVAL;
-            if (j < i && overlap(o, area_of(oh[j], tokens, dim, params->dtype)))
+            if (j < i && heads_overlap(oh[i], oh[j], tokens, dim, params->dtype))
                 return SDP4_EINVAL;
             if (clash(g, {}, {sums[0], sums[1], sums[2]}) || (norm && clash(x, {}, {sums[0], sums[1], sums[2]})))
                 return SDP4_EINVAL;

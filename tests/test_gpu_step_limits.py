@@ -6,7 +6,7 @@ import pytest
 from paper_2410_15526_amd import sdp4
 from tests import _step as ref
 from tests._gpu import say, torch
-from tests.test_gpu_step import close, dt, f64, normal, scratch
+from tests.test_gpu_step import close, dt, f64, normal, scratch, table_for
 
 pytestmark = pytest.mark.gpu
 
@@ -205,3 +205,37 @@ def test_a_workspace_serves_shorter_batches(vocab):
             sdp4.sdp4_token_logprob(x[:rows], None, k, None, *empties(rows, 2), tl, ti, ws)
             if k == 0:
                 sdp4.sdp4_token_loss(x[:rows], None, None, None, None, None, *empties(rows, 2), t.empty_like(x[:rows]), ws)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,heads", [(1, 3), (5, 1), (7, 4)])
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_qk_inside_heads_of_query_key_and_value(tokens, heads, heads_first, dtype):
+    """A projection that packs each head's query, key and value side by side: strides of three heads.  In place and
+    with both gradients in one array of that layout."""
+    t = torch()
+    g = rng(6)
+    dim = 64
+    shape = (heads, tokens, 3, dim) if heads_first else (tokens, heads, 3, dim)
+
+    def parts(a):
+        a = a.transpose(0, 1) if heads_first else a
+        return a[:, :, 0], a[:, :, 1], a[:, :, 2]
+    qkv, grads = normal(g, *shape, dtype=dtype), normal(g, *shape, dtype=dtype)
+    qw, kw, tab = normal(g, dim, dtype=dtype), normal(g, dim, dtype=dtype), table_for(tokens, dim)
+    (q, k, v), (gq, gk, gv) = parts(qkv), parts(grads)
+    at = np.arange(tokens)
+    q0, k0, v0, gv0 = q.clone(), k.clone(), v.clone(), gv.clone()
+    want = [ref.qk(f64(x), f64(w), 1e-6, f64(tab), at, False, dtype) for x, w in ((q0, qw), (k0, kw))]
+    wg = [ref.qk_grad(f64(y), f64(x), f64(w), 1e-6, f64(tab), at, False, dtype) for y, x, w in ((gq, q0, qw), (gk, k0, kw))]
+    sdp4.sdp4_qk_norm_rope(q, k, qw, kw, 1e-6, tab, None, q, k)
+    close(q, *want[0], "q")
+    close(k, *want[1], "k")
+    assert t.equal(v, v0)
+    dw = [t.empty(dim, device="cuda") for _ in range(2)]
+    sdp4.sdp4_qk_norm_rope_grad(gq, gk, q0, k0, qw, kw, 1e-6, tab, None, gq, gk, *dw,
+                                scratch(sdp4.sdp4_qk_grad_workspace(tokens, heads, heads, dim)))
+    for x, w, ((wx, bx), ww) in ((gq, dw[0], wg[0]), (gk, dw[1], wg[1])):
+        close(x, wx, bx, "dx")
+        close(w, *ww, "dw")
+    assert t.equal(gv, gv0)

@@ -235,3 +235,14 @@ def test_token_workspace_serves_fewer_rows():
             sizes = [f(rows, vocab, min(k, vocab)) for rows in range(1, 4200)]
             assert sizes == sorted(sizes), (vocab, k)
             assert f(100000, vocab, min(k, vocab)) >= sizes[-1]
+
+
+@pytest.mark.cpu_only
+@pytest.mark.parametrize("qo,ko", [(A + 4 * 32, E), (A + 4 * 64, E), (A + 4 * 129, E), (A + 4 * 192, E), (D, A), (D, A + 4),
+                                   (A, A + 4 * 63), (A, A), (A - 4 * 63, A + 4 * 64)])
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_qk_refuses_overlap_inside_packed_heads(qo, ko, heads_first):
+    """Query, key and value of each head side by side (64 elements each, four heads, eight tokens)."""
+    strides = (192, 8 * 192) if heads_first else (4 * 192, 192)
+    f = [(p, *strides, 4) for p in (A, A + 4 * 64, qo, ko)]
+    assert qk(q=f[0], k=f[1], qo=f[2], ko=f[3]) == EINVAL
