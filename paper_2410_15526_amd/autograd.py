@@ -26,6 +26,11 @@ def _laid_out(x):
     return x if ok else x.contiguous()
 
 
+def _dense(x):
+    """x contiguous, or None."""
+    return None if x is None else x.contiguous()
+
+
 class _DropoutAdd(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, bias, residual, p, seed, offset):
@@ -52,7 +57,7 @@ class _DropoutAdd(torch.autograd.Function):
 def dropout_add(x, bias, residual, p: float, seed: int, offset: int):
     """residual + dropout(x + bias) of matrices [rows, cols]; bias and residual
     may be None.  (seed, offset) name the mask, see ``sdp4_dropout_add``."""
-    return _DropoutAdd.apply(_laid_out(x), bias, None if residual is None else _laid_out(residual), p, seed, offset)
+    return _DropoutAdd.apply(_laid_out(x), _dense(bias), None if residual is None else _laid_out(residual), p, seed, offset)
 
 
 class _QkNormRope(torch.autograd.Function):
@@ -86,7 +91,8 @@ class _QkNormRope(torch.autograd.Function):
 def qk_norm_rope(q, k, q_weight, k_weight, eps, table, positions, interleaved: bool = False):
     """RMS norm (none if eps is None) and rotation of query and key heads
     [tokens, heads, head_dim], see ``sdp4_qk_norm_rope``."""
-    return _QkNormRope.apply(_laid_out(q), _laid_out(k), q_weight, k_weight, eps, table, positions, interleaved)
+    return _QkNormRope.apply(_laid_out(q), _laid_out(k), _dense(q_weight), _dense(k_weight), eps, _dense(table),
+                             _dense(positions), interleaved)
 
 
 class _TokenLogprob(torch.autograd.Function):
@@ -112,7 +118,7 @@ class _TokenLogprob(torch.autograd.Function):
 
 def token_logprob(logits, targets, vocab: int | None = None):
     """(logp, lse, entropy) of each row, see ``sdp4_token_logprob``."""
-    return _TokenLogprob.apply(_laid_out(logits), targets, vocab)
+    return _TokenLogprob.apply(_laid_out(logits), _dense(targets), vocab)
 
 
 def token_loss(logits, targets, weights, vocab: int | None = None):
@@ -125,7 +131,7 @@ def token_loss(logits, targets, weights, vocab: int | None = None):
         logp, lse, entropy = (torch.empty(rows, device=logits.device) for _ in range(3))
         d = torch.empty(rows, width, dtype=logits.dtype, device=logits.device)
         work = _workspace(sdp4.sdp4_token_logprob_workspace(rows, vocab or width), logits.device)
-        sdp4.sdp4_token_loss(logits, targets, -weights, None, None, logp, lse, entropy, d, work, vocab=vocab)
+        sdp4.sdp4_token_loss(logits, _dense(targets), _dense(-weights), None, None, logp, lse, entropy, d, work, vocab=vocab)
         return -(weights * logp).sum(), d
 
 
