@@ -18,6 +18,10 @@ def _workspace(nbytes: int, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
+def _f32(device, *shape):
+    return torch.empty(*shape, dtype=torch.float32, device=device)   # whatever the program's default type is
+
+
 def _laid_out(x):
     """x, or a contiguous copy where it is broadcast or its last dimension is
     strided (gradients often are)."""
@@ -48,7 +52,7 @@ class _DropoutAdd(torch.autograd.Function):
         dx = torch.empty(dy.shape, dtype=dtype, device=dy.device)
         dbias = work = None
         if bias_dtype is not None and ctx.needs_input_grad[1]:
-            dbias = torch.empty(dy.shape[1], device=dy.device)
+            dbias = _f32(dy.device, dy.shape[1])
             work = _workspace(sdp4.sdp4_dropout_grad_workspace(*dy.shape), dy.device)
         sdp4.sdp4_dropout_add_grad(dy, p, seed, offset, dx, dbias, work)
         return dx, None if dbias is None else dbias.to(bias_dtype), dy if with_residual else None, None, None, None
@@ -77,7 +81,7 @@ class _QkNormRope(torch.autograd.Function):
         eps, interleaved = ctx.args
         dq_out, dk_out = _laid_out(dq_out), _laid_out(dk_out)
         dq, dk = (torch.empty(d.shape, dtype=d.dtype, device=d.device) for d in (dq_out, dk_out))
-        dws = [None if w is None else torch.empty(w.shape, device=w.device) for w in (q_weight, k_weight)]
+        dws = [None if w is None else _f32(w.device, *w.shape) for w in (q_weight, k_weight)]
         work = None
         if any(w is not None for w in dws):
             tokens, heads, dim = dq_out.shape
@@ -99,7 +103,7 @@ class _TokenLogprob(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, vocab):
         rows = logits.shape[0]
-        out = [torch.empty(rows, device=logits.device) for _ in range(3)]
+        out = [_f32(logits.device, rows) for _ in range(3)]
         work = _workspace(sdp4.sdp4_token_logprob_workspace(rows, vocab or logits.shape[1]), logits.device)
         sdp4.sdp4_token_logprob(logits, targets, 0, *out, workspace=work, vocab=vocab)
         ctx.save_for_backward(logits, targets, out[1], out[2])
@@ -128,7 +132,7 @@ def token_loss(logits, targets, weights, vocab: int | None = None):
     with torch.no_grad():
         logits = _laid_out(logits)
         rows, width = logits.shape
-        logp, lse, entropy = (torch.empty(rows, device=logits.device) for _ in range(3))
+        logp, lse, entropy = (_f32(logits.device, rows) for _ in range(3))
         d = torch.empty(rows, width, dtype=logits.dtype, device=logits.device)
         work = _workspace(sdp4.sdp4_token_logprob_workspace(rows, vocab or width), logits.device)
         sdp4.sdp4_token_loss(logits, _dense(targets), _dense(-weights), None, None, logp, lse, entropy, d, work, vocab=vocab)
@@ -154,6 +158,6 @@ def rope_table(rows: int, rot_dim: int, base: float = 10000.0, stretch: float = 
         turns = length * inv / (2 * torch.pi)
         keep = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
         inv = inv * keep + inv / stretch * (1 - keep)
-    table = torch.empty(rows, rot_dim, device=device)
+    table = _f32(device, rows, rot_dim)
     sdp4.sdp4_rope_table(inv.to(device), table, start, scale)
     return table

@@ -51,3 +51,27 @@ def test_strided_and_broadcast_vectors():
     for eps in (1e-6, None):
         ws = [n(16, 2)[:, 0], n(16, 4)[:, 3]] if eps else []
         both(lambda q, k, *w: autograd.qk_norm_rope(q, k, *(w or (None, None)), eps, tab, pos), n(6, 3, 16), n(6, 2, 16), *ws)
+
+
+@pytest.mark.parametrize("default", ["bfloat16", "float64"])
+def test_default_types_other_than_float32(default):
+    """A program whose default type is another still gets float32 statistics and sums."""
+    import torch
+
+    from paper_2410_15526_amd import autograd
+    g = generator(1)
+    n = lambda *s: torch.randn(*s, device="cuda", generator=g, dtype=torch.float32).requires_grad_()  # noqa: E731
+    torch.set_default_dtype(getattr(torch, default))
+    try:
+        x, b, z, q, w = n(12, 40), n(40), n(12, 32), n(6, 3, 16), n(16)
+        t = torch.randint(0, 30, (12,), device="cuda", generator=g)
+        y = autograd.dropout_add(x, b, None, 0.2, 3, 8)
+        stats = autograd.token_logprob(z, t, 30)
+        loss, d = autograd.token_loss(z.detach(), t, torch.ones(12, device="cuda", dtype=torch.float32), 30)
+        tab = autograd.rope_table(6, 16)
+        qo, ko = autograd.qk_norm_rope(q, q, w, w, 1e-6, tab, None)
+        sum((v * v).sum() for v in (y, *stats, qo, ko)).backward()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    for v in (y, *stats, loss, d, tab, qo, ko, x.grad, b.grad, z.grad, q.grad, w.grad):
+        assert v.dtype == torch.float32 and bool(torch.isfinite(v).all())
