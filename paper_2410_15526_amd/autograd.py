@@ -48,6 +48,8 @@ class _DropoutAdd(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         p, seed, offset, dtype, bias_dtype, with_residual = ctx.args
+        if not any(ctx.needs_input_grad[:2]):
+            return None, None, dy, None, None, None
         dy = _laid_out(dy)
         dx = torch.empty(dy.shape, dtype=dtype, device=dy.device)
         dbias = work = None
@@ -81,7 +83,8 @@ class _QkNormRope(torch.autograd.Function):
         eps, interleaved = ctx.args
         dq_out, dk_out = _laid_out(dq_out), _laid_out(dk_out)
         dq, dk = (torch.empty(d.shape, dtype=d.dtype, device=d.device) for d in (dq_out, dk_out))
-        dws = [None if w is None else _f32(w.device, *w.shape) for w in (q_weight, k_weight)]
+        dws = [_f32(w.device, *w.shape) if w is not None and needed else None
+               for w, needed in zip((q_weight, k_weight), ctx.needs_input_grad[2:4])]
         work = None
         if any(w is not None for w in dws):
             tokens, heads, dim = dq_out.shape
@@ -108,6 +111,7 @@ class _TokenLogprob(torch.autograd.Function):
         sdp4.sdp4_token_logprob(logits, targets, 0, *out, workspace=work, vocab=vocab)
         ctx.save_for_backward(logits, targets, out[1], out[2])
         ctx.vocab = vocab
+        ctx.set_materialize_grads(False)      # no gradient by the entropy: the form without it
         return tuple(out)
 
     @staticmethod
@@ -115,8 +119,8 @@ class _TokenLogprob(torch.autograd.Function):
     def backward(ctx, g_logp, g_lse, g_entropy):
         logits, targets, lse, entropy = ctx.saved_tensors
         d = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        sdp4.sdp4_token_logprob_grad(logits, targets, lse, entropy, g_logp.contiguous(), g_entropy.contiguous(),
-                                     g_lse.contiguous(), d, vocab=ctx.vocab)
+        sdp4.sdp4_token_logprob_grad(logits, targets, lse, entropy, _dense(g_logp), _dense(g_entropy), _dense(g_lse), d,
+                                     vocab=ctx.vocab)
         return d, None, None
 
 
