@@ -124,10 +124,16 @@ def _bind(L) -> None:
         warnings.warn(f"sdp4: native argument marshalling was built for torch {built_for}, not "
                       f"{torch.__version__}, and is not used: calls take longer on the host", RuntimeWarning)
         return
-    _binding.bind(*[C.cast(getattr(L, "sdp4_" + n), C.c_void_p).value for n in
-                    ("qwd_encode", "qwd_decode", "qwd_encode_sym", "qwd_decode_sym", "grad_quant", "grad_quant_sr",
-                     "dequant_reduce", "dequant_reduce_sr", "dropout_add", "dropout_add_grad", "token_logprob",
-                     "token_logprob_grad", "token_loss", "qk_norm_rope", "qk_norm_rope_grad")])
+    addresses = [C.cast(getattr(L, "sdp4_" + n), C.c_void_p).value for n in
+                 ("qwd_encode", "qwd_decode", "qwd_encode_sym", "qwd_decode_sym", "grad_quant", "grad_quant_sr",
+                  "dequant_reduce", "dequant_reduce_sr", "dropout_add", "dropout_add_grad", "token_logprob",
+                  "token_logprob_grad", "token_loss", "qk_norm_rope", "qk_norm_rope_grad")]
+    try:
+        _binding.bind(*addresses)
+    except TypeError:
+        warnings.warn("sdp4: native argument marshalling was built for other entry points and is not used: calls take "
+                      "longer on the host", RuntimeWarning)
+        return
     _fast = _binding
 
 

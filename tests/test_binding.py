@@ -68,6 +68,25 @@ def test_binding_that_does_not_name_its_torch_is_not_used(monkeypatch):
 
 
 @pytest.mark.cpu_only
+def test_binding_of_other_entry_points_is_not_used(monkeypatch):
+    """One left over from sources with fewer of them, whose bind() takes eight addresses."""
+    import sys
+    import types
+
+    import paper_2410_15526_amd as package
+
+    def bind(*addresses):
+        if len(addresses) != 8:
+            raise TypeError("bind: eight addresses")
+    _unbound(monkeypatch)
+    old = types.SimpleNamespace(torch_version=torch.__version__, bind=bind)
+    monkeypatch.setattr(package, "_binding", old)
+    monkeypatch.setitem(sys.modules, "paper_2410_15526_amd._binding", old)
+    with pytest.warns(RuntimeWarning, match="other entry points"):
+        _takes_the_general_path()
+
+
+@pytest.mark.cpu_only
 def test_leaves_what_is_not_on_a_gpu_or_not_ordinary():
     f = native()
     t = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)  # noqa: E731
