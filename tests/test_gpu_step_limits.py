@@ -6,7 +6,7 @@ import pytest
 from paper_2410_15526_amd import sdp4
 from tests import _step as ref
 from tests._gpu import say, torch
-from tests.test_gpu_step import close, dt, f64, normal, scratch, table_for
+from tests.test_gpu_step import check_logprob, close, dt, f64, normal, scratch, table_for
 
 pytestmark = pytest.mark.gpu
 
@@ -239,3 +239,96 @@ def test_qk_inside_heads_of_query_key_and_value(tokens, heads, heads_first, dtyp
         close(x, wx, bx, "dx")
         close(w, *ww, "dw")
     assert t.equal(gv, gv0)
+
+
+# ---------------------------------------------------------------------------
+# forms of their own for long rows and many rows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [262145, 300007, 1 << 20])
+def test_rows_of_more_than_64_slices(vocab, dtype):
+    """The longest rows, whose parts a wave joins in several rounds: ordinary, ties, masks, a peak at the end, NaN."""
+    t = torch()
+    say("long rows", vocab, dtype)
+    x = normal(rng(vocab), 7, vocab, dtype=dtype, scale=3.0)
+    x[1] = (t.arange(vocab, device="cuda") % 5).to(x.dtype)
+    x[2] = float("-inf")
+    x[2, vocab - 2:] = 1.0
+    x[3, :-5] = t.finfo(x.dtype).min
+    x[4, -1] = 90.0
+    x[5] = 0.0
+    tg = t.tensor([5, 4, vocab - 1, vocab - 3, vocab - 1, 0, 1], device="cuda")
+    for k in (0, 1, 8, 9, 32):
+        check_logprob(x, tg, k, dtype=dtype)
+    x[0, vocab - 1] = float("nan")
+    lp, ls, en = empties(7)
+    tl, ti = t.zeros(7, 9, device="cuda"), t.zeros(7, 9, dtype=t.int64, device="cuda")
+    sdp4.sdp4_token_logprob(x, tg, 9, lp, ls, en, tl, ti, scratch(sdp4.sdp4_token_logprob_workspace(7, vocab, 9)))
+    assert bool(t.isnan(tl[0]).all()) and bool((ti[0] == -1).all()) and not bool(t.isnan(tl[1:]).any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_loss_of_rows_of_more_than_64_slices(dtype):
+    t = torch()
+    vocab = 300007
+    x = normal(rng(8), 3, vocab, dtype=dtype, scale=3.0)
+    tg = t.tensor([0, vocab - 1, -1], device="cuda")
+    gs = [normal(rng(9), 3, scale=0.5) for _ in range(3)]
+    xs, tn, gn = f64(x), tg.cpu().numpy(), [f64(a) for a in gs]
+    logp, lse, ent = ref.token_stats(xs, tn)
+    d, (lp, ls, en) = t.full_like(x, float("nan")), empties(3)
+    sdp4.sdp4_token_loss(x, tg, *gs, lp, ls, en, d, scratch(sdp4.sdp4_token_logprob_workspace(3, vocab)))
+    for got, want, b, what in zip((lp, ls, en), (logp, lse, ent), ref.stats_bounds(xs, logp, ent), ("logp", "lse", "entropy")):
+        close(got, want, b, what)
+    want, bound = grad_from(xs, tn, f64(ls), f64(en), *gn, dtype)
+    close(d, want, bound, "dlogits")
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("rows,cols", [(6203, 5120), (6203, 5119), (21001, 515)])
+def test_dropout_gradient_of_many_rows(rows, cols, x_dtype, y_dtype):
+    """Several batches of rows for each block, in place where the types are one: the loop over whole batches, the one at
+    the edges, and what both do to the generator's position."""
+    t = torch()
+    say("dropout gradient", rows, cols, x_dtype, y_dtype)
+    dy = normal(rng(rows + cols), rows, cols, dtype=y_dtype)
+    (want, bound), (wb, bb) = ref.dropout_grad(f64(dy), 0.1, 11, 24, x_dtype)
+    dx = dy if x_dtype == y_dtype else t.full((rows, cols), float("nan"), dtype=dt(x_dtype), device="cuda")
+    db = t.full((cols,), float("nan"), device="cuda")
+    sdp4.sdp4_dropout_add_grad(dy, 0.1, 11, 24, dx, db, scratch(sdp4.sdp4_dropout_grad_workspace(rows, cols)))
+    close(dx, want, bound, "dx")
+    close(db, wb, bb, "dbias")
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [("f32", "bf16")])
+@pytest.mark.parametrize("rows,cols", [(1, 7), (17, 64), (257, 515), (9, 4097), (4099, 96)])
+def test_dropout_gradient_from_bfloat16_to_float32(rows, cols, x_dtype, y_dtype):
+    t = torch()
+    dy = normal(rng(rows), rows, cols, dtype=y_dtype)
+    (want, bound), (wb, bb) = ref.dropout_grad(f64(dy), 0.25, 7, 16, x_dtype)
+    dx, db = t.full((rows, cols), float("nan"), dtype=dt(x_dtype), device="cuda"), t.full((cols,), float("nan"), device="cuda")
+    sdp4.sdp4_dropout_add_grad(dy, 0.25, 7, 16, dx, db, scratch(sdp4.sdp4_dropout_grad_workspace(rows, cols)))
+    close(dx, want, bound, "dx")
+    close(db, wb, bb, "dbias")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,hq,hk,dim,rot,inter", [(4001, 11, 3, 64, 64, False), (2003, 40, 8, 128, 64, True),
+                                                        (3001, 7, 7, 67, 10, False)])
+def test_qk_gradient_with_several_heads_a_lane_group(tokens, hq, hk, dim, rot, inter, dtype):
+    """Numbers of heads that do not divide the step from one of a group's heads to its next."""
+    t = torch()
+    say("qk gradient", tokens, hq, hk, dim, rot, inter, dtype)
+    g = rng(tokens)
+    q, k = normal(g, tokens, hq, dim, dtype=dtype), normal(g, tokens, hk, dim, dtype=dtype)
+    gq, gk = normal(g, tokens, hq, dim, dtype=dtype), normal(g, hk, tokens, dim, dtype=dtype).transpose(0, 1)
+    qw, kw, tab = normal(g, dim, dtype=dtype), normal(g, dim, dtype=dtype), table_for(tokens, rot)
+    want = [ref.qk_grad(f64(y), f64(x), f64(w), 1e-6, f64(tab), np.arange(tokens), inter, dtype)
+            for y, x, w in ((gq, q, qw), (gk, k, kw))]
+    dq, dk = t.full_like(q, float("nan")), t.full_like(k, float("nan"))
+    dw = [t.full((dim,), float("nan"), device="cuda") for _ in range(2)]
+    sdp4.sdp4_qk_norm_rope_grad(gq, gk, q, k, qw, kw, 1e-6, tab, None, dq, dk, *dw,
+                                scratch(sdp4.sdp4_qk_grad_workspace(tokens, hq, hk, dim)), interleaved=inter)
+    for x, w, ((wx, bx), ww) in ((dq, dw[0], want[0]), (dk, dw[1], want[1])):
+        close(x, wx, bx, "dx")
+        close(w, *ww, "dw")
