@@ -334,7 +334,9 @@ int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
  *   p         in [0, 1]
  *   seed      64-bit key; offset: multiple of 8 (EALIGN otherwise).  Calls that
  *             must not share a mask take ranges [offset, offset + rows * ceil8(cols))
- *             that do not overlap, or other seeds
+ *             that do not overlap, or other seeds.  Both are arguments by value: a
+ *             call captured in a HIP graph draws the same mask in every replay, so a
+ *             captured training step updates them in its node (or is captured again)
  *   y         [rows][cols] y_dtype out, row stride y_stride; may be x or residual
  */
 int sdp4_dropout_add(const void *x, int x_dtype, int64_t x_stride, const void *bias, const void *residual,
@@ -370,7 +372,7 @@ int64_t sdp4_dropout_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes
  * counts where -logp is as small.
  *
  *   logits   [rows][vocab] dtype, row stride `stride`; what lies between
- *            vocab and stride is not read
+ *            vocab and stride does not matter
  *   vocab    1 .. SDP4_MAX_VOCAB
  *   targets  [rows] or NULL; a negative target means none (logp = 0), one
  *            >= vocab is a mistake (logp = NaN)
@@ -450,7 +452,9 @@ typedef struct {
  *      pair i of the first rot_dim elements (a, b) -> (a c - b s, b c + a s)
  * with (c, s) = (table[pos][i], table[pos][rot_dim / 2 + i]); the other
  * elements are u.  A position outside the table makes the rotated elements
- * NaN.
+ * NaN (backward with a norm the head's others too).  Squares are float32:
+ * mean(x^2) + eps has to be one of its normal numbers, so heads as a whole
+ * stay below 1e19 and, with eps = 0, above 1e-18.
  *
  *   q, k          inputs; k may be NULL (queries only)
  *   q_out, k_out  outputs with the same numbers of heads, any strides; each

@@ -2,9 +2,12 @@
 
 Each function allocates its outputs (and a workspace where the call needs
 one) and calls the entry points of :mod:`paper_2410_15526_amd.sdp4`; a
-program that keeps its buffers calls those directly.  Broadcast or transposed
-arguments are copied; what else must hold of them is checked there.  The
-gradients have no gradients themselves: torch raises where one is asked for.
+program that keeps its buffers, wants alternatives or has gradients by entropy
+and logsumexp for the loss in one pass calls those directly.  Broadcast or
+transposed arguments are copied; what else must hold of them is checked there:
+matrices have two dimensions, heads three, and norm weights the type of the
+heads.  The gradients have no gradients themselves: torch raises where one is
+asked for.
 """
 from __future__ import annotations
 
@@ -62,7 +65,8 @@ class _DropoutAdd(torch.autograd.Function):
 
 def dropout_add(x, bias, residual, p: float, seed: int, offset: int):
     """residual + dropout(x + bias) of matrices [rows, cols]; bias and residual
-    may be None.  (seed, offset) name the mask, see ``sdp4_dropout_add``."""
+    may be None.  (seed, offset) name the mask, see ``sdp4_dropout_add``: a step
+    captured in a HIP graph draws the same one in every replay."""
     return _DropoutAdd.apply(_laid_out(x), _dense(bias), None if residual is None else _laid_out(residual), p, seed, offset)
 
 
