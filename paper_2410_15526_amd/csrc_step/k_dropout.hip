@@ -343,12 +343,6 @@ __global__ __launch_bounds__(kSumThreads) void k_sum_parts(Parts first, Parts se
     }
 }
 
-template <class T, class P>
-Rows<T *> typed(Rows<P> r)
-{
-    return {static_cast<T *>(r.p), r.stride};
-}
-
 // The split of the backward pass: 8-element columns side by side in a block, and the blocks that share a column's rows --
 // about kGradBlocks in all, with 8 rows of a lane for each.
 struct GradSplit {

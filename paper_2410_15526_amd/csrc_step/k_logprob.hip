@@ -806,12 +806,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_token_loss(Rows<const T *> x, in
     });
 }
 
-template <class T, class P>
-Rows<T *> typed(Rows<P> r)
-{
-    return {static_cast<T *>(r.p), r.stride};
-}
-
 // How a row is cut into slices of 64 * nc chunks: the largest that still give 2048 waves, two to a SIMD, and no more than
 // 64 if that can be, which the join reads in one go.  1024 and 4096 waves take the same time within 3 % for 4 to 2048 rows
 // of 131072 and 32000.  Slices of 2048 logits at most instead of 4096: 4096 x 50001 with 5 alternatives 88 us against 81,

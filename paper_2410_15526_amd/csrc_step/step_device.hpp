@@ -4,8 +4,10 @@
 // is only as aligned as one element.  Global memory serves 16-byte accesses
 // at any element address, and a wave that reads 64 neighbouring chunks
 // touches one cache line more than from an aligned start: rows are read and
-// written in whole 16-byte chunks wherever they begin, and only a row's last
-// chunk, where it is not whole, goes element by element.
+// written in whole 16-byte chunks wherever they begin.  A row's last chunk,
+// where it is not whole, is read as the row's last whole chunk of elements and
+// shifted, and written element by element.  (The loss and the gradient of log
+// probabilities read bfloat16 rows at odd addresses from the word before.)
 #pragma once
 
 #include "device.hpp"
@@ -270,6 +272,12 @@ SDP4_DEV float max_wave(float v)
     v = fmaxf(v, dpp_f32<kDppRor8>(v));
     v = fmaxf(v, xor_lane<16>(v));
     return fmaxf(v, xor_lane<32>(v));
+}
+
+template <class T, class P>
+Rows<T *> typed(Rows<P> r)
+{
+    return {static_cast<T *>(r.p), r.stride};
 }
 
 // Two calls of a body, for the element types.

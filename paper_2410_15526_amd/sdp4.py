@@ -480,7 +480,9 @@ def _gradients(logits, targets, g_logp, g_entropy, g_lse, dlogits, vocab):
     dp, ddt, dstride, dshape = _matrix(dlogits, "dlogits")
     if ddt != dt or dshape[0] != rows or dshape[1] < vocab:
         raise ValueError("sdp4: dlogits must have the logits' type and rows, and vocab columns or more")
-    return (p, dt, stride, rows, vocab, _vector(targets, (rows,), torch.int64, "targets")),         [_vector(g, (rows,), f32, n) for g, n in ((g_logp, "g_logp"), (g_entropy, "g_entropy"), (g_lse, "g_lse"))],         (dp, dstride, dshape[1])
+    return (p, dt, stride, rows, vocab, _vector(targets, (rows,), torch.int64, "targets")), \
+        [_vector(g, (rows,), f32, n) for g, n in ((g_logp, "g_logp"), (g_entropy, "g_entropy"), (g_lse, "g_lse"))], \
+        (dp, dstride, dshape[1])
 
 
 def sdp4_token_logprob_grad(logits, targets, lse, entropy, g_logp, g_entropy, g_lse, dlogits, vocab=None, stream=None):
