@@ -9,8 +9,8 @@
 //
 // Forward: a wave takes a slice of a row into registers (up to 4096 logits) and leaves S and T, relative to a logit of
 // the slice, in the workspace; a second launch joins the slices of each row, one wave per row.  A row of one slice is
-// finished by its wave.  For the alternatives each lane also leaves the largest of its 64 logits, and the second launch
-// finds from these which few groups of 64 can hold the row's largest and reads only those again.
+// finished by its wave, unless alternatives are wanted.  For these each lane also leaves the largest of its 64 logits, and the
+// second launch finds from them which few groups of 64 can hold the row's largest and reads only those again.
 //
 // What bounds it: HBM (4096 x 50001 bfloat16 without alternatives 65 us, 6.3 TB/s, float32 122, 6.7), and with bfloat16
 // nearly the vector units too: at the rate of reads 3.5 T logits a second leave 11 issue slots for each, and the kernel
@@ -919,9 +919,9 @@ int token_loss(Rows<const void *> x, int64_t rows, int64_t vocab, const TokenSta
                           typed<T>(dx), width);
     };
     // The fewest waves, then the fewest chunks a lane, that hold the row; longer rows take two launches.  Those where one
-    // would do: 8192 x 1000 14.5 us against 10.1, 4096 x 50000 bfloat16 197 against 150, 4096 x 131072 507 against 405,
-    // float32 4096 x 50000 394 against 299.  (Few long rows leave units empty here, but a loss is taken of many:
-    // 64 x 131072 14.5 against 16.4.)
+    // would do: 8192 x 1000 14.9 us against 10.1, 4096 x 50000 bfloat16 198 against 150, 4096 x 131072 507 against 402,
+    // float32 4096 x 50000 414 against 318.  (Few long rows leave units empty here, but a loss is taken of many:
+    // 64 x 131072 15.7 against 17.7.)
     using std::integral_constant;
     if (chunks <= 256)
         return run(integral_constant<int, 1>{}, integral_constant<int, 4>{});
