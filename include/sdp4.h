@@ -304,7 +304,8 @@ int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
  *             needs 16 bytes.
  *  Aliasing   An output may be the input it replaces (the same address,
  *             element type and strides), or rows of an array whose other
- *             columns are an input; other overlap is EINVAL.
+ *             columns are an input, and heads may lie between the heads of
+ *             another set of the same strides; other overlap is EINVAL.
  *  Inputs     May be infinite or NaN, with the results stated below.
  *  Workspace  Scratch memory for one call, of at least the bytes its helper
  *             names; its contents before and after do not matter.

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void k_qk(Layout l, Side<T> q, Side<T> k, floa
 // Backward.  A block takes every blocks-th run of heads of its side; with DW it adds up the weights' gradient in
 // registers, its lane groups and waves join at the end, and the block's sums go to the workspace.  The next head's loads
 // are under way before the present one's stores: loads that follow stores wait for these.  8192 x 48 bfloat16 heads of 128:
-// 306 MB in 51 us, 6.0 TB/s, and 4.5 for the sums over the blocks; without weight gradients 54.
+// 306 MB in 51 us, 6.0 TB/s, and 4.5 for the sums over the blocks; without weight gradients 55.
 template <class T, class K, bool DW>
 __global__ __launch_bounds__(256) void k_qk_grad(Layout l, Side<T> q, Side<T> k, float eps, Rope rope)
 {
