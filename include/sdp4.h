@@ -292,8 +292,9 @@ int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
  *
  * The streaming passes of a decoder's training step that stand between its
  * matrix products and make the gradients sdp4_grad_quant takes: bias +
- * dropout + residual, norm and rotation of queries and keys, and the log
- * probabilities of the target tokens, each with its backward pass.
+ * dropout + residual, norm and rotation of queries and keys, the log
+ * probabilities of the target tokens, attention, the norms between blocks and
+ * the embedding, each with its backward pass.
  *
  * They keep the conventions above (caller-owned device memory, checked
  * arguments, one stream, no state) with these differences:
@@ -318,6 +319,10 @@ int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
 #define SDP4_MAX_TOP 32                      /* alternatives of a row */
 #define SDP4_MAX_VOCAB ((int64_t)1 << 20)    /* logits of a row */
 #define SDP4_MAX_HEAD_DIM 512                /* elements of a head */
+#define SDP4_MIN_ATTENTION_DIM 8             /* elements of a head, for attention */
+#define SDP4_MAX_ATTENTION_DIM 256
+#define SDP4_MAX_TOKENS ((int64_t)1 << 30)   /* rows of a packed batch; its sequences */
+#define SDP4_MAX_HIDDEN 16384                /* columns of a normed row */
 
 /*
  * Bias, dropout and residual:
@@ -490,6 +495,148 @@ int64_t sdp4_qk_grad_workspace(int64_t tokens, int q_heads, int k_heads, int hea
  */
 int sdp4_rope_table(const double *inv_freq, int half, int64_t start, int64_t rows, double scale, float *table,
                     void *stream);
+
+/* Causal attention over packed sequences, shared by the forward and backward pass. */
+typedef struct {
+    int dtype;               /* of all heads */
+    int head_dim;            /* SDP4_MIN_ATTENTION_DIM .. SDP4_MAX_ATTENTION_DIM */
+    float scale;             /* of the scores: > 0, finite */
+    const int64_t *offsets;  /* [sequences + 1] on the device, never falling, 0 .. tokens; NULL: one sequence of all tokens */
+    int64_t sequences;
+} sdp4_attention_params;
+
+/*
+ * Attention of each row to itself and the rows before it in its sequence:
+ * sequence n has rows offsets[n] .. offsets[n + 1] - 1, and for its rows j <= i
+ *      s_ij = scale q_i . k_j,  lse_i = log sum_j exp(s_ij),
+ *      out_i = sum_j exp(s_ij - lse_i) v_j.
+ * The query heads share the key and value heads: head h uses head
+ * h / (q heads / k heads), and k's heads divide q's.  Sequences may be empty.
+ * Rows before the first sequence and behind the last one are not read as keys
+ * (whatever they hold) and their out and lse are left as they were.  Offsets
+ * that fall or leave 0 .. tokens give wrong rows, but touch nothing outside
+ * the arrays.
+ *
+ * What a row must not see does not count, infinite or NaN or not.  An infinity
+ * or NaN that a row sees (its own query included) makes elements of its result
+ * infinite or NaN: those that depend on it, or the whole row.  Of a row whose
+ * scores are all -inf, out is 0 and lse -inf.
+ *
+ * Scores, their sums and the results are float32; with bfloat16 heads the
+ * probabilities are rounded to bfloat16 for their product with the values.
+ *
+ *   q, k, v   k and v have the same number of heads
+ *   out       heads like q, any strides; no overlap with an input
+ *   lse       [q heads][tokens] out, or NULL
+ */
+int sdp4_attention(const sdp4_heads *q, const sdp4_heads *k, const sdp4_heads *v, const sdp4_attention_params *params,
+                   int64_t tokens, const sdp4_heads *out, float *lse, void *stream);
+
+/*
+ * Its backward pass, from the gradient of out:
+ *      p_ij = exp(s_ij - lse_i),  ds_ij = p_ij (dout_i . v_j - dout_i . out_i),
+ *      dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+ *      dv_j = sum_i p_ij dout_i,
+ * dk and dv summed over the query heads that share the head, too.  Rows in no
+ * sequence are left as they were; what must not be seen does not count, as
+ * above.  With bfloat16 heads p and ds are rounded to bfloat16 for the
+ * products.
+ *
+ *   out, lse     as sdp4_attention left them
+ *   dq, dk, dv   heads like q, k, v; no overlap with an input or each other
+ *   workspace    sdp4_attention_grad_workspace() bytes, which serve any smaller
+ *                number of tokens too
+ */
+int sdp4_attention_grad(const sdp4_heads *dout, const sdp4_heads *q, const sdp4_heads *k, const sdp4_heads *v,
+                        const sdp4_heads *out, const float *lse, const sdp4_attention_params *params, int64_t tokens,
+                        const sdp4_heads *dq, const sdp4_heads *dk, const sdp4_heads *dv, void *workspace,
+                        int64_t workspace_bytes, void *stream);
+int64_t sdp4_attention_grad_workspace(int64_t tokens, int q_heads, int k_heads, int head_dim); /* -1: out of range */
+
+/* The joint of two blocks, shared by the forward and backward pass. */
+typedef struct {
+    int x_dtype;             /* of a block's output (branch), the next one's input (h) and the weights */
+    int y_dtype;             /* of the residual stream */
+    int post_norm;           /* 0: no norm behind the block */
+    float post_eps, pre_eps; /* >= 0, finite */
+    const void *post_weight; /* [cols], or NULL for ones; also without a post norm */
+    const void *pre_weight;  /* [cols], or NULL for ones */
+    const float *gate;       /* [rows], or NULL for ones */
+    float branch_scale, residual_scale; /* finite */
+} sdp4_block_params;
+
+/*
+ * The norm behind a block, its gate and scale, the residual stream, and the
+ * norm in front of the next block, in one pass over the rows:
+ *      u = branch / sqrt(mean(branch^2) + post_eps) * post_weight
+ *          (branch * post_weight without post_norm),
+ *      y = residual_scale * residual + branch_scale * gate * u,
+ *      h = y / sqrt(mean(y^2) + pre_eps) * pre_weight,
+ * h from y before y is rounded.  As for heads, the squares are float32.  The
+ * row sums take a row as a whole: an infinity or NaN in it reaches all of it.
+ *
+ *   branch    [rows][cols] x_dtype, or NULL (none; then without post_norm,
+ *             post_weight and gate: an RMS norm of the residual stream)
+ *   residual  [rows][cols] y_dtype, or NULL (none); one of both is there
+ *   y         [rows][cols] y_dtype out, or NULL (not wanted); may be an input
+ *   h         [rows][cols] x_dtype out, or NULL; may be an input
+ *   cols      0 .. SDP4_MAX_HIDDEN
+ */
+int sdp4_block_norm(const void *branch, int64_t branch_stride, const void *residual, int64_t residual_stride, int64_t rows,
+                    int64_t cols, const sdp4_block_params *params, void *y, int64_t y_stride, void *h, int64_t h_stride,
+                    void *stream);
+
+/*
+ * Its backward pass, from the gradients by h and by y:
+ *      t = dy + the gradient of h by y, times dh,
+ *      dresidual = residual_scale t,  dbranch = the gradient of u by branch, times branch_scale gate t,
+ *      dpost_weight = sum over rows of branch_scale gate t branch / sqrt(...),
+ *      dpre_weight = sum over rows of dh y / sqrt(...),
+ *      dgate = branch_scale sum over columns of t u.
+ *
+ *   dh, dy     gradients of h and y; NULL: zero (one of both is there)
+ *   branch     as it went in; NULL if neither dbranch through a post norm nor
+ *              dpost_weight nor dgate is wanted
+ *   y          as it came out (NULL without dh)
+ *   dbranch, dresidual, dpost_weight [cols], dpre_weight [cols], dgate [rows]
+ *              out, the last three float32; each NULL if not wanted (a weight's
+ *              needs the weight, dpre_weight dh too, dgate the gate).  dbranch
+ *              and dresidual may be inputs
+ *   workspace  sdp4_block_norm_grad_workspace() bytes, with a weight gradient
+ */
+int sdp4_block_norm_grad(const void *dh, int64_t dh_stride, const void *dy, int64_t dy_stride, const void *branch,
+                         int64_t branch_stride, const void *y, int64_t y_stride, int64_t rows, int64_t cols,
+                         const sdp4_block_params *params, void *dbranch, int64_t dbranch_stride, void *dresidual,
+                         int64_t dresidual_stride, float *dpost_weight, float *dpre_weight, float *dgate, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+int64_t sdp4_block_norm_grad_workspace(int64_t rows, int64_t cols); /* -1 for sizes out of range */
+
+/*
+ * Rows of a table by token: out[r] = scale * table[tokens[r]].  A negative
+ * token gives zeros (padding), one >= vocab is a mistake (NaN).
+ *
+ *   tokens  [rows]; table [vocab][cols] table_dtype; out [rows][cols] out_dtype
+ *   vocab   1 .. SDP4_MAX_VOCAB; scale finite
+ */
+int sdp4_embedding(const int64_t *tokens, int64_t rows, const void *table, int table_dtype, int64_t table_stride, int64_t vocab,
+                   int64_t cols, float scale, void *out, int out_dtype, int64_t out_stride, void *stream);
+
+/*
+ * The table's gradient: dtable[v] = scale * (the sum of dout[r] over the rows r
+ * with token v), a float32 sum in an order that the tokens alone decide,
+ * rounded once.  Tokens outside the table count for nothing.
+ *
+ *   accumulate  0: the whole of dtable is written, rows of no token with zeros;
+ *               else the sums are added to what dtable holds, and rows of no
+ *               token are left alone
+ *   dtable      [vocab][cols] dtable_dtype
+ *   workspace   sdp4_embedding_grad_workspace() bytes, which serve any smaller
+ *               number of rows too
+ */
+int sdp4_embedding_grad(const int64_t *tokens, int64_t rows, const void *dout, int dout_dtype, int64_t dout_stride, int64_t vocab,
+                        int64_t cols, float scale, int accumulate, void *dtable, int dtable_dtype, int64_t dtable_stride,
+                        void *workspace, int64_t workspace_bytes, void *stream);
+int64_t sdp4_embedding_grad_workspace(int64_t rows, int64_t vocab, int64_t cols); /* -1 for sizes out of range */
 
 /* Pure helpers (no device work). */
 int64_t sdp4_codes_bytes(int64_t n, int bits);  /* n * bits / 8, or -1 if bits not 4 or 8 */

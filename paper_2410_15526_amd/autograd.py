@@ -147,6 +147,123 @@ def token_loss(logits, targets, weights, vocab: int | None = None):
         return -(weights * logp).sum(), d
 
 
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, scale):
+        make = torch.empty if offsets is None else torch.zeros      # rows in no sequence are left as they were
+        out = make(q.shape, dtype=q.dtype, device=q.device)
+        lse = make(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+        sdp4.sdp4_attention(q, k, v, scale, offsets, out, lse)
+        ctx.save_for_backward(q, k, v, offsets, out, lse)
+        ctx.scale = scale
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        q, k, v, offsets, out, lse = ctx.saved_tensors
+        make = torch.empty if offsets is None else torch.zeros
+        grads = [make(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v)]
+        work = _workspace(sdp4.sdp4_attention_grad_workspace(q.shape[0], q.shape[1], k.shape[1], q.shape[2]), q.device)
+        sdp4.sdp4_attention_grad(_laid_out(dout), q, k, v, out, lse, ctx.scale, offsets, *grads, work)
+        return *grads, None, None
+
+
+def attention(q, k, v, offsets=None, scale: float | None = None):
+    """Causal attention of heads [tokens, heads, head_dim] over packed sequences
+    (rows offsets[n] .. offsets[n + 1] - 1; None: one sequence), see
+    ``sdp4_attention``; scale is head_dim^-1/2 by default.  Rows in no sequence
+    come out as zeros, and so do their gradients."""
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    return _Attention.apply(_laid_out(q), _laid_out(k), _laid_out(v), _dense(offsets), float(scale))
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, branch, residual, post_weight, pre_weight, gate, post_eps, pre_eps, branch_scale, residual_scale, dtype):
+        stream = branch if residual is None else residual
+        y = torch.empty(stream.shape, dtype=stream.dtype, device=stream.device)
+        h = torch.empty(stream.shape, dtype=dtype, device=stream.device)
+        sdp4.sdp4_block_norm(branch, residual, post_eps, post_weight, gate, branch_scale, residual_scale, y, pre_eps, pre_weight, h)
+        ctx.save_for_backward(branch, y, post_weight, pre_weight, gate)
+        ctx.args = (post_eps, pre_eps, branch_scale, residual_scale, residual is not None)
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        branch, y, post_weight, pre_weight, gate = ctx.saved_tensors
+        post_eps, pre_eps, branch_scale, residual_scale, with_residual = ctx.args
+        need = ctx.needs_input_grad
+        if (dy is None and dh is None) or not any(need[:5]):
+            return (None,) * 10
+        like = lambda x: torch.empty(x.shape, dtype=x.dtype, device=x.device)  # noqa: E731
+        rows, cols = y.shape
+        dbranch = like(branch) if branch is not None and need[0] else None
+        dresidual = like(y) if with_residual and need[1] else None
+        dpost = _f32(y.device, cols) if post_weight is not None and need[2] else None
+        dpre = _f32(y.device, cols) if pre_weight is not None and need[3] and dh is not None else None
+        dgate = _f32(y.device, rows) if gate is not None and need[4] else None
+        if any(d is not None for d in (dbranch, dresidual, dpost, dpre, dgate)):
+            work = _workspace(sdp4.sdp4_block_norm_grad_workspace(rows, cols), y.device) if dpost is not None or dpre is not None \
+                else None
+            sdp4.sdp4_block_norm_grad(None if dh is None else _laid_out(dh), None if dy is None else _laid_out(dy), branch, y,
+                                      post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight, dbranch,
+                                      dresidual, dpost, dpre, dgate, work)
+        if need[3] and pre_weight is not None and dpre is None:      # no gradient by h
+            dpre = torch.zeros(cols, dtype=torch.float32, device=y.device)
+        dpost, dpre = (None if d is None else d.to(w.dtype) for d, w in ((dpost, post_weight), (dpre, pre_weight)))
+        return dbranch, dresidual, dpost, dpre, dgate, None, None, None, None, None
+
+
+def block_norm(branch, residual, pre_weight=None, pre_eps: float = 1e-6, *, post_weight=None, post_eps: float | None = None,
+               gate=None, branch_scale: float = 1.0, residual_scale: float = 1.0, dtype=None):
+    """(y, h) of matrices [rows, cols]: y = residual_scale * residual +
+    branch_scale * gate * u with u the branch, normed if post_eps is not None and
+    times post_weight if there is one, and h the RMS norm of y times pre_weight;
+    see ``sdp4_block_norm``.  Without a branch y is the scaled residual stream.
+    gate [rows] is float32; h has the branch's type, or ``dtype`` without one
+    (the residual stream's by default)."""
+    if branch is not None:
+        dtype = branch.dtype
+    elif dtype is None:
+        dtype = residual.dtype
+    rows = lambda x: None if x is None else _laid_out(x)  # noqa: E731
+    return _BlockNorm.apply(rows(branch), rows(residual), _dense(post_weight), _dense(pre_weight), _dense(gate),
+                            None if post_eps is None else float(post_eps), float(pre_eps), float(branch_scale),
+                            float(residual_scale), dtype)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale, dtype):
+        out = torch.empty(tokens.shape[0], table.shape[1], dtype=dtype, device=table.device)
+        sdp4.sdp4_embedding(tokens, table, scale, out)
+        ctx.save_for_backward(tokens)
+        ctx.args = (table.shape, table.dtype, scale)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        tokens, = ctx.saved_tensors
+        shape, dtype, scale = ctx.args
+        dout = _laid_out(dout)
+        dtable = torch.empty(shape, dtype=dtype, device=dout.device)
+        work = _workspace(sdp4.sdp4_embedding_grad_workspace(tokens.shape[0], *shape), dout.device)
+        sdp4.sdp4_embedding_grad(tokens, dout, scale, dtable, work)
+        return None, dtable, None, None
+
+
+def embedding(tokens, table, scale: float = 1.0, dtype=None):
+    """scale * table[tokens] for tokens [rows] (negative: zeros), in the table's
+    type by default; see ``sdp4_embedding``.  The table's gradient is summed
+    token by token in float32."""
+    return _Embedding.apply(_dense(tokens), _laid_out(table), float(scale), table.dtype if dtype is None else dtype)
+
+
 def rope_table(rows: int, rot_dim: int, base: float = 10000.0, stretch: float = 1.0, ramp: tuple | None = None,
                scale: float = 1.0, start: int = 0, device="cuda"):
     """Table of ``sdp4_qk_norm_rope`` for positions start .. start + rows - 1.

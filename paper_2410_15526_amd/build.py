@@ -22,7 +22,9 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsdp4.so")
 SOURCES = ["k_qwd.hip", "k_grad.hip", "k_sr.hip", "k_reduce.hip", "k_reduce_f32_in8.hip", "k_reduce_f32_in4.hip",
            "launch.cpp", "abi.cpp",
-           *(os.path.join("..", "csrc_step", f) for f in ("k_dropout.hip", "k_logprob.hip", "k_qk.hip", "abi_step.cpp"))]
+           *(os.path.join("..", "csrc_step", f) for f in ("k_attention.hip", "k_attention_grad.hip", "k_block_norm.hip",
+                                                         "k_dropout.hip", "k_embedding.hip", "k_logprob.hip", "k_qk.hip",
+                                                         "abi_step.cpp", "abi_layer.cpp"))]
 BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 

@@ -39,11 +39,26 @@ struct Entry {
     decltype(&sdp4_token_loss) token_loss;
     decltype(&sdp4_qk_norm_rope) qk_norm_rope;
     decltype(&sdp4_qk_norm_rope_grad) qk_norm_rope_grad;
+    decltype(&sdp4_attention) attention;
+    decltype(&sdp4_attention_grad) attention_grad;
+    decltype(&sdp4_block_norm) block_norm;
+    decltype(&sdp4_block_norm_grad) block_norm_grad;
+    decltype(&sdp4_embedding) embedding;
+    decltype(&sdp4_embedding_grad) embedding_grad;
 } lib; // set once by bind()
 
 // Arguments of one call; `ok` turns false at the first that is not ordinary.
 struct Args {
     bool ok = true;
+    int device = -1; // of the tensors so far
+    bool devices = false; // they lie on several
+
+    void note(const at::Tensor &t)
+    {
+        const int d = t.get_device();
+        devices |= device >= 0 && d != device;
+        device = d;
+    }
 
     // n or a tensor's element count in its place
     int64_t count(PyObject *n, PyObject *of)
@@ -84,6 +99,7 @@ struct Args {
             ok = false;
             return nullptr;
         }
+        note(t);
         return &t;
     }
     // address of an array of at least `bytes`: a tensor, or an address whose size is the caller's
@@ -396,6 +412,7 @@ struct StepArgs : Args {
             ok = false;
             return nullptr;
         }
+        note(t);
         return &t;
     }
     int element(const at::Tensor &t)
@@ -721,10 +738,184 @@ PyObject *py_qk_norm_rope_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
     });
 }
 
+// Attention, block norms and the embedding launch on the current device: where their tensors lie on another one, or on
+// several, the general path sees to it.
+void on_current_device(StepArgs &a)
+{
+    if (a.ok && (a.devices || a.device != (int)c10::hip::current_device()))
+        a.ok = false;
+}
+
+sdp4_attention_params attention_params(StepArgs &a, const StepArgs::Arr &q, PyObject *scale, PyObject *offsets)
+{
+    sdp4_attention_params p{};
+    if (q.dim < 1 || q.dim > SDP4_MAX_ATTENTION_DIM) {
+        a.ok = false;
+        return p;
+    }
+    p.dtype = q.dtype, p.head_dim = (int)q.dim, p.scale = a.real(scale);
+    if (offsets != Py_None) {
+        const at::Tensor *t = a.tensor(offsets);
+        if (!t || t->dim() != 1 || t->scalar_type() != at::kLong || t->size(0) < 1) {
+            a.ok = false;
+            return p;
+        }
+        p.offsets = static_cast<const int64_t *>(t->data_ptr()), p.sequences = t->size(0) - 1;
+    }
+    return p;
+}
+
+// q, k, v, scale, offsets, out, lse, stream
+PyObject *py_attention(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.attention, nargs, 8, [&](StepArgs &a) {
+        const auto q = a.heads(v[0]), k = a.heads(v[1]), val = a.heads(v[2], &k), out = a.heads(v[5], &q);
+        if (!beside(k, q))
+            a.ok = false;
+        const sdp4_attention_params p = attention_params(a, q, v[3], v[4]);
+        float *lse = a.exact_as<float>(v[6], q.h.heads, q.tokens);
+        on_current_device(a);
+        void *stream = a.stream(v[7]);
+        return [=] { return lib.attention(&q.h, &k.h, &val.h, &p, q.tokens, &out.h, lse, stream); };
+    });
+}
+
+// dout, q, k, v, out, lse, scale, offsets, dq, dk, dv, workspace, stream
+PyObject *py_attention_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.attention_grad, nargs, 13, [&](StepArgs &a) {
+        const auto q = a.heads(v[1]), dout = a.heads(v[0], &q), k = a.heads(v[2]), val = a.heads(v[3], &k), out = a.heads(v[4], &q),
+                   dq = a.heads(v[8], &q), dk = a.heads(v[9], &k), dv = a.heads(v[10], &k);
+        if (!beside(k, q) || v[5] == Py_None)
+            a.ok = false;
+        const float *lse = a.exact_as<const float>(v[5], q.h.heads, q.tokens);
+        const sdp4_attention_params p = attention_params(a, q, v[6], v[7]);
+        int64_t bytes;
+        void *work = a.scratch(v[11], bytes);
+        on_current_device(a);
+        void *stream = a.stream(v[12]);
+        return [=] {
+            return lib.attention_grad(&dout.h, &q.h, &k.h, &val.h, &out.h, lse, &p, q.tokens, &dq.h, &dk.h, &dv.h, work, bytes,
+                                      stream);
+        };
+    });
+}
+
+// A matrix beside others of its shape, or none.  The types of the branch's (0) and the residual stream's (1) have to agree.
+struct BlockArgs {
+    StepArgs &a;
+    int64_t rows = -1, cols = 0;
+    int types[2] = {-1, -1};
+    StepArgs::Mat take(PyObject *o, int kind)
+    {
+        if (o == Py_None)
+            return {};
+        const StepArgs::Mat m = a.matrix(o);
+        if ((rows >= 0 && (m.rows != rows || m.cols != cols)) || (types[kind] >= 0 && types[kind] != m.dtype) || !m.p)
+            a.ok = false; // an empty matrix has no address: the general path passes its sizes on
+        rows = m.rows, cols = m.cols, types[kind] = m.dtype;
+        return m;
+    }
+    sdp4_block_params params(PyObject *post_eps, PyObject *post_weight, PyObject *gate, PyObject *branch_scale,
+                             PyObject *residual_scale, PyObject *pre_eps, PyObject *pre_weight)
+    {
+        sdp4_block_params p{};
+        if (rows < 0) {
+            a.ok = false;
+            return p;
+        }
+        p.x_dtype = types[0] >= 0 ? types[0] : types[1], p.y_dtype = types[1] >= 0 ? types[1] : types[0];
+        const at::ScalarType type = p.x_dtype == SDP4_F32 ? at::kFloat : at::kBFloat16;
+        p.post_norm = post_eps != Py_None;
+        p.post_eps = p.post_norm ? a.real(post_eps) : 0.0f;
+        p.pre_eps = pre_eps != Py_None ? a.real(pre_eps) : 0.0f;
+        p.post_weight = a.exact(post_weight, type, cols), p.pre_weight = a.exact(pre_weight, type, cols);
+        p.gate = a.exact_as<const float>(gate, rows);
+        p.branch_scale = a.real(branch_scale), p.residual_scale = a.real(residual_scale);
+        return p;
+    }
+};
+
+// branch, residual, post_eps, post_weight, gate, branch_scale, residual_scale, y, pre_eps, pre_weight, h, stream
+PyObject *py_block_norm(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.block_norm, nargs, 12, [&](StepArgs &a) {
+        BlockArgs s{a};
+        const auto b = s.take(v[0], 0), r = s.take(v[1], 1), y = s.take(v[7], 1), h = s.take(v[10], 0);
+        const sdp4_block_params p = s.params(v[2], v[3], v[4], v[5], v[6], v[8], v[9]);
+        const int64_t rows = s.rows, cols = s.cols;
+        on_current_device(a);
+        void *stream = a.stream(v[11]);
+        return [=] {
+            return lib.block_norm(b.p, b.stride, r.p, r.stride, rows, cols, &p, y.p, y.stride, h.p, h.stride, stream);
+        };
+    });
+}
+
+// dh, dy, branch, y, post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight, dbranch, dresidual,
+// dpost_weight, dpre_weight, dgate, workspace, stream
+PyObject *py_block_norm_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.block_norm_grad, nargs, 18, [&](StepArgs &a) {
+        BlockArgs s{a};
+        const auto dh = s.take(v[0], 0), dy = s.take(v[1], 1), b = s.take(v[2], 0), y = s.take(v[3], 1), db = s.take(v[11], 0),
+                   dr = s.take(v[12], 1);
+        const sdp4_block_params p = s.params(v[4], v[5], v[6], v[7], v[8], v[9], v[10]);
+        const int64_t rows = s.rows, cols = s.cols;
+        float *dpost = a.exact_as<float>(v[13], cols), *dpre = a.exact_as<float>(v[14], cols), *dgate = a.exact_as<float>(v[15], rows);
+        int64_t bytes;
+        void *work = a.scratch(v[16], bytes);
+        on_current_device(a);
+        void *stream = a.stream(v[17]);
+        return [=] {
+            return lib.block_norm_grad(dh.p, dh.stride, dy.p, dy.stride, b.p, b.stride, y.p, y.stride, rows, cols, &p, db.p,
+                                       db.stride, dr.p, dr.stride, dpost, dpre, dgate, work, bytes, stream);
+        };
+    });
+}
+
+// tokens, table, scale, out, stream
+PyObject *py_embedding(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.embedding, nargs, 5, [&](StepArgs &a) {
+        const auto t = a.matrix(v[1]), o = a.matrix(v[3]);
+        auto ids = a.exact_as<const int64_t>(v[0], o.rows);
+        if (t.cols != o.cols || v[0] == Py_None || !t.p || !o.p)
+            a.ok = false;
+        const float scale = a.real(v[2]);
+        on_current_device(a);
+        void *stream = a.stream(v[4]);
+        return [=] {
+            return lib.embedding(ids, o.rows, t.p, t.dtype, t.stride, t.rows, t.cols, scale, o.p, o.dtype, o.stride, stream);
+        };
+    });
+}
+
+// tokens, dout, scale, dtable, workspace, accumulate, stream
+PyObject *py_embedding_grad(PyObject *, PyObject *const *v, Py_ssize_t nargs)
+{
+    return run_step(lib.embedding_grad, nargs, 7, [&](StepArgs &a) {
+        const auto d = a.matrix(v[1]), t = a.matrix(v[3]);
+        auto ids = a.exact_as<const int64_t>(v[0], d.rows);
+        if (t.cols != d.cols || v[0] == Py_None || !t.p || !d.p)
+            a.ok = false;
+        const float scale = a.real(v[2]);
+        int64_t bytes;
+        void *work = a.scratch(v[4], bytes);
+        const int accumulate = a.flag(v[5]);
+        on_current_device(a);
+        void *stream = a.stream(v[6]);
+        return [=] {
+            return lib.embedding_grad(ids, d.rows, d.p, d.dtype, d.stride, t.rows, t.cols, scale, accumulate, t.p, t.dtype,
+                                      t.stride, work, bytes, stream);
+        };
+    });
+}
+
 // Addresses of the C entry points, in the order of Entry.
 PyObject *py_bind(PyObject *, PyObject *const *v, Py_ssize_t nargs)
 {
-    constexpr int kEntries = 15;
+    constexpr int kEntries = 21;
     void *p[kEntries];
     if (nargs != kEntries) {
         PyErr_SetString(PyExc_TypeError, "bind: one address for each entry point");
@@ -753,6 +944,12 @@ PyObject *py_bind(PyObject *, PyObject *const *v, Py_ssize_t nargs)
     lib.token_loss = (decltype(lib.token_loss))p[12];
     lib.qk_norm_rope = (decltype(lib.qk_norm_rope))p[13];
     lib.qk_norm_rope_grad = (decltype(lib.qk_norm_rope_grad))p[14];
+    lib.attention = (decltype(lib.attention))p[15];
+    lib.attention_grad = (decltype(lib.attention_grad))p[16];
+    lib.block_norm = (decltype(lib.block_norm))p[17];
+    lib.block_norm_grad = (decltype(lib.block_norm_grad))p[18];
+    lib.embedding = (decltype(lib.embedding))p[19];
+    lib.embedding_grad = (decltype(lib.embedding_grad))p[20];
     Py_RETURN_NONE;
 }
 
@@ -762,7 +959,9 @@ PyMethodDef methods[] = {
     SDP4_METHOD(qwd_decode_sym), SDP4_METHOD(grad_quant),     SDP4_METHOD(grad_quant_sr),  SDP4_METHOD(dequant_reduce),
     SDP4_METHOD(dequant_reduce_sr), SDP4_METHOD(chunk_addresses),
     SDP4_METHOD(dropout_add),   SDP4_METHOD(dropout_add_grad), SDP4_METHOD(token_logprob), SDP4_METHOD(token_logprob_grad),
-    SDP4_METHOD(token_loss),    SDP4_METHOD(qk_norm_rope),    SDP4_METHOD(qk_norm_rope_grad), {nullptr, nullptr, 0, nullptr},
+    SDP4_METHOD(token_loss),    SDP4_METHOD(qk_norm_rope),    SDP4_METHOD(qk_norm_rope_grad),
+    SDP4_METHOD(attention),     SDP4_METHOD(attention_grad),  SDP4_METHOD(block_norm),     SDP4_METHOD(block_norm_grad),
+    SDP4_METHOD(embedding),     SDP4_METHOD(embedding_grad),  {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

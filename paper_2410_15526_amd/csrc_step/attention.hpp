@@ -1,0 +1,312 @@
+// attention.hpp -- device building blocks of the attention kernels: tiles of
+// rows in LDS, matrix fragments, and which rows see which.
+//
+// Matrix instructions take 32 x 16 by 16 x 32 products.  Of an operand, lane l
+// holds eight elements along the summed axis of one row (column) l % 32:
+// places 8 h .. 8 h + 7 with h = l / 32.  Of the 32 x 32 result it holds
+// column l % 32 and rows 8 a + 4 h + b, register 4 a + b.  float32 takes eight
+// 32 x 32 x 2 products for the same fragments.
+//
+// Scores are computed transposed (rows: keys, columns: queries), so that a
+// query's scores lie in two lanes, and the registers of a result, taken eight
+// by eight, are an operand of the next product as they stand: the summed axis
+// may be walked in any order that both operands share, here keys 8 a + 4 h + b
+// of a step of 16 at place 4 a + b.
+#pragma once
+
+#include "step_device.hpp"
+
+#include <limits.h>
+
+namespace sdp4 {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// Eight elements of an operand.
+template <class T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+    bf16x8 v;
+    SDP4_DEV void set(const float (&x)[8])
+    {
+        const u32x4 w{bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3]), bf16x2_rne(x[4], x[5]), bf16x2_rne(x[6], x[7])};
+        v = __builtin_bit_cast(bf16x8, w);
+    }
+    SDP4_DEV float get(int j) const { return (float)v[j]; }
+};
+template <>
+struct Frag<float> {
+    float v[8];
+    SDP4_DEV void set(const float (&x)[8])
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = x[j];
+    }
+    SDP4_DEV float get(int j) const { return v[j]; }
+};
+
+SDP4_DEV void mma(const Frag<bf16_t> &a, const Frag<bf16_t> &b, f32x16 &c)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+SDP4_DEV void mma(const Frag<float> &a, const Frag<float> &b, f32x16 &c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+}
+
+// Eight elements of one row in global memory, from element e on; zeros from `dim` on.
+template <class T>
+SDP4_DEV void load_frag(const T *row, int e, int dim, Frag<T> &f)
+{
+    float x[8];
+    if (e + 8 <= dim) {
+        if constexpr (sizeof(T) == 2) {
+            f.v = __builtin_bit_cast(bf16x8, load_chunk<false>(row + e));
+            return;
+        } else {
+            const u32x4 a = load_chunk<false>(row + e), b = load_chunk<false>(row + e + 4);
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                x[j] = __uint_as_float(w[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            x[j] = e + j < dim ? to_f32<T>(row[e + j]) : 0.0f;
+    }
+    f.set(x);
+}
+
+// Heads of up to 32 * DB elements, as rows of LD elements in LDS.
+//
+// 16-byte chunk c of row r lies at chunk c ^ f(r), so that both kinds of reads spread over the banks: 16 lanes that read one
+// chunk of 16 neighbouring rows (f takes 16 values, or eight for the rows of one parity where two rows fill the banks), and
+// the transposing reads, where a group of 32 lanes takes four neighbouring chunks of four rows (f moves them apart by four).
+template <class T, int DB>
+struct HeadTile {
+    static constexpr int D = 32 * DB, LD = D <= 64 ? 64 : D <= 128 ? 128 : 256, N = kChunk<T>;
+    static constexpr int CHUNKS = LD / N, USED = D / N, ROW = LD * (int)sizeof(T), STEPS = 2 * DB;
+
+    SDP4_DEV static int twist(int r)
+    {
+        return CHUNKS == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3);
+    }
+    SDP4_DEV static int at(int r, int chunk) { return r * ROW + ((chunk ^ twist(r)) << 4); }
+
+    // Operand with rows r0 + l % 32, elements 16 s + ... along the sum.
+    SDP4_DEV static void rows(const char *tile, int r0, int s, Frag<T> &f)
+    {
+        const int l = lane_id(), r = l & 31, h = l >> 5;
+        const char *row = tile + r0 * ROW + r * ROW;
+        if constexpr (sizeof(T) == 2) {
+            f.v = *reinterpret_cast<const bf16x8 *>(row + (((2 * s + h) ^ twist(r)) << 4));
+        } else {
+            const u32x4 a = *reinterpret_cast<const u32x4 *>(row + (((4 * s + 2 * h) ^ twist(r)) << 4));
+            const u32x4 b = *reinterpret_cast<const u32x4 *>(row + (((4 * s + 2 * h + 1) ^ twist(r)) << 4));
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                f.v[j] = __uint_as_float(w[j]);
+        }
+    }
+
+    // Operand with the tile's elements 32 db + l % 32 as rows and its rows r0 + 8 a + 4 h + b along the sum.
+    SDP4_DEV static void columns(const char *tile, int r0, int db, Frag<T> &f)
+    {
+        const int l = lane_id(), h = l >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // a transposing read gives lane i of 16 element i of four rows, of which lane i points at a quarter of row i / 4
+            const int i = l & 15, row = 4 * h + (i >> 2), chunk = 4 * db + 2 * ((l >> 4) & 1) + ((i & 3) >> 1), half = 8 * (i & 1);
+            s16x8 w;
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const char *p = tile + r0 * ROW + (8 * a + row) * ROW + ((chunk ^ twist(8 * a + row)) << 4) + half;
+                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(p));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[4 * a + j] = v[j];
+            }
+            f.v = __builtin_bit_cast(bf16x8, w);
+        } else {
+            const int d = 32 * db + (l & 31);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int row = 8 * (j >> 2) + 4 * h + (j & 3);
+                f.v[j] = *reinterpret_cast<const float *>(tile + r0 * ROW + row * ROW + (((d >> 2) ^ twist(row)) << 4) + 4 * (d & 3));
+            }
+        }
+    }
+};
+
+// Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile, by THREADS threads.  Rows from `limit`
+// on and elements from `dim` (>= a chunk) on become zeros; other rows and elements are read in their place, so that all loads
+// are in flight together, and a head's last chunk, where it is not whole, as the head's last whole one, shifted.
+template <class T, int DB, int ROWS, int THREADS>
+struct TileLoad {
+    using H = HeadTile<T, DB>;
+    static constexpr int COUNT = ROWS * H::USED / THREADS;
+    static_assert(COUNT * THREADS == ROWS * H::USED, "whole rounds");
+    u32x4 v[COUNT];
+
+    SDP4_DEV void load(const T *head, int64_t stride, int first, int limit, int dim)
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int id = i * THREADS + (int)threadIdx.x, r = id / H::USED, e = (id - r * H::USED) * H::N;
+            const int row = first + r < limit ? first + r : limit - 1;
+            v[i] = load_chunk<false>(head + row * stride + (e + H::N <= dim ? e : dim - H::N));
+        }
+    }
+    SDP4_DEV void store(char *tile, int first, int limit, int dim) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int id = i * THREADS + (int)threadIdx.x, r = id / H::USED, e = (id - r * H::USED) * H::N;
+            u32x4 w = v[i];
+            if (dim % H::N)
+                w = e + H::N <= dim ? w : shifted(w, e + H::N - dim);
+            *reinterpret_cast<u32x4 *>(tile + H::at(r, e / H::N)) = first + r < limit && e < dim ? w : u32x4{0, 0, 0, 0};
+        }
+    }
+    SDP4_DEV static u32x4 shifted(u32x4 w, int by) // by elements toward the first, with zeros behind; by >= N is not used
+    {
+        const int bits = 8 * sizeof(T) * (by & (H::N - 1));
+        return __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, w) >> bits);
+    }
+};
+
+// A fragment whose masked places must not reach the product: what is infinite or NaN becomes 0 and is noted in `found`
+// (bit j: element j), since 0 times such a value would be NaN.
+SDP4_DEV uint32_t scrub(Frag<bf16_t> &f)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, f.v);
+    uint32_t found = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool lo = (w[j] & 0x7F80u) == 0x7F80u, hi = (w[j] & 0x7F800000u) == 0x7F800000u;
+        w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+        found |= (lo ? 1u << (2 * j) : 0u) | (hi ? 2u << (2 * j) : 0u);
+    }
+    f.v = __builtin_bit_cast(bf16x8, w);
+    return found;
+}
+SDP4_DEV uint32_t scrub(Frag<float> &f)
+{
+    uint32_t found = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const bool bad = (__float_as_uint(f.v[j]) & 0x7F800000u) == 0x7F800000u;
+        f.v[j] = bad ? 0.0f : f.v[j];
+        found |= bad ? 1u << j : 0u;
+    }
+    return found;
+}
+// The tile rows (bits) of the elements that scrub found in the fragment at r0 of a tile of up to 64 rows.
+SDP4_DEV uint64_t tile_rows(uint32_t found, int r0)
+{
+    const int h = lane_id() >> 5;
+    const uint64_t bits = (found & 0xFu) | (found & 0xF0u) << 4; // places 4 a + b -> rows 8 a + b
+    return bits << (r0 + 4 * h);
+}
+SDP4_DEV uint64_t or_wave(uint64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t lo = __shfl_xor((uint32_t)v, d), hi = __shfl_xor((uint32_t)(v >> 32), d);
+        v |= (uint64_t)hi << 32 | lo;
+    }
+    return v;
+}
+
+// The sequence of a row: `samples` (LDS, kSeqSamples numbers, filled by fill_samples) narrow the search to a few offsets.
+constexpr int kSeqSamples = 256;
+SDP4_DEV int64_t sample_step(const Sequences &s) { return (s.count + kSeqSamples) / kSeqSamples; } // of count + 1 offsets
+template <int THREADS>
+SDP4_DEV void fill_samples(const Sequences &s, int64_t *samples)
+{
+    if (!s.offsets)
+        return;
+    const int64_t step = sample_step(s);
+    for (int i = threadIdx.x; i < kSeqSamples; i += THREADS)
+        samples[i] = i * step <= s.count ? s.offsets[i * step] : INT64_MAX;
+    __syncthreads();
+}
+struct Span {
+    int first, end; // rows of the sequence
+    bool on;        // false: the row is in none
+};
+// Whatever the offsets hold, 0 <= first <= row < end <= tokens.
+SDP4_DEV Span span_of(const Sequences &s, const int64_t *samples, int row)
+{
+    Span r{0, s.tokens, row < s.tokens};
+    if (!s.offsets || !r.on)
+        return r;
+    int lo = 0, hi = kSeqSamples; // the last sample <= row lies in [lo, hi), if there is one
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (samples[mid] <= row)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    if (samples[0] > row) {
+        r.on = false;
+        return r;
+    }
+    const int64_t step = sample_step(s);
+    int64_t a = lo * step, b = a + step < s.count + 1 ? a + step : s.count + 1;
+    while (b - a > 1) {
+        const int64_t mid = (a + b) / 2;
+        if (s.offsets[mid] <= row)
+            a = mid;
+        else
+            b = mid;
+    }
+    if (a >= s.count) {
+        r.on = false;
+        return r;
+    }
+    const int64_t first = s.offsets[a], end = s.offsets[a + 1];
+    r.first = first < 0 ? 0 : first > row ? row : (int)first;
+    r.end = end <= row ? row + 1 : end > s.tokens ? s.tokens : (int)end;
+    return r;
+}
+
+// Smallest and largest value over a wave, on the scalar unit.
+SDP4_DEV int min_wave(int v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_xor(v, d);
+        v = o < v ? o : v;
+    }
+    return (int)uniform((uint32_t)v);
+}
+SDP4_DEV int max_wave(int v) { return -min_wave(-v); }
+
+// Work items in eight shares, one for each XCD: blocks are dealt to the XCDs in turn, so the blocks of one share, which read the
+// same keys and values, meet in one L2.
+SDP4_DEV int64_t shared_item(int64_t block, int64_t items)
+{
+    const int64_t each = (items + 7) / 8;
+    return (block & 7) * each + (block >> 3);
+}
+inline int64_t shared_blocks(int64_t items) { return 8 * ((items + 7) / 8); }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// From here on (octaves) a reference is subtracted from the scores before their product with c = scale log2(e), whose rounding
+// would otherwise move exponents by more than the 2^-12 that it is here: as much as the rounding of such a score itself.
+constexpr float kLargeScore = 4096.0f;
+
+SDP4_DEV float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+} // namespace sdp4

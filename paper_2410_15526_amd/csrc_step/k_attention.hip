@@ -1,0 +1,235 @@
+// k_attention.hip -- causal attention over packed sequences.
+//
+// Row i of a sequence that begins at row b sees keys b .. i of it:
+//      s_ij = scale q_i . k_j,  lse_i = log sum_j exp(s_ij),
+//      out_i = sum_j exp(s_ij - lse_i) v_j,
+// in one pass over the keys with a running reference of the maximum and a
+// running sum.  A block takes rows of the batch as they lie, whatever
+// sequences they belong to, and masks what lies outside a row's own: many
+// short sequences share a block.
+#include "attention.hpp"
+
+namespace sdp4 {
+
+namespace {
+
+// WAVES waves of 32 rows each, BN keys at a time, STAGES tiles in LDS.
+template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
+__global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Heads qh, Heads kh, Heads vh, Heads oh, float *lse,
+                                                             int tiles, int64_t items)
+{
+    using H = HeadTile<T, DB>;
+    constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
+    __shared__ __align__(16) char kt[STAGES][BN * H::ROW];
+    __shared__ __align__(16) char vt[STAGES][BN * H::ROW];
+    __shared__ int64_t samples[kSeqSamples];
+    __shared__ int edges[WAVES][2];
+
+    const int64_t item = shared_item(work_block(), items);
+    if (item >= items)
+        return;
+    const int64_t per_head = (int64_t)tiles * at.group;
+    const int kv = (int)(item / per_head);
+    const int64_t rest = item - kv * per_head;
+    const int tile = tiles - 1 - (int)(rest / at.group), head = kv * at.group + (int)(rest % at.group);
+
+    const int wave = uniform(threadIdx.x / kWave), lane = lane_id(), h = lane >> 5;
+    const int q0 = tile * BM + 32 * wave, row = q0 + (lane & 31);
+    fill_samples<THREADS>(at.seq, samples);
+    const Span span = span_of(at.seq, samples, row);
+    const int start = span.on ? span.first : INT_MAX;
+    const int w_first = min_wave(start), w_last = max_wave(span.on ? row : -1); // keys that the wave's rows see
+    const int w_full = max_wave(start);                                        // from here to q0 all of them see all
+    if (lane == 0)
+        edges[wave][0] = w_first, edges[wave][1] = w_last;
+    __syncthreads();
+    int first = INT_MAX, last = -1;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        first = edges[w][0] < first ? edges[w][0] : first;
+        last = edges[w][1] > last ? edges[w][1] : last;
+    }
+    if (last < 0) // no row of the block is in a sequence
+        return;
+
+    const T *qrow = static_cast<const T *>(qh.p) + (int64_t)(row < at.seq.tokens ? row : at.seq.tokens - 1) * qh.token_stride +
+                    head * qh.head_stride;
+    Frag<T> q[H::STEPS];
+#pragma unroll
+    for (int s = 0; s < H::STEPS; ++s)
+        load_frag(qrow, 16 * s + 8 * h, at.dim, q[s]);
+    const T *kp = static_cast<const T *>(kh.p) + kv * kh.head_stride, *vp = static_cast<const T *>(vh.p) + kv * vh.head_stride;
+
+    const float c = at.scale * kLog2e;
+    float m = -__builtin_inff(), total = 0.0f; // reference (a score) and the lane's share of the sum
+    bool poison = false;
+    f32x16 o[DB] = {};
+
+    TileLoad<T, DB, BN, THREADS> kl, vl;
+    kl.load(kp, kh.token_stride, first, last + 1, at.dim);
+    vl.load(vp, vh.token_stride, first, last + 1, at.dim);
+    int stage = 0;
+    for (int k0 = first; k0 <= last; k0 += BN) {
+        if (STAGES == 1 && k0 != first)
+            __syncthreads();
+        kl.store(kt[stage], k0, last + 1, at.dim);
+        vl.store(vt[stage], k0, last + 1, at.dim);
+        __syncthreads();
+        if (k0 + BN <= last) {
+            kl.load(kp, kh.token_stride, k0 + BN, last + 1, at.dim);
+            vl.load(vp, vh.token_stride, k0 + BN, last + 1, at.dim);
+        }
+        const char *kb = kt[stage], *vb = vt[stage];
+        if (STAGES == 2)
+            stage ^= 1;
+        if (k0 > w_last || k0 + BN <= w_first)
+            continue;
+        const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
+
+        f32x16 x[RB] = {};
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int s = 0; s < H::STEPS; ++s) {
+                Frag<T> a;
+                H::rows(kb, 32 * rb, s, a);
+                mma(a, q[s], x[rb]);
+            }
+        if (masked) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
+                    x[rb][r] = key >= start && key <= row ? x[rb][r] : -__builtin_inff();
+                }
+        }
+        float mx = x[0][0];
+#pragma unroll
+        for (int i = 1; i < 16 * RB; ++i)
+            mx = fmaxf(mx, x[i / 16][i % 16]);
+        mx = fmaxf(mx, xor_lane<32>(mx));
+        // The reference is the largest score so far, so that a key which takes a row alone has p = 1, without a rounding.  Tiles
+        // that raise none of the wave's rows leave the results as they are.
+        const bool up = mx > m;
+        if (__any(up)) {
+            const float to = up ? mx : m;
+            const float from = m * c, ref = to * c; // as the exponents below take them
+            const bool large = __builtin_fabsf(from) >= kLargeScore || __builtin_fabsf(ref) >= kLargeScore;
+            const float by = up ? exp2_of(large ? (m - to) * c : from - ref) : 1.0f;
+            m = to;
+            total *= by;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    o[db][r] *= by;
+        }
+        float ref = m == -__builtin_inff() ? 0.0f : m * c;
+        const bool large = __builtin_fabsf(ref) >= kLargeScore;
+        if (__any(large)) { // a product's rounding would move its exponent: subtract first
+#pragma unroll
+            for (int i = 0; i < 16 * RB; ++i)
+                x[i / 16][i % 16] -= large ? m : 0.0f;
+            ref = large ? 0.0f : ref;
+        }
+#pragma unroll
+        for (int i = 0; i < 16 * RB; ++i) {
+            const float p = exp2_of(__builtin_fmaf(x[i / 16][i % 16], c, -ref));
+            x[i / 16][i % 16] = p;
+            total += p;
+        }
+        Frag<T> p[2 * RB]; // bfloat16: the one rounding on the way to the second product
+#pragma unroll
+        for (int s = 0; s < 2 * RB; ++s) {
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                w[j] = x[s / 2][8 * (s % 2) + j];
+            p[s].set(w);
+        }
+        if (!masked) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int s = 0; s < 2 * RB; ++s) {
+                    Frag<T> a;
+                    H::columns(vb, 16 * s, db, a);
+                    mma(a, p[s], o[db]);
+                }
+        } else {
+            uint64_t found = 0;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int s = 0; s < 2 * RB; ++s) {
+                    Frag<T> a;
+                    H::columns(vb, 16 * s, db, a);
+                    found |= tile_rows(scrub(a), 16 * s);
+                    mma(a, p[s], o[db]);
+                }
+            if (__any(found != 0)) {
+                found = or_wave(found);
+                for (int j = 0; j < BN; ++j)
+                    poison |= (found >> j & 1) && k0 + j >= start && k0 + j <= row;
+            }
+        }
+    }
+
+    total += xor_lane<32>(total);
+    if (!span.on)
+        return;
+    // a row whose scores are all -inf: zeros
+    const float inv = poison ? __builtin_nanf("") : total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    T *orow = static_cast<T *>(oh.p) + (int64_t)row * oh.token_stride + head * oh.head_stride;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int d = 32 * db + 8 * a + 4 * h;
+            float w[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                w[b] = o[db][4 * a + b] * inv;
+            store_elems(orow + d, (int64_t)at.dim - d, w);
+        }
+    if (lse && h == 0) // a small reference was taken as the rounded product
+        lse[(int64_t)head * at.seq.tokens + row] =
+            total > 0.0f ? (__builtin_fabsf(m * c) < kLargeScore ? (m * c + __log2f(total)) * kLn2 : m * at.scale + __logf(total))
+            : total == 0.0f ? -__builtin_inff() : total;
+}
+
+template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
+int run(const Attention &at, const Heads &q, const Heads &k, const Heads &v, const Heads &out, float *lse, hipStream_t s)
+{
+    const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
+    const int64_t items = (int64_t)tiles * q.heads;
+    return launch<WAVES>(k_attention<T, DB, WAVES, BN, STAGES, OCC>, shared_blocks(items), kUncapped, s, at, q, k, v, out, lse,
+                         tiles, items);
+}
+
+} // namespace
+
+int launch_attention(int dtype, const Attention &at, const Heads &q, const Heads &k, const Heads &v, const Heads &out,
+                     float *lse, hipStream_t s)
+{
+    const int db = (at.dim + 31) / 32;
+    if (dtype == SDP4_BF16) {
+        if (db <= 2)
+            return run<bf16_t, 2, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
+        if (db == 3)
+            return run<bf16_t, 3, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
+        if (db == 4)
+            return run<bf16_t, 4, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
+        return run<bf16_t, 8, 4, 32, 2, 1>(at, q, k, v, out, lse, s);
+    }
+    if (db <= 2)
+        return run<float, 2, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
+    if (db == 3)
+        return run<float, 3, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
+    if (db == 4)
+        return run<float, 4, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
+    return run<float, 8, 4, 32, 2, 1>(at, q, k, v, out, lse, s);
+}
+
+} // namespace sdp4

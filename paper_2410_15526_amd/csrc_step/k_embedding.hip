@@ -1,0 +1,347 @@
+// k_embedding.hip -- rows of a table by token, and the table's gradient.
+//
+// The gradient of a table row is the sum of the rows of dy whose token it is.
+// To take it in one order whatever the timing, the rows are sorted by token:
+//  1. tiles of kTile rows, each row's place in its tile counted against the
+//     whole tile (a comparison a pair: no exchange between lanes, no passes);
+//  2. with more than one tile, each row's place among all by binary searches
+//     in the other tiles;
+//  3. where each token's rows begin, by binary search, and the sums of runs of
+//     kRun sorted rows of one token;
+//  4. the table, every row written once: zeros, or the sum of its rows, whole
+//     runs of them from step 3.
+// The rest is HBM's: dy is read once, the table written once.
+#include "step_device.hpp"
+
+#include <limits.h>
+
+namespace sdp4 {
+
+namespace {
+
+template <class X, class Y>
+constexpr int kEmbed = sizeof(X) == 4 || sizeof(Y) == 4 ? 4 : 8; // elements of a lane in one access
+
+// A wave for 64 accesses of a row.
+template <class X, class Y>
+__global__ __launch_bounds__(256) void k_embedding(Tokens t, int64_t cols, float scale, Divisor per_row, int64_t waves,
+                                                   Rows<const X *> table, Rows<Y *> y)
+{
+    constexpr int N = kEmbed<X, Y>;
+    const int64_t w = work_block() * 4 + uniform(threadIdx.x / kWave);
+    if (w >= waves)
+        return;
+    uint64_t part;
+    const int64_t row = (int64_t)divide((uint64_t)w, per_row, part);
+    const int64_t c = N * ((int64_t)part * kWave + lane_id());
+    const int64_t token = (int64_t)uniform((uint64_t)t.p[row]);
+    float v[N];
+    if (token >= 0 && token < t.vocab) {
+        load_row(table.p + token * table.stride, c, cols, v);
+        end_row(c, cols, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] *= scale;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] = token < 0 ? 0.0f : __builtin_nanf("");
+    }
+    store_elems(y.p + row * y.stride + c, cols - c, v);
+}
+
+// ---------------------------------------------------------------------------
+// sorting
+// ---------------------------------------------------------------------------
+constexpr int kTileLog2 = 13, kTile = 1 << kTileLog2, kRun = 64;
+constexpr int kSortRows = 32, kSortThreads = 512, kShares = kSortThreads / kSortRows; // rows of a block; threads of a row
+
+// Tokens without a row of the table sort behind all others.
+SDP4_DEV uint32_t key_of(const Tokens &t, int64_t row)
+{
+    if (row >= t.rows)
+        return ~0u;
+    const int64_t v = t.p[row];
+    return v < 0 || v >= t.vocab ? (uint32_t)t.vocab : (uint32_t)v;
+}
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_tiles(Tokens t, int tile_log2, uint32_t *keys, uint32_t *order)
+{
+    __shared__ __align__(16) uint32_t all[kTile];
+    __shared__ int below[kShares][kSortRows];
+    const int64_t first = work_block() * kSortRows, base = first >> tile_log2 << tile_log2;
+    if (first >= t.rows)
+        return;
+    const int size = 1 << tile_log2;
+    for (int i = threadIdx.x; i < size; i += kSortThreads)
+        all[i] = key_of(t, base + i);
+    __syncthreads();
+    const int mine = (int)(first - base), share = threadIdx.x / kSortRows, r = threadIdx.x % kSortRows;
+    const uint32_t key = all[mine + r];
+    // earlier rows come first where tokens are equal
+    const int each = size / kShares, a = share * each, b = a + each;
+    int count = 0;
+    const int before = b < mine ? b : mine, after = a > mine + kSortRows ? a : mine + kSortRows;
+    for (int j = a; j < before; j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(all + j);
+        count += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+    }
+    for (int j = after; j < b; j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(all + j);
+        count += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    }
+    for (int j = a > mine ? a : mine; j < (b < mine + kSortRows ? b : mine + kSortRows); ++j)
+        count += all[j] < key || (all[j] == key && j < mine + r);
+    below[share][r] = count;
+    __syncthreads();
+    if (threadIdx.x < kSortRows && first + r < t.rows) {
+        int place = 0;
+#pragma unroll
+        for (int i = 0; i < kShares; ++i)
+            place += below[i][r];
+        keys[base + place] = key, order[base + place] = (uint32_t)(first + r);
+    }
+}
+
+// Numbers below `key` (or up to it) among n sorted ones.
+template <bool EQUAL>
+SDP4_DEV int64_t count_below(const uint32_t *keys, int64_t n, uint32_t key)
+{
+    int64_t a = 0;
+    while (n > 0) {
+        const int64_t half = n / 2;
+        const uint32_t k = keys[a + half];
+        if (EQUAL ? k <= key : k < key)
+            a += half + 1, n -= half + 1;
+        else
+            n = half;
+    }
+    return a;
+}
+
+__global__ __launch_bounds__(256) void k_merge_tiles(int64_t rows, const uint32_t *keys, const uint32_t *order, uint32_t *to_keys,
+                                                     uint32_t *to_order)
+{
+    const int64_t i = work_block() * 256 + threadIdx.x;
+    if (i >= rows)
+        return;
+    const uint32_t key = keys[i];
+    const int64_t mine = i >> kTileLog2;
+    int64_t place = i - (mine << kTileLog2);
+    for (int64_t tile = 0, at = 0; at < rows; ++tile, at += kTile) {
+        const int64_t n = rows - at < kTile ? rows - at : kTile;
+        if (tile < mine)
+            place += count_below<true>(keys + at, n, key);
+        else if (tile > mine)
+            place += count_below<false>(keys + at, n, key);
+    }
+    to_keys[place] = key, to_order[place] = order[i];
+}
+
+// ---------------------------------------------------------------------------
+// sums
+// ---------------------------------------------------------------------------
+// Adds rows order[a .. b) of dy (scaled) to v, in order: a wave, the same rows in all lanes, eight loads under way.
+template <class X, int N>
+SDP4_DEV void add_rows(const Rows<const X *> &dy, const uint32_t *order, int64_t a, int64_t b, int64_t c, int64_t cols, float (&v)[N])
+{
+    constexpr int U = 8;
+    for (int64_t i = a; i < b; i += U) {
+        Raw<X, N> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t row = uniform(order[i + u < b ? i + u : b - 1]);
+            load_row(dy.p + (int64_t)row * dy.stride, c, cols, r[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float w[N];
+            r[u].get(w);
+            end_row(c, cols, w);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[j] += i + u < b ? w[j] : 0.0f;
+        }
+    }
+}
+
+template <int N>
+SDP4_DEV void load_sums(const float *p, float (&v)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        float w[4];
+        load_whole(p + j, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[j + i] = w[i];
+    }
+}
+
+// The first `token_blocks` blocks: where each token's rows begin.  The others: sums of whole runs, a wave for 64 accesses.
+template <class X, int N>
+__global__ __launch_bounds__(256) void k_runs(Tokens t, int64_t cols, Rows<const X *> dy, const uint32_t *keys, const uint32_t *order,
+                                              int64_t token_blocks, uint32_t *starts, int64_t col_parts, int64_t pitch, float *runs)
+{
+    const int64_t block = work_block();
+    if (block < token_blocks) {
+        const int64_t v = block * 256 + threadIdx.x;
+        if (v <= t.vocab)
+            starts[v] = (uint32_t)count_below<false>(keys, t.rows, (uint32_t)v);
+        return;
+    }
+    const int64_t w = (block - token_blocks) * 4 + uniform(threadIdx.x / kWave), run = w / col_parts, part = w - run * col_parts;
+    const int64_t a = run * kRun;
+    if (a + kRun > t.rows || keys[a] != keys[a + kRun - 1] || keys[a] >= (uint32_t)t.vocab)
+        return;
+    const int64_t c = N * (part * kWave + lane_id());
+    float v[N] = {};
+    add_rows(dy, order, a, a + kRun, c < cols ? c : 0, cols, v);
+    if (c < cols) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            runs[run * pitch + c + j] = v[j];
+    }
+}
+
+// A wave for 64 accesses of a table row, or (ADD) of the row of a sorted position where its token's rows begin.
+template <class X, class Y, bool ADD>
+__global__ __launch_bounds__(256) void k_table(Tokens t, int64_t cols, float scale, Rows<const X *> dy, const uint32_t *keys,
+                                               const uint32_t *order, const uint32_t *starts, int64_t pitch, const float *runs,
+                                               Divisor per_row, int64_t waves, Rows<Y *> table)
+{
+    constexpr int N = kEmbed<X, Y>;
+    const int64_t w = work_block() * 4 + uniform(threadIdx.x / kWave);
+    if (w >= waves)
+        return;
+    uint64_t part;
+    int64_t token = (int64_t)divide((uint64_t)w, per_row, part);
+    int64_t a, b;
+    if constexpr (ADD) {
+        a = token;
+        const uint32_t k = uniform(keys[a]);
+        if (k >= (uint32_t)t.vocab || (a > 0 && uniform(keys[a - 1]) == k))
+            return;
+        token = k, b = uniform(starts[token + 1]);
+    } else {
+        a = uniform(starts[token]), b = uniform(starts[token + 1]);
+    }
+    const int64_t place = N * ((int64_t)part * kWave + lane_id()), c = place < cols ? place : 0;
+    float v[N] = {};
+    const int64_t whole = (a + kRun - 1) / kRun, behind = b / kRun; // whole runs of the token's rows
+    if (behind <= whole) {
+        add_rows(dy, order, a, b, c, cols, v);
+    } else {
+        add_rows(dy, order, a, whole * kRun, c, cols, v);
+        for (int64_t i = whole; i < behind; i += 8) {
+            float r[8][N];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                load_sums(runs + (i + u < behind ? i + u : behind - 1) * pitch + c, r[u]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    v[j] += i + u < behind ? r[u][j] : 0.0f;
+        }
+        add_rows(dy, order, behind * kRun, b, c, cols, v);
+    }
+    Y *row = table.p + token * table.stride;
+    if constexpr (ADD) {
+        float before[N];
+        load_row(row, c, cols, before);
+        end_row(c, cols, before);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] = __builtin_fmaf(v[j], scale, before[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            v[j] *= scale;
+    }
+    store_elems(row + place, cols - place, v);
+}
+
+// The workspace: sorted tokens and rows, the same before the tiles are merged, starts, sums of runs.
+struct Layout {
+    int64_t keys, order, tile_keys, tile_order, starts, runs, bytes, pitch;
+    Layout(int64_t rows, int64_t vocab, int64_t cols)
+    {
+        int64_t at = 0;
+        auto take = [&](int64_t n) {
+            const int64_t here = at;
+            at += (4 * n + 15) / 16 * 16;
+            return here;
+        };
+        const bool merged = rows > kTile;
+        pitch = (cols + 7) / 8 * 8;
+        keys = take(rows), order = take(rows);
+        tile_keys = take(merged ? rows : 0), tile_order = take(merged ? rows : 0);
+        starts = take(vocab + 1);
+        runs = take(rows / kRun * pitch);
+        bytes = at;
+    }
+};
+
+} // namespace
+
+int launch_embedding(const Tokens &t, int64_t cols, float scale, int in, Rows<const void *> table, int out, Rows<void *> y,
+                     hipStream_t s)
+{
+    return with_type(in, [&](auto in_tag) {
+        return with_type(out, [&](auto out_tag) {
+            using X = decltype(in_tag);
+            using Y = decltype(out_tag);
+            constexpr int64_t width = kEmbed<X, Y> * kWave;
+            const int64_t per_row = (cols + width - 1) / width, waves = t.rows * per_row;
+            return launch<4>(k_embedding<X, Y>, (waves + 3) / 4, kUncapped, s, t, cols, scale, Divisor((uint64_t)per_row), waves,
+                             typed<const X>(table), typed<Y>(y));
+        });
+    });
+}
+
+int64_t embedding_grad_workspace(int64_t rows, int64_t vocab, int64_t cols) { return Layout(rows, vocab, cols).bytes; }
+
+int launch_embedding_grad(const Tokens &t, int64_t cols, float scale, bool accumulate, int in, Rows<const void *> dy, int out,
+                          Rows<void *> dtable, void *workspace, hipStream_t s)
+{
+    const Layout l(t.rows, t.vocab, cols);
+    char *base = static_cast<char *>(workspace);
+    auto at = [&](int64_t offset) { return reinterpret_cast<uint32_t *>(base + offset); };
+    const bool merged = t.rows > kTile;
+    int tile_log2 = kTileLog2;
+    while (tile_log2 > 6 && (1 << (tile_log2 - 1)) >= t.rows) // one tile: only as large as the rows take
+        --tile_log2;
+    int rc = 0;
+    if (t.rows > 0) {
+        rc = launch<kSortThreads / kWave>(k_sort_tiles, (t.rows + kSortRows - 1) / kSortRows, kUncapped, s, t, tile_log2,
+                                          at(merged ? l.tile_keys : l.keys), at(merged ? l.tile_order : l.order));
+        if (!rc && merged)
+            rc = launch<4>(k_merge_tiles, (t.rows + 255) / 256, kUncapped, s, t.rows, at(l.tile_keys), at(l.tile_order), at(l.keys),
+                           at(l.order));
+    }
+    if (rc)
+        return rc;
+    return with_type(in, [&](auto in_tag) {
+        return with_type(out, [&](auto out_tag) {
+            using X = decltype(in_tag);
+            using Y = decltype(out_tag);
+            constexpr int N = kEmbed<X, Y>;
+            const int64_t per_row = (cols + N * kWave - 1) / (N * kWave), token_blocks = (t.vocab + 256) / 256;
+            const int64_t run_waves = t.rows / kRun * per_row;
+            float *runs = reinterpret_cast<float *>(base + l.runs);
+            int rc = launch<4>(k_runs<X, N>, token_blocks + (run_waves + 3) / 4, kUncapped, s, t, cols, typed<const X>(dy), at(l.keys),
+                               at(l.order), token_blocks, at(l.starts), per_row, l.pitch, runs);
+            if (rc)
+                return rc;
+            const int64_t waves = (accumulate ? t.rows : t.vocab) * per_row;
+            if (waves == 0)
+                return 0;
+            auto k = accumulate ? k_table<X, Y, true> : k_table<X, Y, false>;
+            return launch<4>(k, (waves + 3) / 4, kUncapped, s, t, cols, scale, typed<const X>(dy), at(l.keys), at(l.order),
+                             at(l.starts), l.pitch, runs, Divisor((uint64_t)per_row), waves, typed<Y>(dtable));
+        });
+    });
+}
+
+} // namespace sdp4

@@ -1,6 +1,7 @@
-// step.hpp -- interface between the C ABI layer (abi_step.cpp) and the
-// launchers of the training-step operators (k_dropout.hip, k_logprob.hip,
-// k_qk.hip).  Launchers assume validated arguments.
+// step.hpp -- interface between the C ABI layer (abi_step.cpp, abi_layer.cpp)
+// and the launchers of the training-step operators (k_dropout.hip,
+// k_logprob.hip, k_qk.hip, k_attention.hip, k_attention_grad.hip,
+// k_block_norm.hip, k_embedding.hip).  Launchers assume validated arguments.
 #pragma once
 
 #include "launch.hpp"
@@ -78,6 +79,63 @@ int launch_qk_grad(int dtype, const Heads (&dy)[2], const Heads (&x)[2], const H
 int64_t qk_grad_workspace(int64_t tokens, int q_heads, int k_heads, int dim);
 int launch_rope_table(const double *inv_freq, int half, int64_t start, int64_t rows, double scale, float *table,
                       hipStream_t s);
+
+// Packed sequences: sequence i has rows offsets[i] .. offsets[i + 1] - 1.
+struct Sequences {
+    const int64_t *offsets; // null: one sequence of all rows
+    int64_t count;
+    int tokens;
+};
+struct Attention {
+    Sequences seq;
+    int dim, group; // elements of a head; query heads that share a key and value head
+    float scale;
+};
+int launch_attention(int dtype, const Attention &a, const Heads &q, const Heads &k, const Heads &v, const Heads &out,
+                     float *lse, hipStream_t s);
+int launch_attention_grad(int dtype, const Attention &a, const Heads &dout, const Heads &q, const Heads &k, const Heads &v,
+                          const Heads &out, const float *lse, const Heads &dq, const Heads &dk, const Heads &dv,
+                          float *workspace, hipStream_t s);
+int64_t attention_grad_workspace(int64_t tokens, int q_heads, int k_heads, int dim);
+
+// The joint of two blocks; arrays of the branch's element type, the residual stream's, weights of the branch's.
+struct BlockNorm {
+    bool post_norm;
+    float post_eps, pre_eps;
+    const void *post_weight, *pre_weight; // null: ones
+    const float *gate;                    // of a row; null: ones
+    float branch_scale, residual_scale;
+};
+int launch_block_norm(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows, int64_t cols, Rows<const void *> branch,
+                      Rows<const void *> residual, Rows<void *> y, Rows<void *> h, hipStream_t s);
+struct BlockNormArrays {
+    Rows<const void *> dh, dy, branch, y;
+    Rows<void *> dbranch, dresidual;
+    float *dpost_weight, *dpre_weight, *dgate;
+};
+template <class X, class Y>
+struct BlockNormGrad {
+    Rows<const X *> dh;
+    Rows<const Y *> dy;
+    Rows<const X *> branch;
+    Rows<const Y *> y;
+    Rows<X *> dbranch;
+    Rows<Y *> dres;
+    float *dgate, *post_parts, *pre_parts;
+};
+int launch_block_norm_grad(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows, int64_t cols, const BlockNormArrays &a,
+                           float *workspace, hipStream_t s);
+int64_t block_norm_grad_workspace(int64_t rows, int64_t cols);
+
+struct Tokens {
+    const int64_t *p;
+    int64_t rows, vocab;
+};
+int launch_embedding(const Tokens &t, int64_t cols, float scale, int in, Rows<const void *> table, int out, Rows<void *> y,
+                     hipStream_t s);
+int launch_embedding_grad(const Tokens &t, int64_t cols, float scale, bool accumulate, int in, Rows<const void *> dy, int out,
+                          Rows<void *> dtable, void *workspace, hipStream_t s);
+int64_t embedding_grad_workspace(int64_t rows, int64_t vocab, int64_t cols);
 
 // out[c] = the sum of p[i * pitch + c] over i < count, for c < cols, in a fixed order; one or two such sums (out null: none).
 struct Parts {

@@ -2,9 +2,10 @@
 through the compression path: ``python -m paper_2410_15526_amd.decoder``.
 
 One worker's share of a sharded data-parallel step, end to end: the forward
-and backward pass run norm and rotation of queries and keys, bias + dropout
-+ residual, and the loss with its gradient through the library, with torch's
-matrix products between them; the gradients then take the two-level path of
+and backward pass run the embedding, the norms of the blocks, norm and
+rotation of queries and keys, attention, bias + dropout + residual, and the
+loss with its gradient through the library, with torch's matrix products
+between them; the gradients then take the two-level path of
 :class:`~paper_2410_15526_amd.pipeline.HotPath` (one peer at each level, so
 what comes out is the worker's own gradient after both quantizations), the
 optimizer updates the float32 main weights, and the bfloat16 model weights
@@ -31,6 +32,7 @@ class Config:
     seq: int = 64
     batch: int = 16
     dropout: float = 0.1
+    post_norm: bool = False  # a weighted norm behind each block, too
     lr: float = 3e-3
     group: int = 128
     hadamard_block: int = 128
@@ -47,6 +49,8 @@ class Decoder:
         for i in range(cfg.layers):
             shapes += [(f"{i}.qkv", (3 * h, h)), (f"{i}.q_norm", (d,)), (f"{i}.k_norm", (d,)), (f"{i}.out", (h, h)),
                        (f"{i}.out_bias", (h,)), (f"{i}.up", (4 * h, h)), (f"{i}.down", (h, 4 * h)), (f"{i}.down_bias", (h,))]
+            if cfg.post_norm:
+                shapes += [(f"{i}.attention_norm", (h,)), (f"{i}.mlp_norm", (h,))]
         count = sum(torch.Size(s).numel() for _, s in shapes)
         n = -(-count // cfg.group) * cfg.group
         self.path = HotPath(n, cfg.group, cfg.hadamard_block, 1, 1, cfg.group, "bf16")
@@ -68,30 +72,36 @@ class Decoder:
         self.path.w_prev.copy_(self.path.w_new)
         self.moments = [torch.zeros(n, device="cuda") for _ in range(2)]
         self.table = autograd.rope_table(cfg.seq, d)
+        # what attention adds to the scores of one sequence, for forms of the model that spell it out
         self.mask = torch.full((cfg.seq, cfg.seq), float("-inf"), device="cuda").triu(1)
 
     def logits(self, tokens, weights, step: int, p: float):
         """Logits [batch * seq, width] of tokens [batch, seq]."""
         c = self.cfg
         rows, d = tokens.numel(), c.hidden // c.heads
-        norm = lambda v: v * torch.rsqrt((v.float() ** 2).mean(1, keepdim=True) + 1e-6).to(v.dtype)  # noqa: E731
         positions = torch.arange(c.seq, device="cuda").repeat(tokens.shape[0])
-        x = weights["embed"][tokens.reshape(-1)]
+        sequences = torch.arange(0, rows + 1, c.seq, device="cuda")
+        x = autograd.embedding(tokens.reshape(-1), weights["embed"])
+        h = autograd.block_norm(None, x)[1]
         for i in range(c.layers):
             w = {k[len(f"{i}."):]: v for k, v in weights.items() if k.startswith(f"{i}.")}
             # masks of this step, layer and place: a range of element numbers each
             offset = [(((step * c.layers + i) * 2 + j) * rows * c.hidden) for j in range(2)]
-            qkv = (norm(x) @ w["qkv"].t()).view(rows, 3 * c.heads, d)
+            qkv = (h @ w["qkv"].t()).view(rows, 3 * c.heads, d)
             q, k = autograd.qk_norm_rope(qkv[:, :c.heads], qkv[:, c.heads:2 * c.heads], w["q_norm"], w["k_norm"], 1e-6,
                                          self.table, positions)
-            q, k, v = (t.reshape(-1, c.seq, c.heads, d).transpose(1, 2).float().contiguous()
-                       for t in (q, k, qkv[:, 2 * c.heads:]))
-            a = torch.softmax(q @ k.transpose(2, 3).contiguous() * d ** -0.5 + self.mask, -1) @ v
-            a = a.transpose(1, 2).reshape(rows, c.hidden).to(x.dtype)
-            x = autograd.dropout_add(a @ w["out"].t(), w["out_bias"], x, p, self.seed, offset[0])
-            u = torch.nn.functional.gelu(norm(x) @ w["up"].t())
-            x = autograd.dropout_add(u @ w["down"].t(), w["down_bias"], x, p, self.seed, offset[1])
-        return norm(x) @ weights["embed"].t()
+            a = autograd.attention(q, k, qkv[:, 2 * c.heads:], sequences).view(rows, c.hidden)
+            x, h = self.join(a @ w["out"].t(), w["out_bias"], w.get("attention_norm"), x, p, offset[0])
+            u = torch.nn.functional.gelu(h @ w["up"].t())
+            x, h = self.join(u @ w["down"].t(), w["down_bias"], w.get("mlp_norm"), x, p, offset[1])
+        return h @ weights["embed"].t()
+
+    def join(self, branch, bias, post_weight, x, p: float, offset: int):
+        """The residual stream behind a block, and the next block's input."""
+        if post_weight is None:
+            return autograd.block_norm(None, autograd.dropout_add(branch, bias, x, p, self.seed, offset))
+        branch = autograd.dropout_add(branch, bias, None, p, self.seed, offset)
+        return autograd.block_norm(branch, x, post_weight=post_weight, post_eps=1e-6)
 
     def backward(self, tokens, targets, p: float | None = None):
         """Mean loss over the targets (negative: none); fills ``grads``."""

@@ -29,6 +29,7 @@ OK, EINVAL, EALIGN, ERANGE, EHIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
 MIN_GROUP, MAX_GROUP, MAX_HADAMARD, MAX_PEERS = 32, 4096, 1024, 16
 MAX_TOP, MAX_VOCAB, MAX_HEAD_DIM = 32, 1 << 20, 512
+MIN_ATTENTION_DIM, MAX_ATTENTION_DIM, MAX_TOKENS, MAX_HIDDEN = 8, 256, 1 << 30, 16384
 
 
 class Sdp4Error(RuntimeError):
@@ -50,6 +51,19 @@ class QkParams(C.Structure):
     _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("norm", C.c_int), ("eps", C.c_float),
                 ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("table_rows", C.c_int64),
                 ("rot_dim", C.c_int), ("interleaved", C.c_int), ("positions", C.c_void_p)]
+
+
+class AttentionParams(C.Structure):
+    """``sdp4_attention_params``: packed sequences and their scores' scale."""
+    _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("scale", C.c_float), ("offsets", C.c_void_p),
+                ("sequences", C.c_int64)]
+
+
+class BlockParams(C.Structure):
+    """``sdp4_block_params``: the joint of two blocks."""
+    _fields_ = [("x_dtype", C.c_int), ("y_dtype", C.c_int), ("post_norm", C.c_int), ("post_eps", C.c_float),
+                ("pre_eps", C.c_float), ("post_weight", C.c_void_p), ("pre_weight", C.c_void_p), ("gate", C.c_void_p),
+                ("branch_scale", C.c_float), ("residual_scale", C.c_float)]
 
 
 def lib() -> C.CDLL:
@@ -91,6 +105,16 @@ def lib() -> C.CDLL:
                 "sdp4_qk_norm_rope_grad": (i32, [vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, i64, vp]),
                 "sdp4_qk_grad_workspace": (i64, [i64, i32, i32, i32]),
                 "sdp4_rope_table": (i32, [vp, i32, i64, i64, C.c_double, vp, vp]),
+                "sdp4_attention": (i32, [vp, vp, vp, vp, i64, vp, vp, vp]),
+                "sdp4_attention_grad": (i32, [vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, i64, vp]),
+                "sdp4_attention_grad_workspace": (i64, [i64, i32, i32, i32]),
+                "sdp4_block_norm": (i32, [vp, i64, vp, i64, i64, i64, vp, vp, i64, vp, i64, vp]),
+                "sdp4_block_norm_grad": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, vp,
+                                               vp, i64, vp]),
+                "sdp4_block_norm_grad_workspace": (i64, [i64, i64]),
+                "sdp4_embedding": (i32, [vp, i64, vp, i32, i64, i64, i64, f32, vp, i32, i64, vp]),
+                "sdp4_embedding_grad": (i32, [vp, i64, vp, i32, i64, i64, i64, f32, i32, vp, i32, i64, vp, i64, vp]),
+                "sdp4_embedding_grad_workspace": (i64, [i64, i64, i64]),
                 "sdp4_codes_bytes": (i64, [i64, i32]),
                 "sdp4_num_groups": (i64, [i64, i32]),
                 "sdp4_status_string": (C.c_char_p, [i32]),
@@ -127,7 +151,8 @@ def _bind(L) -> None:
     addresses = [C.cast(getattr(L, "sdp4_" + n), C.c_void_p).value for n in
                  ("qwd_encode", "qwd_decode", "qwd_encode_sym", "qwd_decode_sym", "grad_quant", "grad_quant_sr",
                   "dequant_reduce", "dequant_reduce_sr", "dropout_add", "dropout_add_grad", "token_logprob",
-                  "token_logprob_grad", "token_loss", "qk_norm_rope", "qk_norm_rope_grad")]
+                  "token_logprob_grad", "token_loss", "qk_norm_rope", "qk_norm_rope_grad", "attention", "attention_grad",
+                  "block_norm", "block_norm_grad", "embedding", "embedding_grad")]
     try:
         _binding.bind(*addresses)
     except TypeError:
@@ -608,6 +633,180 @@ def sdp4_rope_table(inv_freq, table, start=0, scale=1.0, stream=None):
     _ck("sdp4_rope_table", lib().sdp4_rope_table(
         _vector(inv_freq, (half,), torch.float64, "inv_freq", False), half, start, table.shape[0], float(scale),
         _vector(table, (table.shape[0], 2 * half), torch.float32, "table", False), _stream(stream)))
+
+
+# Attention, block norms and the embedding run on the device of their arrays, which have to lie on one.
+class _device:
+    """Makes the tensors' device the current one; raises where they lie on several."""
+
+    def __init__(self, *tensors):
+        import torch
+        devices = {t.device for t in tensors if isinstance(t, torch.Tensor)}
+        if len(devices) > 1:
+            raise ValueError(f"sdp4: arrays must lie on one device, not on {sorted(map(str, devices))}")
+        device = devices.pop() if devices else None
+        self.guard = torch.cuda.device(device if device is not None and device.type == "cuda" else None)
+
+    def __enter__(self):
+        self.guard.__enter__()
+
+    def __exit__(self, *error):
+        self.guard.__exit__(*error)
+
+
+def _attention_params(q, scale, offsets):
+    import torch
+    if offsets is None:
+        return AttentionParams(_float_dtype(q, "q"), q.shape[2], scale, None, 0)
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("sdp4: offsets must be [sequences + 1]")
+    count = offsets.shape[0] - 1
+    return AttentionParams(_float_dtype(q, "q"), q.shape[2], scale, _vector(offsets, (count + 1,), torch.int64, "offsets"),
+                           count)
+
+
+def _key_heads(x, what, q, like=None):
+    h = _heads(x, what, like, q.dtype)
+    if x.shape[0] != q.shape[0] or x.shape[2] != q.shape[2]:
+        raise ValueError(f"sdp4: {what} must have the queries' tokens and head_dim")
+    return h
+
+
+def sdp4_attention(q, k, v, scale, offsets, out, lse=None, stream=None):
+    """out <- causal attention of heads [tokens, heads, head_dim] over packed
+    sequences: rows offsets[n] .. offsets[n + 1] - 1 (int64, on the device;
+    None: one sequence), k and v with a divisor of q's heads.  lse
+    [q heads, tokens] float32 may be None."""
+    if _fast is not None and _done("sdp4_attention", _fast.attention(q, k, v, scale, offsets, out, lse, stream)):
+        return
+    import torch
+    hs = [_heads(q, "q"), _key_heads(k, "k", q), _key_heads(v, "v", q, k), _heads(out, "out", q, q.dtype)]
+    prm = _attention_params(q, scale, offsets)
+    lp = _vector(lse, (q.shape[1], q.shape[0]), torch.float32, "lse")
+    with _device(q, k, v, offsets, out, lse):
+        _ck("sdp4_attention", lib().sdp4_attention(*(C.addressof(h) for h in hs[:3]), C.addressof(prm), q.shape[0],
+                                                   C.addressof(hs[3]), lp, _stream(stream)))
+
+
+def sdp4_attention_grad(dout, q, k, v, out, lse, scale, offsets, dq, dk, dv, workspace, stream=None):
+    """dq, dk, dv <- the gradients of sdp4_attention from that of its out;
+    needs out and lse as it left them and a workspace of
+    sdp4_attention_grad_workspace bytes."""
+    if _fast is not None and _done("sdp4_attention_grad", _fast.attention_grad(
+            dout, q, k, v, out, lse, scale, offsets, dq, dk, dv, workspace, stream)):
+        return
+    import torch
+    hs = [_heads(dout, "dout", q, q.dtype), _heads(q, "q"), _key_heads(k, "k", q), _key_heads(v, "v", q, k),
+          _heads(out, "out", q, q.dtype)]
+    outs = [_heads(dq, "dq", q, q.dtype), _heads(dk, "dk", k, q.dtype), _heads(dv, "dv", k, q.dtype)]
+    prm = _attention_params(q, scale, offsets)
+    lp = _vector(lse, (q.shape[1], q.shape[0]), torch.float32, "lse", False)
+    with _device(dout, q, k, v, out, lse, offsets, dq, dk, dv, workspace):
+        _ck("sdp4_attention_grad", lib().sdp4_attention_grad(
+            *(C.addressof(h) for h in hs), lp, C.addressof(prm), q.shape[0], *(C.addressof(h) for h in outs),
+            *_scratch(workspace), _stream(stream)))
+
+
+def sdp4_attention_grad_workspace(tokens, q_heads, k_heads, head_dim) -> int:
+    return lib().sdp4_attention_grad_workspace(tokens, q_heads, k_heads, head_dim)
+
+
+def _block(arrays, post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight):
+    """``sdp4_block_params``, the matrices' addresses and strides, and their shape; ``arrays``: (matrix or None, name, whether
+    it is of the residual stream)."""
+    import torch
+    shape, types, out = None, [None, None], []
+    for x, what, stream in arrays:
+        if x is None:
+            out.append((None, 0))
+            continue
+        p, dt, stride, shape = _matrix(x, what, shape)
+        if types[stream] not in (None, dt):
+            raise ValueError(f"sdp4: {what} must have the type of the {'residual stream' if stream else 'branch'}")
+        types[stream] = dt
+        out.append((p, stride))
+    if shape is None:
+        raise ValueError("sdp4: no matrix given")
+    x_type = types[0] if types[0] is not None else types[1]
+    y_type = types[1] if types[1] is not None else types[0]
+    weight = torch.float32 if x_type == F32 else torch.bfloat16
+    prm = BlockParams(x_type, y_type, post_eps is not None, 0.0 if post_eps is None else post_eps,
+                      0.0 if pre_eps is None else pre_eps, _vector(post_weight, shape[1:], weight, "post_weight"),
+                      _vector(pre_weight, shape[1:], weight, "pre_weight"),
+                      _vector(gate, shape[:1], torch.float32, "gate"), branch_scale, residual_scale)
+    return prm, out, shape
+
+
+def sdp4_block_norm(branch, residual, post_eps, post_weight, gate, branch_scale, residual_scale, y, pre_eps, pre_weight, h,
+                    stream=None):
+    """u <- the RMS norm of branch times post_weight (post_eps None: no norm),
+    y <- residual_scale * residual + branch_scale * gate * u, h <- the RMS norm
+    of y times pre_weight.  gate [rows] is float32; branch or residual, y or
+    h, weights and gate may be None."""
+    if _fast is not None and _done("sdp4_block_norm", _fast.block_norm(
+            branch, residual, post_eps, post_weight, gate, branch_scale, residual_scale, y, pre_eps, pre_weight, h, stream)):
+        return
+    prm, (b, r, yo, ho), shape = _block([(branch, "branch", 0), (residual, "residual", 1), (y, "y", 1), (h, "h", 0)], post_eps,
+                                        post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight)
+    with _device(branch, residual, post_weight, gate, y, pre_weight, h):
+        _ck("sdp4_block_norm", lib().sdp4_block_norm(*b, *r, *shape, C.addressof(prm), *yo, *ho, _stream(stream)))
+
+
+def sdp4_block_norm_grad(dh, dy, branch, y, post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight,
+                         dbranch, dresidual, dpost_weight=None, dpre_weight=None, dgate=None, workspace=None, stream=None):
+    """dbranch, dresidual and the float32 dpost_weight, dpre_weight, dgate <-
+    the gradients of sdp4_block_norm from those of h and y (None: zero); what
+    is None is left out.  Weight gradients need a workspace of
+    sdp4_block_norm_grad_workspace bytes."""
+    if _fast is not None and _done("sdp4_block_norm_grad", _fast.block_norm_grad(
+            dh, dy, branch, y, post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight, dbranch, dresidual,
+            dpost_weight, dpre_weight, dgate, workspace, stream)):
+        return
+    import torch
+    prm, (g, gy, b, yi, db, dr), shape = _block(
+        [(dh, "dh", 0), (dy, "dy", 1), (branch, "branch", 0), (y, "y", 1), (dbranch, "dbranch", 0), (dresidual, "dresidual", 1)],
+        post_eps, post_weight, gate, branch_scale, residual_scale, pre_eps, pre_weight)
+    with _device(dh, dy, branch, y, post_weight, gate, pre_weight, dbranch, dresidual, dpost_weight, dpre_weight, dgate,
+                 workspace):
+        _ck("sdp4_block_norm_grad", lib().sdp4_block_norm_grad(
+            *g, *gy, *b, *yi, *shape, C.addressof(prm), *db, *dr, _vector(dpost_weight, shape[1:], torch.float32, "dpost_weight"),
+            _vector(dpre_weight, shape[1:], torch.float32, "dpre_weight"), _vector(dgate, shape[:1], torch.float32, "dgate"),
+            *_scratch(workspace), _stream(stream)))
+
+
+def sdp4_block_norm_grad_workspace(rows, cols) -> int:
+    return lib().sdp4_block_norm_grad_workspace(rows, cols)
+
+
+def sdp4_embedding(tokens, table, scale, out, stream=None):
+    """out[r] <- scale * table[tokens[r]] for int64 tokens (negative: zeros)."""
+    if _fast is not None and _done("sdp4_embedding", _fast.embedding(tokens, table, scale, out, stream)):
+        return
+    import torch
+    tp, tt, ts, (vocab, cols) = _matrix(table, "table")
+    op, ot, os_, (rows, _) = _matrix(out, "out", (out.shape[0], cols))
+    ids = _vector(tokens, (rows,), torch.int64, "tokens", False)
+    with _device(tokens, table, out):
+        _ck("sdp4_embedding", lib().sdp4_embedding(ids, rows, tp, tt, ts, vocab, cols, scale, op, ot, os_, _stream(stream)))
+
+
+def sdp4_embedding_grad(tokens, dout, scale, dtable, workspace, accumulate=False, stream=None):
+    """dtable <- (accumulate: +=) the gradient of sdp4_embedding's table;
+    needs a workspace of sdp4_embedding_grad_workspace bytes."""
+    if _fast is not None and _done("sdp4_embedding_grad", _fast.embedding_grad(
+            tokens, dout, scale, dtable, workspace, accumulate, stream)):
+        return
+    import torch
+    tp, tt, ts, (vocab, cols) = _matrix(dtable, "dtable")
+    dp, dt, ds, (rows, _) = _matrix(dout, "dout", (dout.shape[0], cols))
+    ids = _vector(tokens, (rows,), torch.int64, "tokens", False)
+    with _device(tokens, dout, dtable, workspace):
+        _ck("sdp4_embedding_grad", lib().sdp4_embedding_grad(ids, rows, dp, dt, ds, vocab, cols, scale, bool(accumulate), tp, tt,
+                                                             ts, *_scratch(workspace), _stream(stream)))
+
+
+def sdp4_embedding_grad_workspace(rows, vocab, cols) -> int:
+    return lib().sdp4_embedding_grad_workspace(rows, vocab, cols)
 
 
 def sdp4_codes_bytes(n, bits):
