@@ -101,63 +101,146 @@ struct HeadTile {
     }
     SDP4_DEV static int at(int r, int chunk) { return r * ROW + ((chunk ^ twist(r)) << 4); }
 
-    // Operand with rows r0 + l % 32, elements 16 s + ... along the sum.
-    SDP4_DEV static void rows(const char *tile, int r0, int s, Frag<T> &f)
-    {
-        const int l = lane_id(), r = l & 31, h = l >> 5;
-        const char *row = tile + r0 * ROW + r * ROW;
-        if constexpr (sizeof(T) == 2) {
-            f.v = *reinterpret_cast<const bf16x8 *>(row + (((2 * s + h) ^ twist(r)) << 4));
-        } else {
-            const u32x4 a = *reinterpret_cast<const u32x4 *>(row + (((4 * s + 2 * h) ^ twist(r)) << 4));
-            const u32x4 b = *reinterpret_cast<const u32x4 *>(row + (((4 * s + 2 * h + 1) ^ twist(r)) << 4));
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                f.v[j] = __uint_as_float(w[j]);
-        }
-    }
+};
 
-    // Operand with the tile's elements 32 db + l % 32 as rows and its rows r0 + 8 a + 4 h + b along the sum.
-    SDP4_DEV static void columns(const char *tile, int r0, int db, Frag<T> &f)
+// Where a lane finds its parts of the operands in a tile, computed once: an access adds a tile's address and a constant.
+template <class T, int DB>
+struct Reader;
+
+template <int DB>
+struct Reader<bf16_t, DB> {
+    using H = HeadTile<bf16_t, DB>;
+    uint32_t in_row[H::STEPS], in_column[DB][2];
+    SDP4_DEV Reader()
     {
-        const int l = lane_id(), h = l >> 5;
-        if constexpr (sizeof(T) == 2) {
-            // a transposing read gives lane i of 16 element i of four rows, of which lane i points at a quarter of row i / 4
-            const int i = l & 15, row = 4 * h + (i >> 2), chunk = 4 * db + 2 * ((l >> 4) & 1) + ((i & 3) >> 1), half = 8 * (i & 1);
-            s16x8 w;
+        const int l = lane_id(), r = l & 31, h = l >> 5, i = l & 15;
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                const char *p = tile + r0 * ROW + (8 * a + row) * ROW + ((chunk ^ twist(8 * a + row)) << 4) + half;
-                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(p));
+        for (int s = 0; s < H::STEPS; ++s)
+            in_row[s] = H::at(r, 2 * s + h);
+        // a transposing read gives lane i of 16 element i of four rows, of which lane i points at a quarter of row i / 4
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    w[4 * a + j] = v[j];
-            }
-            f.v = __builtin_bit_cast(bf16x8, w);
-        } else {
-            const int d = 32 * db + (l & 31);
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = 8 * (j >> 2) + 4 * h + (j & 3);
-                f.v[j] = *reinterpret_cast<const float *>(tile + r0 * ROW + row * ROW + (((d >> 2) ^ twist(row)) << 4) + 4 * (d & 3));
-            }
-        }
+            for (int a = 0; a < 2; ++a)
+                in_column[db][a] = H::at(8 * a + 4 * h + (i >> 2), 4 * db + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 8 * (i & 1);
+    }
+    // Operand with rows r0 + l % 32, elements 16 s + ... along the sum.
+    SDP4_DEV void rows(const char *tile, int r0, int s, Frag<bf16_t> &f) const
+    {
+        f.v = *reinterpret_cast<const bf16x8 *>(tile + in_row[s] + r0 * H::ROW);
+    }
+    // Operand with the tile's elements 32 db + l % 32 as rows and its rows r0 + 8 a + 4 h + b along the sum.
+    SDP4_DEV void columns(const char *tile, int r0, int db, Frag<bf16_t> &f) const
+    {
+        s16x4 v[2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+            v[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(tile + in_column[db][a] + r0 * H::ROW));
+        f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
-// Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile, by THREADS threads.  Rows from `limit`
-// on and elements from `dim` (>= a chunk) on become zeros; other rows and elements are read in their place, so that all loads
-// are in flight together, and a head's last chunk, where it is not whole, as the head's last whole one, shifted.
-template <class T, int DB, int ROWS, int THREADS>
+template <int DB>
+struct Reader<float, DB> {
+    using H = HeadTile<float, DB>;
+    uint32_t in_row[H::STEPS], in_column[8];
+    SDP4_DEV Reader()
+    {
+        const int l = lane_id(), r = l & 31, h = l >> 5;
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+            in_row[s] = H::at(r, 4 * s + 2 * h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            in_column[j] = H::at(8 * (j >> 2) + 4 * h + (j & 3), r >> 2) % (H::ROW * 16) + 4 * (r & 3);
+    }
+    SDP4_DEV void rows(const char *tile, int r0, int s, Frag<float> &f) const
+    {
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(tile + in_row[s] + r0 * H::ROW);
+        const u32x4 b = *reinterpret_cast<const u32x4 *>(tile + (in_row[s] ^ 16) + r0 * H::ROW);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            f.v[j] = __uint_as_float(w[j]);
+    }
+    SDP4_DEV void columns(const char *tile, int r0, int db, Frag<float> &f) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) // in_column is element block 0's place: block db lies eight chunks a block away, twisted by bit 3
+            f.v[j] = *reinterpret_cast<const float *>(tile + in_column[j] + r0 * H::ROW +
+                                                      ((((8 * db) ^ ((j & 2) << 2)) - ((j & 2) << 2)) << 4));
+    }
+};
+
+// Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile: load() starts them, store() has them
+// in the tile before the next barrier.  Rows from `limit` on hold other rows of the head: they are masked, and masked
+// rows may hold anything.  Elements from `dim` on meet zeros of the other operand.
+//
+// Straight into LDS, past the registers, where every row begins on 16 bytes and holds whole chunks: an instruction moves 64
+// chunks to 64 places in turn, so the lanes fetch what belongs at theirs.  A place beyond the head's elements gets the row's
+// first chunk, which is as finite as the row.
+template <class T, int DB, int ROWS, int WAVES, bool DIRECT>
 struct TileLoad {
     using H = HeadTile<T, DB>;
-    static constexpr int COUNT = ROWS * H::USED / THREADS;
+    static constexpr int COUNT = ROWS * H::CHUNKS / (64 * WAVES);
+    static_assert(COUNT * 64 * WAVES == ROWS * H::CHUNKS, "whole rounds");
+    const char *head;
+    int64_t pitch; // bytes from row to row
+    uint32_t offset[COUNT], element[COUNT], row[COUNT];
+
+    SDP4_DEV void begin(const T *h, int64_t stride, int dim)
+    {
+        head = reinterpret_cast<const char *>(h), pitch = stride * (int64_t)sizeof(T);
+        const int wave = uniform(threadIdx.x / kWave);
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int id = (wave * COUNT + i) * 64 + lane_id(), r = id / H::CHUNKS, c = (id % H::CHUNKS) ^ H::twist(r);
+            row[i] = r;
+            element[i] = (c * H::N < dim ? c : 0) * 16;
+            offset[i] = row[i] * (uint32_t)pitch + element[i];
+        }
+    }
+    SDP4_DEV void move(const T *h) { head = reinterpret_cast<const char *>(h); }
+    SDP4_DEV void load(char *tile, int first, int limit)
+    {
+        const uint64_t base = uniform((uint64_t)(head + first * pitch));
+        const uint32_t at = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile + threadIdx.x / kWave * COUNT * 1024);
+        if (first + ROWS <= limit) {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i)
+                start(at + i * 1024, offset[i], base);
+        } else {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const uint32_t last = limit - first - 1;
+                start(at + i * 1024, (row[i] < last ? row[i] : last) * (uint32_t)pitch + element[i], base);
+            }
+        }
+    }
+    // No register is written, so the compiler need not know that this is under way: store() waits for it.
+    SDP4_DEV static void start(uint32_t at, uint32_t off, uint64_t base)
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory");
+    }
+    SDP4_DEV void store(char *, int, int) const { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+};
+
+// Through registers, for all other heads: a head's last chunk, where it is not whole, is read as the head's last whole one and
+// shifted.
+template <class T, int DB, int ROWS, int WAVES>
+struct TileLoad<T, DB, ROWS, WAVES, false> {
+    using H = HeadTile<T, DB>;
+    static constexpr int THREADS = 64 * WAVES, COUNT = ROWS * H::USED / THREADS;
     static_assert(COUNT * THREADS == ROWS * H::USED, "whole rounds");
     u32x4 v[COUNT];
+    const T *head;
+    int64_t stride;
+    int dim;
 
-    SDP4_DEV void load(const T *head, int64_t stride, int first, int limit, int dim)
+    SDP4_DEV void begin(const T *h, int64_t s, int d) { head = h, stride = s, dim = d; }
+    SDP4_DEV void move(const T *h) { head = h; }
+    SDP4_DEV void load(char *, int first, int limit)
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
@@ -166,7 +249,7 @@ struct TileLoad {
             v[i] = load_chunk<false>(head + row * stride + (e + H::N <= dim ? e : dim - H::N));
         }
     }
-    SDP4_DEV void store(char *tile, int first, int limit, int dim) const
+    SDP4_DEV void store(char *tile, int, int) const
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
@@ -174,7 +257,7 @@ struct TileLoad {
             u32x4 w = v[i];
             if (dim % H::N)
                 w = e + H::N <= dim ? w : shifted(w, e + H::N - dim);
-            *reinterpret_cast<u32x4 *>(tile + H::at(r, e / H::N)) = first + r < limit && e < dim ? w : u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(tile + H::at(r, e / H::N)) = e < dim ? w : u32x4{0, 0, 0, 0};
         }
     }
     SDP4_DEV static u32x4 shifted(u32x4 w, int by) // by elements toward the first, with zeros behind; by >= N is not used
@@ -183,6 +266,14 @@ struct TileLoad {
         return __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, w) >> bits);
     }
 };
+
+// Heads whose rows can go straight into LDS: whole chunks at multiples of 16 bytes, 64 rows within 2 GB.
+inline bool direct(const Heads &h, int dtype, int dim)
+{
+    const int64_t size = dtype == SDP4_BF16 ? 2 : 4;
+    return reinterpret_cast<uintptr_t>(h.p) % 16 == 0 && dim * size % 16 == 0 && h.token_stride * size % 16 == 0 &&
+           h.head_stride * size % 16 == 0 && 64 * h.token_stride * size < (int64_t(1) << 31);
+}
 
 // A fragment whose masked places must not reach the product: what is infinite or NaN becomes 0 and is noted in `found`
 // (bit j: element j), since 0 times such a value would be NaN.

@@ -14,14 +14,14 @@ namespace sdp4 {
 namespace {
 
 // WAVES waves of 32 rows each, BN keys at a time, STAGES tiles in LDS.
-template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
+template <class T, int DB, int WAVES, int BN, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Heads qh, Heads kh, Heads vh, Heads oh, float *lse,
                                                              int tiles, int64_t items)
 {
     using H = HeadTile<T, DB>;
     constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
-    __shared__ __align__(16) char kt[STAGES][BN * H::ROW];
-    __shared__ __align__(16) char vt[STAGES][BN * H::ROW];
+    __shared__ __align__(16) char kt[2][BN * H::ROW];
+    __shared__ __align__(16) char vt[2][BN * H::ROW];
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
@@ -38,6 +38,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
     fill_samples<THREADS>(at.seq, samples);
     const Span span = span_of(at.seq, samples, row);
     const int start = span.on ? span.first : INT_MAX;
+    const uint32_t seen = span.on ? row - start + 1 : 0; // keys of the row, from start on
     const int w_first = min_wave(start), w_last = max_wave(span.on ? row : -1); // keys that the wave's rows see
     const int w_full = max_wave(start);                                        // from here to q0 all of them see all
     if (lane == 0)
@@ -51,6 +52,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
     }
     if (last < 0) // no row of the block is in a sequence
         return;
+    first = (int)uniform((uint32_t)first), last = (int)uniform((uint32_t)last);
 
     const T *qrow = static_cast<const T *>(qh.p) + (int64_t)(row < at.seq.tokens ? row : at.seq.tokens - 1) * qh.token_stride +
                     head * qh.head_stride;
@@ -65,115 +67,120 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
     bool poison = false;
     f32x16 o[DB] = {};
 
-    TileLoad<T, DB, BN, THREADS> kl, vl;
-    kl.load(kp, kh.token_stride, first, last + 1, at.dim);
-    vl.load(vp, vh.token_stride, first, last + 1, at.dim);
-    int stage = 0;
-    for (int k0 = first; k0 <= last; k0 += BN) {
-        if (STAGES == 1 && k0 != first)
+    const Reader<T, DB> read;
+    TileLoad<T, DB, BN, WAVES, DIRECT> kl, vl;
+    kl.begin(kp, kh.token_stride, at.dim);
+    vl.begin(vp, vh.token_stride, at.dim);
+    // CAREFUL: infinities and NaN in masked places are kept from the product, where 0 times them would be NaN
+    auto walk = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        kl.load(kt[0], first, last + 1);
+        vl.load(vt[0], first, last + 1);
+        int stage = 0;
+        for (int k0 = first; k0 <= last; k0 += BN) {
+            kl.store(kt[stage], k0, last + 1);
+            vl.store(vt[stage], k0, last + 1);
             __syncthreads();
-        kl.store(kt[stage], k0, last + 1, at.dim);
-        vl.store(vt[stage], k0, last + 1, at.dim);
-        __syncthreads();
-        if (k0 + BN <= last) {
-            kl.load(kp, kh.token_stride, k0 + BN, last + 1, at.dim);
-            vl.load(vp, vh.token_stride, k0 + BN, last + 1, at.dim);
-        }
-        const char *kb = kt[stage], *vb = vt[stage];
-        if (STAGES == 2)
-            stage ^= 1;
-        if (k0 > w_last || k0 + BN <= w_first)
-            continue;
-        const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
-
-        f32x16 x[RB] = {};
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int s = 0; s < H::STEPS; ++s) {
-                Frag<T> a;
-                H::rows(kb, 32 * rb, s, a);
-                mma(a, q[s], x[rb]);
+            if (k0 + BN <= last) {
+                kl.load(kt[stage ^ 1], k0 + BN, last + 1);
+                vl.load(vt[stage ^ 1], k0 + BN, last + 1);
             }
-        if (masked) {
+            const char *kb = kt[stage], *vb = vt[stage];
+            stage ^= 1;
+            if (k0 > w_last || k0 + BN <= w_first)
+                continue;
+            const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
+
+            f32x16 x[RB] = {};
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
+            for (int s = 0; s < H::STEPS; ++s)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                    x[rb][r] = key >= start && key <= row ? x[rb][r] : -__builtin_inff();
-                }
-        }
-        float mx = x[0][0];
-#pragma unroll
-        for (int i = 1; i < 16 * RB; ++i)
-            mx = fmaxf(mx, x[i / 16][i % 16]);
-        mx = fmaxf(mx, xor_lane<32>(mx));
-        // The reference is the largest score so far, so that a key which takes a row alone has p = 1, without a rounding.  Tiles
-        // that raise none of the wave's rows leave the results as they are.
-        const bool up = mx > m;
-        if (__any(up)) {
-            const float to = up ? mx : m;
-            const float from = m * c, ref = to * c; // as the exponents below take them
-            const bool large = __builtin_fabsf(from) >= kLargeScore || __builtin_fabsf(ref) >= kLargeScore;
-            const float by = up ? exp2_of(large ? (m - to) * c : from - ref) : 1.0f;
-            m = to;
-            total *= by;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    o[db][r] *= by;
-        }
-        float ref = m == -__builtin_inff() ? 0.0f : m * c;
-        const bool large = __builtin_fabsf(ref) >= kLargeScore;
-        if (__any(large)) { // a product's rounding would move its exponent: subtract first
-#pragma unroll
-            for (int i = 0; i < 16 * RB; ++i)
-                x[i / 16][i % 16] -= large ? m : 0.0f;
-            ref = large ? 0.0f : ref;
-        }
-#pragma unroll
-        for (int i = 0; i < 16 * RB; ++i) {
-            const float p = exp2_of(__builtin_fmaf(x[i / 16][i % 16], c, -ref));
-            x[i / 16][i % 16] = p;
-            total += p;
-        }
-        Frag<T> p[2 * RB]; // bfloat16: the one rounding on the way to the second product
-#pragma unroll
-        for (int s = 0; s < 2 * RB; ++s) {
-            float w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                w[j] = x[s / 2][8 * (s % 2) + j];
-            p[s].set(w);
-        }
-        if (!masked) {
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int s = 0; s < 2 * RB; ++s) {
+                for (int rb = 0; rb < RB; ++rb) {
                     Frag<T> a;
-                    H::columns(vb, 16 * s, db, a);
-                    mma(a, p[s], o[db]);
+                    read.rows(kb, 32 * rb, s, a);
+                    mma(a, q[s], x[rb]);
                 }
-        } else {
+            if (masked) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
+                        x[rb][r] = key - start < seen ? x[rb][r] : -__builtin_inff();
+                    }
+            }
+            float mx = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 16 * RB; ++i)
+                mx = fmaxf(mx, x[i / 16][i % 16]);
+            mx = fmaxf(mx, xor_lane<32>(mx));
+            // The reference is the largest score so far, so that a key which takes a row alone has p = 1, without a rounding.
+            // Tiles that raise none of the wave's rows leave the results as they are.
+            const bool up = mx > m;
+            if (__any(up)) {
+                const float to = up ? mx : m;
+                const float from = m * c, ref = to * c; // as the exponents below take them
+                const bool large = __builtin_fabsf(from) >= kLargeScore || __builtin_fabsf(ref) >= kLargeScore;
+                const float by = up ? exp2_of(large ? (m - to) * c : from - ref) : 1.0f;
+                m = to;
+                total *= by;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        o[db][r] *= by;
+            }
+            float ref = m == -__builtin_inff() ? 0.0f : m * c;
+            const bool large = __builtin_fabsf(ref) >= kLargeScore;
+            if (__any(large)) { // a product's rounding would move its exponent: subtract first
+#pragma unroll
+                for (int i = 0; i < 16 * RB; ++i)
+                    x[i / 16][i % 16] -= large ? m : 0.0f;
+                ref = large ? 0.0f : ref;
+            }
+            Frag<T> p[2 * RB]; // bfloat16: the one rounding on the way to the second product
+#pragma unroll
+            for (int s = 0; s < 2 * RB; ++s) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    w[j] = exp2_of(__builtin_fmaf(x[s / 2][8 * (s % 2) + j], c, -ref));
+                    total += w[j];
+                }
+                p[s].set(w);
+            }
             uint64_t found = 0;
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+            for (int s = 0; s < 2 * RB; ++s)
 #pragma unroll
-                for (int s = 0; s < 2 * RB; ++s) {
+                for (int db = 0; db < DB; ++db) {
                     Frag<T> a;
-                    H::columns(vb, 16 * s, db, a);
-                    found |= tile_rows(scrub(a), 16 * s);
+                    read.columns(vb, 16 * s, db, a);
+                    if (CAREFUL && masked)
+                        found |= tile_rows(scrub(a), 16 * s);
                     mma(a, p[s], o[db]);
                 }
-            if (__any(found != 0)) {
+            if (CAREFUL && __any(found != 0)) {
                 found = or_wave(found);
                 for (int j = 0; j < BN; ++j)
-                    poison |= (found >> j & 1) && k0 + j >= start && k0 + j <= row;
+                    poison |= (found >> j & 1) && (uint32_t)(k0 + j - start) < seen;
             }
         }
+    };
+    walk(std::false_type{});
+    // NaN: some value that is not finite, perhaps one that no row of the wave may see
+    bool bad = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            bad |= o[db][r] != o[db][r];
+    if (__syncthreads_or(bad)) {
+        m = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            o[db] = f32x16{};
+        walk(std::true_type{});
     }
 
     total += xor_lane<32>(total);
@@ -199,13 +206,14 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
             : total == 0.0f ? -__builtin_inff() : total;
 }
 
-template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
-int run(const Attention &at, const Heads &q, const Heads &k, const Heads &v, const Heads &out, float *lse, hipStream_t s)
+template <class T, int DB, int WAVES, int BN, int OCC>
+int run(int dtype, const Attention &at, const Heads &q, const Heads &k, const Heads &v, const Heads &out, float *lse, hipStream_t s)
 {
     const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
     const int64_t items = (int64_t)tiles * q.heads;
-    return launch<WAVES>(k_attention<T, DB, WAVES, BN, STAGES, OCC>, shared_blocks(items), kUncapped, s, at, q, k, v, out, lse,
-                         tiles, items);
+    auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention<T, DB, WAVES, BN, OCC, true>
+                                                                       : k_attention<T, DB, WAVES, BN, OCC, false>;
+    return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, q, k, v, out, lse, tiles, items);
 }
 
 } // namespace
@@ -216,20 +224,20 @@ int launch_attention(int dtype, const Attention &at, const Heads &q, const Heads
     const int db = (at.dim + 31) / 32;
     if (dtype == SDP4_BF16) {
         if (db <= 2)
-            return run<bf16_t, 2, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
+            return run<bf16_t, 2, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
         if (db == 3)
-            return run<bf16_t, 3, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
+            return run<bf16_t, 3, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
         if (db == 4)
-            return run<bf16_t, 4, 4, 64, 2, 2>(at, q, k, v, out, lse, s);
-        return run<bf16_t, 8, 4, 32, 2, 1>(at, q, k, v, out, lse, s);
+            return run<bf16_t, 4, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
+        return run<bf16_t, 8, 4, 32, 1>(dtype, at, q, k, v, out, lse, s);
     }
     if (db <= 2)
-        return run<float, 2, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
+        return run<float, 2, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
     if (db == 3)
-        return run<float, 3, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
+        return run<float, 3, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
     if (db == 4)
-        return run<float, 4, 4, 32, 2, 2>(at, q, k, v, out, lse, s);
-    return run<float, 8, 4, 32, 2, 1>(at, q, k, v, out, lse, s);
+        return run<float, 4, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
+    return run<float, 8, 4, 32, 1>(dtype, at, q, k, v, out, lse, s);
 }
 
 } // namespace sdp4

@@ -46,21 +46,39 @@ SDP4_DEV void operands(const f32x16 &x, Frag<T> (&f)[2])
     }
 }
 
-// out += tile's columns times p, for 32 rows of the tile from r0 on
-template <class T, int DB>
-SDP4_DEV void add_product(const char *tile, int r0, const Frag<T> (&p)[2], bool masked, f32x16 (&out)[DB], uint64_t &found)
+// out += tile's columns times p, for 32 rows of the tile from r0 on.  CAREFUL: what is infinite or NaN stays out and is noted.
+template <bool CAREFUL, class T, int DB>
+SDP4_DEV void add_product(const Reader<T, DB> &read, const char *tile, int r0, const Frag<T> (&p)[2], f32x16 (&out)[DB], uint64_t &found)
 {
-    using H = HeadTile<T, DB>;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int db = 0; db < DB; ++db) {
             Frag<T> a;
-            H::columns(tile, r0 + 16 * s, db, a);
-            if (masked)
+            read.columns(tile, r0 + 16 * s, db, a);
+            if (CAREFUL)
                 found |= tile_rows(scrub(a), r0 + 16 * s);
             mma(a, p[s], out[db]);
         }
+}
+
+template <int DB>
+SDP4_DEV bool has_nan(const f32x16 (&x)[DB])
+{
+    bool bad = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            bad |= x[db][r] != x[db][r];
+    return bad;
+}
+template <int DB>
+SDP4_DEV void clear(f32x16 (&x)[DB])
+{
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        x[db] = f32x16{};
 }
 
 template <class T, int DB>
@@ -80,15 +98,15 @@ SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
         }
 }
 
-template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
+template <class T, int DB, int WAVES, int BN, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, Heads doh, Heads qh, Heads kh, Heads vh, Heads oh,
                                                                 const float *lse, Heads dqh, float *delta, int tiles,
                                                                 int64_t items)
 {
     using H = HeadTile<T, DB>;
     constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
-    __shared__ __align__(16) char kt[STAGES][BN * H::ROW];
-    __shared__ __align__(16) char vt[STAGES][BN * H::ROW];
+    __shared__ __align__(16) char kt[2][BN * H::ROW];
+    __shared__ __align__(16) char vt[2][BN * H::ROW];
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
@@ -105,6 +123,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
     fill_samples<THREADS>(at.seq, samples);
     const Span span = span_of(at.seq, samples, row);
     const int start = span.on ? span.first : INT_MAX;
+    const uint32_t seen = span.on ? row - start + 1 : 0; // keys of the row, from start on
     const int w_first = min_wave(start), w_last = max_wave(span.on ? row : -1), w_full = max_wave(start);
     if (lane == 0)
         edges[wave][0] = w_first, edges[wave][1] = w_last;
@@ -117,6 +136,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
     }
     if (last < 0)
         return;
+    first = (int)uniform((uint32_t)first), last = (int)uniform((uint32_t)last);
 
     const int64_t at_row = row < at.seq.tokens ? row : at.seq.tokens - 1;
     const T *qrow = static_cast<const T *>(qh.p) + at_row * qh.token_stride + head * qh.head_stride;
@@ -144,58 +164,69 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
 
     bool poison = false;
     f32x16 dq[DB] = {};
-    TileLoad<T, DB, BN, THREADS> kl, vl;
-    kl.load(kp, kh.token_stride, first, last + 1, at.dim);
-    vl.load(vp, vh.token_stride, first, last + 1, at.dim);
-    int stage = 0;
-    for (int k0 = first; k0 <= last; k0 += BN) {
-        if (STAGES == 1 && k0 != first)
+    const Reader<T, DB> read;
+    TileLoad<T, DB, BN, WAVES, DIRECT> kl, vl;
+    kl.begin(kp, kh.token_stride, at.dim);
+    vl.begin(vp, vh.token_stride, at.dim);
+    auto walk = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        kl.load(kt[0], first, last + 1);
+        vl.load(vt[0], first, last + 1);
+        int stage = 0;
+        for (int k0 = first; k0 <= last; k0 += BN) {
+            kl.store(kt[stage], k0, last + 1);
+            vl.store(vt[stage], k0, last + 1);
             __syncthreads();
-        kl.store(kt[stage], k0, last + 1, at.dim);
-        vl.store(vt[stage], k0, last + 1, at.dim);
-        __syncthreads();
-        if (k0 + BN <= last) {
-            kl.load(kp, kh.token_stride, k0 + BN, last + 1, at.dim);
-            vl.load(vp, vh.token_stride, k0 + BN, last + 1, at.dim);
-        }
-        const char *kb = kt[stage], *vb = vt[stage];
-        if (STAGES == 2)
+            if (k0 + BN <= last) {
+                kl.load(kt[stage ^ 1], k0 + BN, last + 1);
+                vl.load(vt[stage ^ 1], k0 + BN, last + 1);
+            }
+            const char *kb = kt[stage], *vb = vt[stage];
             stage ^= 1;
-        if (k0 > w_last || k0 + BN <= w_first)
-            continue;
-        const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
-        uint64_t found = 0;
+            if (k0 > w_last || k0 + BN <= w_first)
+                continue;
+            const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
+            uint64_t found = 0;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            f32x16 x = {}, y = {};
+            for (int rb = 0; rb < RB; ++rb) {
+                f32x16 x = {}, y = {};
 #pragma unroll
-            for (int s = 0; s < H::STEPS; ++s) {
-                Frag<T> a;
-                H::rows(kb, 32 * rb, s, a);
-                mma(a, q[s], x);
-                H::rows(vb, 32 * rb, s, a);
-                mma(a, g[s], y);
-            }
-            probabilities(x, c, l, large);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                x[r] *= y[r] - along;
-            if (masked) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                    x[r] = key >= start && key <= row ? x[r] : 0.0f;
+                for (int s = 0; s < H::STEPS; ++s) {
+                    Frag<T> a, b;
+                    read.rows(kb, 32 * rb, s, a);
+                    read.rows(vb, 32 * rb, s, b);
+                    mma(a, q[s], x);
+                    mma(b, g[s], y);
                 }
+                probabilities(x, c, l, large);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x[r] *= y[r] - along;
+                if (masked) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
+                        x[r] = key - start < seen ? x[r] : 0.0f;
+                    }
+                }
+                Frag<T> p[2];
+                operands(x, p);
+                if (CAREFUL && masked)
+                    add_product<true>(read, kb, 32 * rb, p, dq, found);
+                else
+                    add_product<false>(read, kb, 32 * rb, p, dq, found);
             }
-            Frag<T> p[2];
-            operands(x, p);
-            add_product<T, DB>(kb, 32 * rb, p, masked, dq, found);
+            if (CAREFUL && __any(found != 0)) {
+                found = or_wave(found);
+                for (int j = 0; j < BN; ++j)
+                    poison |= (found >> j & 1) && (uint32_t)(k0 + j - start) < seen;
+            }
         }
-        if (masked && __any(found != 0)) {
-            found = or_wave(found);
-            for (int j = 0; j < BN; ++j)
-                poison |= (found >> j & 1) && k0 + j >= start && k0 + j <= row;
-        }
+    };
+    walk(std::false_type{});
+    if (__syncthreads_or(has_nan(dq))) { // some value is not finite, perhaps one that no row of the wave may see
+        clear(dq);
+        walk(std::true_type{});
     }
     if (span.on)
         store_row(static_cast<T *>(dqh.p) + at_row * dqh.token_stride + head * dqh.head_stride, at.dim, dq,
@@ -203,7 +234,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
 }
 
 // Columns are keys here: a lane's key and value stay in registers as operands.  PARTS: 1 dv, 2 dk, 3 both.
-template <class T, int DB, int WAVES, int BQ, int STAGES, int OCC, int PARTS>
+template <class T, int DB, int WAVES, int BQ, int OCC, bool DIRECT, int PARTS>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at, Heads doh, Heads qh, Heads kh, Heads vh,
                                                                  const float *lse, Heads dkh, Heads dvh, const float *delta,
                                                                  int tiles, int64_t items)
@@ -211,9 +242,9 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at,
     using H = HeadTile<T, DB>;
     constexpr int BK = 32 * WAVES, THREADS = 64 * WAVES, RB = BQ / 32;
     constexpr bool WITH_V = PARTS & 1, WITH_K = PARTS & 2;
-    __shared__ __align__(16) char qt[STAGES][BQ * H::ROW];
-    __shared__ __align__(16) char gt[STAGES][BQ * H::ROW];
-    __shared__ __align__(16) float lt[STAGES][BQ], dt[STAGES][BQ];
+    __shared__ __align__(16) char qt[2][BQ * H::ROW];
+    __shared__ __align__(16) char gt[2][BQ * H::ROW];
+    __shared__ __align__(16) float lt[2][BQ], dt[2][BQ];
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
@@ -240,6 +271,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at,
     }
     if (limit < 0)
         return;
+    first = (int)uniform((uint32_t)first), limit = (int)uniform((uint32_t)limit);
 
     const int64_t at_key = key < at.seq.tokens ? key : at.seq.tokens - 1;
     const T *krow = static_cast<const T *>(kh.p) + at_key * kh.token_stride + kv * kh.head_stride;
@@ -257,99 +289,117 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at,
 
     bool poison_k = false, poison_v = false;
     f32x16 dk[WITH_K ? DB : 1] = {}, dv[WITH_V ? DB : 1] = {};
-    TileLoad<T, DB, BQ, THREADS> ql, gl;
-    float stat = 0.0f; // threads 0 .. BQ - 1: lse, the next BQ: D
-    int nq = first, nhead = kv * at.group;
-    auto fetch = [&] {
-        ql.load(static_cast<const T *>(qh.p) + nhead * qh.head_stride, qh.token_stride, nq, limit, at.dim);
-        gl.load(static_cast<const T *>(doh.p) + nhead * doh.head_stride, doh.token_stride, nq, limit, at.dim);
-        if (threadIdx.x < 2 * BQ) {
-            const int r = nq + (threadIdx.x & (BQ - 1));
-            stat = (threadIdx.x < BQ ? lse : delta)[(int64_t)nhead * at.seq.tokens + (r < limit ? r : limit - 1)];
-        }
-    };
-    fetch();
-    int stage = 0;
-    for (int64_t i = 0; i < count; ++i) {
-        const int q0 = nq;
-        if (STAGES == 1 && i > 0)
+    const Reader<T, DB> read;
+    TileLoad<T, DB, BQ, WAVES, DIRECT> ql, gl;
+    ql.begin(nullptr, qh.token_stride, at.dim);
+    gl.begin(nullptr, doh.token_stride, at.dim);
+    const uint32_t seen = span.on ? end - key : 0; // queries that see the key, from its own on
+    auto walk = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        float stat = 0.0f; // threads 0 .. BQ - 1: lse, the next BQ: D
+        int nq = first, nhead = kv * at.group;
+        auto fetch = [&](int stage) {
+            ql.move(static_cast<const T *>(qh.p) + nhead * qh.head_stride);
+            gl.move(static_cast<const T *>(doh.p) + nhead * doh.head_stride);
+            ql.load(qt[stage], nq, limit);
+            gl.load(gt[stage], nq, limit);
+            if (threadIdx.x < 2 * BQ) {
+                const int r = nq + (threadIdx.x & (BQ - 1));
+                stat = (threadIdx.x < BQ ? lse : delta)[(int64_t)nhead * at.seq.tokens + (r < limit ? r : limit - 1)];
+            }
+        };
+        fetch(0);
+        int stage = 0;
+        for (int64_t i = 0; i < count; ++i) {
+            const int q0 = nq;
+            ql.store(qt[stage], q0, limit);
+            gl.store(gt[stage], q0, limit);
+            if (threadIdx.x < BQ)
+                lt[stage][threadIdx.x] = octaves(stat);
+            else if (threadIdx.x < 2 * BQ)
+                dt[stage][threadIdx.x - BQ] = stat;
             __syncthreads();
-        ql.store(qt[stage], q0, limit, at.dim);
-        gl.store(gt[stage], q0, limit, at.dim);
-        if (threadIdx.x < BQ)
-            lt[stage][threadIdx.x] = octaves(stat);
-        else if (threadIdx.x < 2 * BQ)
-            dt[stage][threadIdx.x - BQ] = stat;
-        __syncthreads();
-        nq += BQ;
-        if (nq >= limit)
-            nq = first, ++nhead;
-        if (i + 1 < count)
-            fetch();
-        const char *qb = qt[stage], *gb = gt[stage];
-        const float *lb = lt[stage], *db = dt[stage];
-        if (STAGES == 2)
+            nq += BQ;
+            if (nq >= limit)
+                nq = first, ++nhead;
+            if (i + 1 < count)
+                fetch(stage ^ 1);
+            const char *qb = qt[stage], *gb = gt[stage];
+            const float *lb = lt[stage], *db = dt[stage];
             stage ^= 1;
-        if (q0 >= w_end || q0 + BQ <= w_first)
-            continue;
-        const bool masked = !(q0 >= w_all && q0 + BQ <= w_until);
-        uint64_t found_q = 0, found_g = 0;
+            if (q0 >= w_end || q0 + BQ <= w_first)
+                continue;
+            const bool masked = !(q0 >= w_all && q0 + BQ <= w_until);
+            uint64_t found_q = 0, found_g = 0;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            f32x16 x = {}, y = {};
+            for (int rb = 0; rb < RB; ++rb) {
+                f32x16 x = {}, y = {};
 #pragma unroll
-            for (int s = 0; s < H::STEPS; ++s) {
-                Frag<T> a;
-                H::rows(qb, 32 * rb, s, a);
-                mma(a, k[s], x);
-                if constexpr (WITH_K) {
-                    H::rows(gb, 32 * rb, s, a);
-                    mma(a, v[s], y);
+                for (int s = 0; s < H::STEPS; ++s) {
+                    Frag<T> a, b;
+                    read.rows(qb, 32 * rb, s, a);
+                    if constexpr (WITH_K)
+                        read.rows(gb, 32 * rb, s, b);
+                    mma(a, k[s], x);
+                    if constexpr (WITH_K)
+                        mma(b, v[s], y);
                 }
-            }
-            float l[16];
-            bool large = false;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                l[r] = lb[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
-                large |= __builtin_fabsf(l[r]) >= kLargeScore;
-            }
-            probabilities(x, c, l, __any(large));
-            if (masked) {
+                float l[16];
+                bool large = false;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                    x[r] = q >= key && q < end ? x[r] : 0.0f;
+                    l[r] = lb[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
+                    large |= __builtin_fabsf(l[r]) >= kLargeScore;
                 }
-            }
-            Frag<T> p[2];
-            if constexpr (WITH_V) {
-                operands(x, p);
-                add_product<T, DB>(gb, 32 * rb, p, masked, dv, found_g);
-            }
-            if constexpr (WITH_K) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    x[r] *= y[r] - db[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
-                if (masked) { // what stands in masked places may be NaN
+                probabilities(x, c, l, __any(large));
+                if (masked) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                        x[r] = q >= key && q < end ? x[r] : 0.0f;
+                        const uint32_t q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
+                        x[r] = q - key < seen ? x[r] : 0.0f;
                     }
                 }
-                operands(x, p);
-                add_product<T, DB>(qb, 32 * rb, p, masked, dk, found_q);
+                Frag<T> p[2];
+                if constexpr (WITH_V) {
+                    operands(x, p);
+                    if (CAREFUL && masked)
+                        add_product<true>(read, gb, 32 * rb, p, dv, found_g);
+                    else
+                        add_product<false>(read, gb, 32 * rb, p, dv, found_g);
+                }
+                if constexpr (WITH_K) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        x[r] *= y[r] - db[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
+                    if (masked) { // y and D may be NaN in masked places
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const uint32_t q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
+                            x[r] = q - key < seen ? x[r] : 0.0f;
+                        }
+                    }
+                    operands(x, p);
+                    if (CAREFUL && masked)
+                        add_product<true>(read, qb, 32 * rb, p, dk, found_q);
+                    else
+                        add_product<false>(read, qb, 32 * rb, p, dk, found_q);
+                }
+            }
+            if (CAREFUL && __any((found_q | found_g) != 0)) {
+                found_q = or_wave(found_q), found_g = or_wave(found_g);
+                for (int j = 0; j < BQ; ++j) {
+                    const bool sees = (uint32_t)(q0 + j - key) < seen;
+                    poison_k |= (found_q >> j & 1) && sees;
+                    poison_v |= (found_g >> j & 1) && sees;
+                }
             }
         }
-        if (masked && __any((found_q | found_g) != 0)) {
-            found_q = or_wave(found_q), found_g = or_wave(found_g);
-            for (int j = 0; j < BQ; ++j) {
-                const bool sees = q0 + j >= key && q0 + j < end;
-                poison_k |= (found_q >> j & 1) && sees;
-                poison_v |= (found_g >> j & 1) && sees;
-            }
-        }
+    };
+    walk(std::false_type{});
+    if (__syncthreads_or(has_nan(dk) || has_nan(dv))) { // some value is not finite, perhaps one that is masked
+        clear(dk);
+        clear(dv);
+        walk(std::true_type{});
     }
     if (!span.on)
         return;
@@ -369,21 +419,25 @@ struct Grad {
     float *delta;
     hipStream_t s;
 
-    template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
+    int dtype;
+
+    template <class T, int DB, int WAVES, int BN, int OCC>
     int queries() const
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * q.heads;
-        return launch<WAVES>(k_attention_dq<T, DB, WAVES, BN, STAGES, OCC>, shared_blocks(items), kUncapped, s, at, dout, q, k, v,
-                             out, lse, dq, delta, tiles, items);
+        auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention_dq<T, DB, WAVES, BN, OCC, true>
+                                                                           : k_attention_dq<T, DB, WAVES, BN, OCC, false>;
+        return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, out, lse, dq, delta, tiles, items);
     }
-    template <class T, int DB, int WAVES, int BQ, int STAGES, int OCC, int PARTS = 3>
+    template <class T, int DB, int WAVES, int BQ, int OCC, int PARTS = 3>
     int keys() const
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * k.heads;
-        return launch<WAVES>(k_attention_dkv<T, DB, WAVES, BQ, STAGES, OCC, PARTS>, shared_blocks(items), kUncapped, s, at, dout,
-                             q, k, v, lse, dk, dv, delta, tiles, items);
+        auto kernel = direct(q, dtype, at.dim) && direct(dout, dtype, at.dim) ? k_attention_dkv<T, DB, WAVES, BQ, OCC, true, PARTS>
+                                                                             : k_attention_dkv<T, DB, WAVES, BQ, OCC, false, PARTS>;
+        return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, lse, dk, dv, delta, tiles, items);
     }
 };
 
@@ -398,27 +452,27 @@ int launch_attention_grad(int dtype, const Attention &at, const Heads &dout, con
                           const Heads &out, const float *lse, const Heads &dq, const Heads &dk, const Heads &dv,
                           float *workspace, hipStream_t s)
 {
-    const Grad g{at, dout, q, k, v, out, lse, dq, dk, dv, workspace, s};
+    const Grad g{at, dout, q, k, v, out, lse, dq, dk, dv, workspace, s, dtype};
     const int db = (at.dim + 31) / 32;
     int rc;
     if (dtype == SDP4_BF16) {
         if (db <= 2)
-            return (rc = g.queries<bf16_t, 2, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 2, 4, 32, 2, 2>();
+            return (rc = g.queries<bf16_t, 2, 4, 64, 2>()) ? rc : g.keys<bf16_t, 2, 4, 32, 2>();
         if (db == 3)
-            return (rc = g.queries<bf16_t, 3, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 3, 4, 64, 2, 1>();
+            return (rc = g.queries<bf16_t, 3, 4, 64, 2>()) ? rc : g.keys<bf16_t, 3, 4, 64, 1>();
         if (db == 4)
-            return (rc = g.queries<bf16_t, 4, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 4, 4, 32, 2, 1>();
-        return (rc = g.queries<bf16_t, 8, 4, 32, 2, 1>()) ? rc : g.keys<bf16_t, 8, 4, 32, 2, 1>();
+            return (rc = g.queries<bf16_t, 4, 4, 64, 2>()) ? rc : g.keys<bf16_t, 4, 4, 32, 1>();
+        return (rc = g.queries<bf16_t, 8, 4, 32, 1>()) ? rc : g.keys<bf16_t, 8, 4, 32, 1>();
     }
     if (db <= 2)
-        return (rc = g.queries<float, 2, 4, 32, 2, 1>()) ? rc : g.keys<float, 2, 4, 32, 2, 1>();
+        return (rc = g.queries<float, 2, 4, 32, 1>()) ? rc : g.keys<float, 2, 4, 32, 1>();
     if (db == 3)
-        return (rc = g.queries<float, 3, 4, 32, 2, 1>()) ? rc : g.keys<float, 3, 4, 32, 2, 1>();
+        return (rc = g.queries<float, 3, 4, 32, 1>()) ? rc : g.keys<float, 3, 4, 32, 1>();
     if (db == 4)
-        return (rc = g.queries<float, 4, 4, 32, 2, 1>()) ? rc : g.keys<float, 4, 4, 32, 2, 1>();
-    if ((rc = g.queries<float, 8, 4, 32, 2, 1>()) || (rc = g.keys<float, 8, 4, 32, 2, 1, 1>()))
+        return (rc = g.queries<float, 4, 4, 32, 1>()) ? rc : g.keys<float, 4, 4, 32, 1>();
+    if ((rc = g.queries<float, 8, 4, 32, 1>()) || (rc = g.keys<float, 8, 4, 32, 1, 1>()))
         return rc;
-    return g.keys<float, 8, 4, 32, 2, 1, 2>(); // both results and both operands would not fit the registers
+    return g.keys<float, 8, 4, 32, 1, 2>(); // both results and both operands would not fit the registers
 }
 
 } // namespace sdp4
