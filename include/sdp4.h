@@ -500,7 +500,7 @@ int sdp4_rope_table(const double *inv_freq, int half, int64_t start, int64_t row
 typedef struct {
     int dtype;               /* of all heads */
     int head_dim;            /* SDP4_MIN_ATTENTION_DIM .. SDP4_MAX_ATTENTION_DIM */
-    float scale;             /* of the scores: > 0, finite */
+    float scale;             /* of the scores: 2^-40 .. 2^40 */
     const int64_t *offsets;  /* [sequences + 1] on the device, never falling, 0 .. tokens; NULL: one sequence of all tokens */
     int64_t sequences;
 } sdp4_attention_params;

@@ -16,7 +16,7 @@ using namespace sdp4::checks;
 int check_attention(const sdp4_attention_params *p, int64_t tokens)
 {
     if (!p || tokens < 0 || tokens > SDP4_MAX_TOKENS || !valid_dtype(p->dtype) || p->head_dim < SDP4_MIN_ATTENTION_DIM ||
-        p->head_dim > SDP4_MAX_ATTENTION_DIM || !(p->scale > 0.0f) || !std::isfinite(p->scale) ||
+        p->head_dim > SDP4_MAX_ATTENTION_DIM || !(p->scale >= 0x1p-40f && p->scale <= 0x1p40f) ||
         (p->offsets && (p->sequences < 0 || p->sequences > SDP4_MAX_TOKENS)))
         return SDP4_EINVAL;
     return aligned(p->offsets, 8) ? SDP4_OK : SDP4_EALIGN;

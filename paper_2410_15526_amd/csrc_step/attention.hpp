@@ -103,7 +103,15 @@ struct HeadTile {
 
 };
 
-// Where a lane finds its parts of the operands in a tile, computed once: an access adds a tile's address and a constant.
+// Where in LDS a lane finds its parts of the operands: addresses that are computed once and follow the tiles by move(); an
+// access adds a constant, which is the instruction's.  AT: bytes from where the addresses point to the tile.
+template <class V>
+SDP4_DEV V read_lds(uint32_t at)
+{
+    return *(__attribute__((address_space(3))) const V *)(uintptr_t)at;
+}
+SDP4_DEV uint32_t lds_address(const void *p) { return uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p); }
+
 template <class T, int DB>
 struct Reader;
 
@@ -111,32 +119,45 @@ template <int DB>
 struct Reader<bf16_t, DB> {
     using H = HeadTile<bf16_t, DB>;
     uint32_t in_row[H::STEPS], in_column[DB][2];
-    SDP4_DEV Reader()
+    SDP4_DEV explicit Reader(uint32_t base)
     {
         const int l = lane_id(), r = l & 31, h = l >> 5, i = l & 15;
 #pragma unroll
         for (int s = 0; s < H::STEPS; ++s)
-            in_row[s] = H::at(r, 2 * s + h);
+            in_row[s] = base + H::at(r, 2 * s + h);
         // a transposing read gives lane i of 16 element i of four rows, of which lane i points at a quarter of row i / 4
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int a = 0; a < 2; ++a)
-                in_column[db][a] = H::at(8 * a + 4 * h + (i >> 2), 4 * db + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 8 * (i & 1);
+                in_column[db][a] = base + H::at(8 * a + 4 * h + (i >> 2), 4 * db + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 8 * (i & 1);
+    }
+    SDP4_DEV void move(uint32_t by)
+    {
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+            in_row[s] += by;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+                in_column[db][a] += by;
     }
     // Operand with rows r0 + l % 32, elements 16 s + ... along the sum.
-    SDP4_DEV void rows(const char *tile, int r0, int s, Frag<bf16_t> &f) const
+    template <int AT>
+    SDP4_DEV void rows(int r0, int s, Frag<bf16_t> &f) const
     {
-        f.v = *reinterpret_cast<const bf16x8 *>(tile + in_row[s] + r0 * H::ROW);
+        f.v = read_lds<bf16x8>(in_row[s] + (AT + r0 * H::ROW));
     }
     // Operand with the tile's elements 32 db + l % 32 as rows and its rows r0 + 8 a + 4 h + b along the sum.
-    SDP4_DEV void columns(const char *tile, int r0, int db, Frag<bf16_t> &f) const
+    template <int AT>
+    SDP4_DEV void columns(int r0, int db, Frag<bf16_t> &f) const
     {
         s16x4 v[2];
 #pragma unroll
         for (int a = 0; a < 2; ++a)
             v[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(tile + in_column[db][a] + r0 * H::ROW));
+                (__attribute__((address_space(3))) s16x4 *)(uintptr_t)(in_column[db][a] + (AT + r0 * H::ROW)));
         f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -145,36 +166,95 @@ template <int DB>
 struct Reader<float, DB> {
     using H = HeadTile<float, DB>;
     uint32_t in_row[H::STEPS], in_column[8];
-    SDP4_DEV Reader()
+    SDP4_DEV explicit Reader(uint32_t base)
     {
         const int l = lane_id(), r = l & 31, h = l >> 5;
 #pragma unroll
         for (int s = 0; s < H::STEPS; ++s)
-            in_row[s] = H::at(r, 4 * s + 2 * h);
+            in_row[s] = base + H::at(r, 4 * s + 2 * h); // tiles begin at multiples of 32 bytes, for the other half (^ 16)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            in_column[j] = H::at(8 * (j >> 2) + 4 * h + (j & 3), r >> 2) % (H::ROW * 16) + 4 * (r & 3);
+            in_column[j] = base + H::at(8 * (j >> 2) + 4 * h + (j & 3), r >> 2) + 4 * (r & 3);
     }
-    SDP4_DEV void rows(const char *tile, int r0, int s, Frag<float> &f) const
+    SDP4_DEV void move(uint32_t by)
     {
-        const u32x4 a = *reinterpret_cast<const u32x4 *>(tile + in_row[s] + r0 * H::ROW);
-        const u32x4 b = *reinterpret_cast<const u32x4 *>(tile + (in_row[s] ^ 16) + r0 * H::ROW);
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+            in_row[s] += by;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            in_column[j] += by;
+    }
+    template <int AT>
+    SDP4_DEV void rows(int r0, int s, Frag<float> &f) const
+    {
+        const u32x4 a = read_lds<u32x4>(in_row[s] + (AT + r0 * H::ROW)), b = read_lds<u32x4>((in_row[s] ^ 16) + (AT + r0 * H::ROW));
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             f.v[j] = __uint_as_float(w[j]);
     }
-    SDP4_DEV void columns(const char *tile, int r0, int db, Frag<float> &f) const
+    template <int AT>
+    SDP4_DEV void columns(int r0, int db, Frag<float> &f) const
     {
 #pragma unroll
         for (int j = 0; j < 8; ++j) // in_column is element block 0's place: block db lies eight chunks a block away, twisted by bit 3
-            f.v[j] = *reinterpret_cast<const float *>(tile + in_column[j] + r0 * H::ROW +
-                                                      ((((8 * db) ^ ((j & 2) << 2)) - ((j & 2) << 2)) << 4));
+            f.v[j] = read_lds<float>(in_column[j] + (AT + r0 * H::ROW + ((((8 * db) ^ ((j & 2) << 2)) - ((j & 2) << 2)) << 4)));
     }
 };
 
-// Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile: load() starts them, store() has them
-// in the tile before the next barrier.  Rows from `limit` on hold other rows of the head: they are masked, and masked
+// The rows of a tile that stays where it is.
+template <class T, int DB>
+struct RowReader {
+    using H = HeadTile<T, DB>;
+    uint32_t in_row[H::STEPS];
+    SDP4_DEV explicit RowReader(uint32_t base)
+    {
+        const int r = lane_id() & 31, h = lane_id() >> 5;
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+            in_row[s] = base + H::at(r, sizeof(T) == 2 ? 2 * s + h : 4 * s + 2 * h);
+    }
+    template <int AT>
+    SDP4_DEV void rows(int s, Frag<T> &f) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            f.v = read_lds<bf16x8>(in_row[s] + AT);
+        } else {
+            const u32x4 a = read_lds<u32x4>(in_row[s] + AT), b = read_lds<u32x4>((in_row[s] ^ 16) + AT);
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                f.v[j] = __uint_as_float(w[j]);
+        }
+    }
+};
+// Puts a lane's fragment s of row l % 32 into a tile.
+template <class T, int DB>
+SDP4_DEV void put_row(char *tile, int s, const Frag<T> &f)
+{
+    using H = HeadTile<T, DB>;
+    const int r = lane_id() & 31, h = lane_id() >> 5;
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<bf16x8 *>(tile + H::at(r, 2 * s + h)) = f.v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<u32x4 *>(tile + H::at(r, 4 * s + 2 * h + i)) =
+                u32x4{__float_as_uint(f.v[4 * i]), __float_as_uint(f.v[4 * i + 1]), __float_as_uint(f.v[4 * i + 2]),
+                      __float_as_uint(f.v[4 * i + 3])};
+    }
+}
+
+// All but the N youngest loads of the wave have arrived.
+template <int N>
+SDP4_DEV void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile: load() starts them; after wait_loads()
+// and store() they are in the tile, for all waves from the next barrier on.  Rows from `limit` on hold other rows of the head: they are masked, and masked
 // rows may hold anything.  Elements from `dim` on meet zeros of the other operand.
 //
 // Straight into LDS, past the registers, where every row begins on 16 bytes and holds whole chunks: an instruction moves 64
@@ -205,7 +285,7 @@ struct TileLoad {
     SDP4_DEV void load(char *tile, int first, int limit)
     {
         const uint64_t base = uniform((uint64_t)(head + first * pitch));
-        const uint32_t at = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile + threadIdx.x / kWave * COUNT * 1024);
+        const uint32_t at = lds_address(tile) + uniform(threadIdx.x / kWave) * (COUNT * 1024);
         if (first + ROWS <= limit) {
 #pragma unroll
             for (int i = 0; i < COUNT; ++i)
@@ -218,21 +298,27 @@ struct TileLoad {
             }
         }
     }
-    // No register is written, so the compiler need not know that this is under way: store() waits for it.
+    // No register is written, so the compiler need not know that this is under way: wait_loads() sees to it.
     SDP4_DEV static void start(uint32_t at, uint32_t off, uint64_t base)
     {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory");
     }
-    SDP4_DEV void store(char *, int, int) const { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    SDP4_DEV void store(char *, int, int) const {}
 };
+
+// A number for each lane from its own address into LDS, as TileLoad does.
+SDP4_DEV void load_word(float *to, const float *from)
+{
+    const uint32_t at = lds_address(to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(at), "v"(from) : "memory");
+}
 
 // Through registers, for all other heads: a head's last chunk, where it is not whole, is read as the head's last whole one and
 // shifted.
 template <class T, int DB, int ROWS, int WAVES>
 struct TileLoad<T, DB, ROWS, WAVES, false> {
     using H = HeadTile<T, DB>;
-    static constexpr int THREADS = 64 * WAVES, COUNT = ROWS * H::USED / THREADS;
-    static_assert(COUNT * THREADS == ROWS * H::USED, "whole rounds");
+    static constexpr int THREADS = 64 * WAVES, CHUNKS = ROWS * H::USED, COUNT = (CHUNKS + THREADS - 1) / THREADS;
     u32x4 v[COUNT];
     const T *head;
     int64_t stride;
@@ -244,8 +330,8 @@ struct TileLoad<T, DB, ROWS, WAVES, false> {
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int id = i * THREADS + (int)threadIdx.x, r = id / H::USED, e = (id - r * H::USED) * H::N;
-            const int row = first + r < limit ? first + r : limit - 1;
+            const int place = i * THREADS + (int)threadIdx.x, id = place < CHUNKS ? place : 0;
+            const int r = id / H::USED, e = (id - r * H::USED) * H::N, row = first + r < limit ? first + r : limit - 1;
             v[i] = load_chunk<false>(head + row * stride + (e + H::N <= dim ? e : dim - H::N));
         }
     }
@@ -257,7 +343,8 @@ struct TileLoad<T, DB, ROWS, WAVES, false> {
             u32x4 w = v[i];
             if (dim % H::N)
                 w = e + H::N <= dim ? w : shifted(w, e + H::N - dim);
-            *reinterpret_cast<u32x4 *>(tile + H::at(r, e / H::N)) = e < dim ? w : u32x4{0, 0, 0, 0};
+            if (id < CHUNKS)
+                *reinterpret_cast<u32x4 *>(tile + H::at(r, e / H::N)) = e < dim ? w : u32x4{0, 0, 0, 0};
         }
     }
     SDP4_DEV static u32x4 shifted(u32x4 w, int by) // by elements toward the first, with zeros behind; by >= N is not used

@@ -14,14 +14,15 @@ namespace sdp4 {
 namespace {
 
 // WAVES waves of 32 rows each, BN keys at a time, STAGES tiles in LDS.
-template <class T, int DB, int WAVES, int BN, int OCC, bool DIRECT>
+template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Heads qh, Heads kh, Heads vh, Heads oh, float *lse,
                                                              int tiles, int64_t items)
 {
     using H = HeadTile<T, DB>;
     constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
-    __shared__ __align__(16) char kt[2][BN * H::ROW];
-    __shared__ __align__(16) char vt[2][BN * H::ROW];
+    constexpr int S = DIRECT ? STAGES : 2; // through registers there is one tile ahead
+    constexpr int TILE = BN * H::ROW;
+    __shared__ __align__(128) char tiles_lds[S][2][TILE]; // keys, values
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
@@ -67,26 +68,35 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
     bool poison = false;
     f32x16 o[DB] = {};
 
-    const Reader<T, DB> read;
     TileLoad<T, DB, BN, WAVES, DIRECT> kl, vl;
     kl.begin(kp, kh.token_stride, at.dim);
     vl.begin(vp, vh.token_stride, at.dim);
     // CAREFUL: infinities and NaN in masked places are kept from the product, where 0 times them would be NaN
     auto walk = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
-        kl.load(kt[0], first, last + 1);
-        vl.load(vt[0], first, last + 1);
-        int stage = 0;
-        for (int k0 = first; k0 <= last; k0 += BN) {
-            kl.store(kt[stage], k0, last + 1);
-            vl.store(vt[stage], k0, last + 1);
-            __syncthreads();
-            if (k0 + BN <= last) {
-                kl.load(kt[stage ^ 1], k0 + BN, last + 1);
-                vl.load(vt[stage ^ 1], k0 + BN, last + 1);
+        constexpr int PER = DIRECT ? kl.COUNT + vl.COUNT : 0;
+        Reader<T, DB> read(lds_address(tiles_lds[S - 1])); // the tile before the first
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (first + i * BN <= last) {
+                kl.load(tiles_lds[i][0], first + i * BN, last + 1);
+                vl.load(tiles_lds[i][1], first + i * BN, last + 1);
             }
-            const char *kb = kt[stage], *vb = vt[stage];
-            stage ^= 1;
+        int stage = 0, ahead = S - 1;
+        for (int k0 = first; k0 <= last; k0 += BN) {
+            if (k0 + (S - 2) * BN <= last)
+                wait_loads<(S - 2) * PER>(); // of the tiles after this one
+            else
+                wait_loads<0>();
+            kl.store(tiles_lds[stage][0], k0, last + 1);
+            vl.store(tiles_lds[stage][1], k0, last + 1);
+            __syncthreads();
+            if (k0 + (S - 1) * BN <= last) {
+                kl.load(tiles_lds[ahead][0], k0 + (S - 1) * BN, last + 1);
+                vl.load(tiles_lds[ahead][1], k0 + (S - 1) * BN, last + 1);
+            }
+            read.move(stage ? 2 * TILE : -(S - 1) * 2 * TILE);
+            stage = stage + 1 == S ? 0 : stage + 1, ahead = ahead + 1 == S ? 0 : ahead + 1;
             if (k0 > w_last || k0 + BN <= w_first)
                 continue;
             const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
@@ -97,7 +107,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     Frag<T> a;
-                    read.rows(kb, 32 * rb, s, a);
+                    read.template rows<0>(32 * rb, s, a);
                     mma(a, q[s], x[rb]);
                 }
             if (masked) {
@@ -155,8 +165,8 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
                     Frag<T> a;
-                    read.columns(vb, 16 * s, db, a);
-                    if (CAREFUL && masked)
+                    read.template columns<TILE>(16 * s, db, a);
+                    if (CAREFUL)
                         found |= tile_rows(scrub(a), 16 * s);
                     mma(a, p[s], o[db]);
                 }
@@ -206,13 +216,13 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
             : total == 0.0f ? -__builtin_inff() : total;
 }
 
-template <class T, int DB, int WAVES, int BN, int OCC>
+template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
 int run(int dtype, const Attention &at, const Heads &q, const Heads &k, const Heads &v, const Heads &out, float *lse, hipStream_t s)
 {
     const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
     const int64_t items = (int64_t)tiles * q.heads;
-    auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention<T, DB, WAVES, BN, OCC, true>
-                                                                       : k_attention<T, DB, WAVES, BN, OCC, false>;
+    auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention<T, DB, WAVES, BN, STAGES, OCC, true>
+                                                                       : k_attention<T, DB, WAVES, BN, STAGES, OCC, false>;
     return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, q, k, v, out, lse, tiles, items);
 }
 
@@ -224,20 +234,20 @@ int launch_attention(int dtype, const Attention &at, const Heads &q, const Heads
     const int db = (at.dim + 31) / 32;
     if (dtype == SDP4_BF16) {
         if (db <= 2)
-            return run<bf16_t, 2, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
+            return run<bf16_t, 2, 4, 64, 2, 2>(dtype, at, q, k, v, out, lse, s);
         if (db == 3)
-            return run<bf16_t, 3, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
+            return run<bf16_t, 3, 4, 64, 2, 2>(dtype, at, q, k, v, out, lse, s);
         if (db == 4)
-            return run<bf16_t, 4, 4, 64, 2>(dtype, at, q, k, v, out, lse, s);
-        return run<bf16_t, 8, 4, 32, 1>(dtype, at, q, k, v, out, lse, s);
+            return run<bf16_t, 4, 4, 64, 2, 2>(dtype, at, q, k, v, out, lse, s);
+        return run<bf16_t, 8, 4, 32, 2, 1>(dtype, at, q, k, v, out, lse, s);
     }
     if (db <= 2)
-        return run<float, 2, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
+        return run<float, 2, 4, 32, 2, 2>(dtype, at, q, k, v, out, lse, s);
     if (db == 3)
-        return run<float, 3, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
+        return run<float, 3, 4, 32, 2, 2>(dtype, at, q, k, v, out, lse, s);
     if (db == 4)
-        return run<float, 4, 4, 32, 2>(dtype, at, q, k, v, out, lse, s);
-    return run<float, 8, 4, 32, 1>(dtype, at, q, k, v, out, lse, s);
+        return run<float, 4, 4, 32, 2, 2>(dtype, at, q, k, v, out, lse, s);
+    return run<float, 8, 4, 32, 2, 1>(dtype, at, q, k, v, out, lse, s);
 }
 
 } // namespace sdp4

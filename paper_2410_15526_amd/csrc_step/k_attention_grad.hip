@@ -5,7 +5,8 @@
 //      dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,
 //      dv_j = sum_i p_ij dout_i,
 // the latter two summed over the query heads of a group.  Two launches: one
-// walks the keys for each block of queries and leaves D for the other, which
+// walks the keys for each block of queries and leaves what a row's scores and
+// dP need taken off for the other, which
 // walks the queries of all heads of the group for each block of keys.  The
 // scores are computed twice (seven products in place of five), which costs
 // less than adding dq up over the blocks of keys: each result is summed in
@@ -16,21 +17,25 @@ namespace sdp4 {
 
 namespace {
 
-// lse in octaves; +inf for a row without a finite score, so that its p are 0
-SDP4_DEV float octaves(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
-
-// p of scores x.  Of large scores the roundings of both sides may leave more than float32's exponents hold: p is at most 1
-// there (`large`: for some row of the wave).
-template <int N>
-SDP4_DEV void probabilities(f32x16 &x, float c, const float (&l)[N], bool large)
+// p of scores x, from exponents fma(x, c, add).  `hard`: some place is masked, where x and y may be anything, or some score is
+// large, whose roundings may leave more than float32's exponents hold: p is at most 1.  Place r is row `first` + 8 (r / 4) +
+// r % 4 of the other side, and `seen` rows from 0 on are seen.
+SDP4_DEV void probabilities(f32x16 &x, f32x16 &y, float c, float add, bool hard, uint32_t first, uint32_t seen)
 {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        float t = __builtin_fmaf(x[r], c, -l[r % N]);
-        if (large)
-            t = t > 0.0f && __builtin_fabsf(l[r % N]) >= kLargeScore ? 0.0f : t;
-        x[r] = exp2_of(t);
+    for (int r = 0; r < 16; ++r)
+        x[r] = __builtin_fmaf(x[r], c, add);
+    if (hard) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const bool on = first + (8 * (r >> 2) + (r & 3)) < seen;
+            x[r] = on ? x[r] > 0.0f ? 0.0f : x[r] : -__builtin_inff();
+            y[r] = on ? y[r] : 0.0f;
+        }
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        x[r] = exp2_of(x[r]);
 }
 
 template <class T>
@@ -47,15 +52,15 @@ SDP4_DEV void operands(const f32x16 &x, Frag<T> (&f)[2])
 }
 
 // out += tile's columns times p, for 32 rows of the tile from r0 on.  CAREFUL: what is infinite or NaN stays out and is noted.
-template <bool CAREFUL, class T, int DB>
-SDP4_DEV void add_product(const Reader<T, DB> &read, const char *tile, int r0, const Frag<T> (&p)[2], f32x16 (&out)[DB], uint64_t &found)
+template <int AT, bool CAREFUL, class T, int DB>
+SDP4_DEV void add_product(const Reader<T, DB> &read, int r0, const Frag<T> (&p)[2], f32x16 (&out)[DB], uint64_t &found)
 {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             Frag<T> a;
-            read.columns(tile, r0 + 16 * s, db, a);
+            read.template columns<AT>(r0 + 16 * s, db, a);
             if (CAREFUL)
                 found |= tile_rows(scrub(a), r0 + 16 * s);
             mma(a, p[s], out[db]);
@@ -81,6 +86,28 @@ SDP4_DEV void clear(f32x16 (&x)[DB])
         x[db] = f32x16{};
 }
 
+// Sums over the groups of waves, in their order, in group 0.
+template <int WAVES, int GROUPS, int DB>
+SDP4_DEV void join_groups(char *lds, int wave, int mine, f32x16 (&x)[DB])
+{
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+        f32x16 *part = reinterpret_cast<f32x16 *>(lds) + wave * DB * 64 + lane_id();
+        __syncthreads();
+        if (mine == g) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                part[db * 64] = x[db];
+        }
+        __syncthreads();
+        if (mine == 0) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                x[db] += part[db * 64];
+        }
+    }
+}
+
 template <class T, int DB>
 SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
 {
@@ -98,15 +125,16 @@ SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
         }
 }
 
-template <class T, int DB, int WAVES, int BN, int OCC, bool DIRECT>
+template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, Heads doh, Heads qh, Heads kh, Heads vh, Heads oh,
                                                                 const float *lse, Heads dqh, float *delta, int tiles,
                                                                 int64_t items)
 {
     using H = HeadTile<T, DB>;
     constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
-    __shared__ __align__(16) char kt[2][BN * H::ROW];
-    __shared__ __align__(16) char vt[2][BN * H::ROW];
+    constexpr int S = DIRECT ? STAGES : 2;
+    constexpr int TILE = BN * H::ROW;
+    __shared__ __align__(128) char tiles_lds[S][2][TILE]; // keys, values
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
@@ -155,37 +183,49 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
             along = __builtin_fmaf(g[s].get(j), o.get(j), along);
     }
     along += xor_lane<32>(along);
-    const int64_t stat = (int64_t)head * at.seq.tokens + at_row;
+    const int64_t at_stat = (int64_t)head * at.seq.tokens + at_row;
+    // What is added to scores and dP, for the other launch too: -lse / scale (-inf for a row without a finite score, so that its
+    // p are 0) and -D.
+    const float c = at.scale * kLog2e, row_lse = lse[at_stat];
+    const float shift = row_lse == -__builtin_inff() ? row_lse : -row_lse * (1.0f / at.scale);
     if (h == 0 && span.on)
-        delta[stat] = along;
-    const float c = at.scale * kLog2e, l[1] = {octaves(lse[stat])};
-    const bool large = __any(span.on && __builtin_fabsf(l[0]) >= kLargeScore);
+        delta[at_stat] = shift, delta[(int64_t)qh.heads * at.seq.tokens + at_stat] = -along;
+    const bool large = __any(span.on && __builtin_fabsf(shift) * c >= kLargeScore);
     const T *kp = static_cast<const T *>(kh.p) + kv * kh.head_stride, *vp = static_cast<const T *>(vh.p) + kv * vh.head_stride;
 
     bool poison = false;
     f32x16 dq[DB] = {};
-    const Reader<T, DB> read;
     TileLoad<T, DB, BN, WAVES, DIRECT> kl, vl;
     kl.begin(kp, kh.token_stride, at.dim);
     vl.begin(vp, vh.token_stride, at.dim);
     auto walk = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
-        kl.load(kt[0], first, last + 1);
-        vl.load(vt[0], first, last + 1);
-        int stage = 0;
-        for (int k0 = first; k0 <= last; k0 += BN) {
-            kl.store(kt[stage], k0, last + 1);
-            vl.store(vt[stage], k0, last + 1);
-            __syncthreads();
-            if (k0 + BN <= last) {
-                kl.load(kt[stage ^ 1], k0 + BN, last + 1);
-                vl.load(vt[stage ^ 1], k0 + BN, last + 1);
+        constexpr int PER = DIRECT ? kl.COUNT + vl.COUNT : 0;
+        Reader<T, DB> read(lds_address(tiles_lds[S - 1])); // the tile before the first
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (first + i * BN <= last) {
+                kl.load(tiles_lds[i][0], first + i * BN, last + 1);
+                vl.load(tiles_lds[i][1], first + i * BN, last + 1);
             }
-            const char *kb = kt[stage], *vb = vt[stage];
-            stage ^= 1;
+        int stage = 0, ahead = S - 1;
+        for (int k0 = first; k0 <= last; k0 += BN) {
+            if (k0 + (S - 2) * BN <= last)
+                wait_loads<(S - 2) * PER>(); // of the tiles after this one
+            else
+                wait_loads<0>();
+            kl.store(tiles_lds[stage][0], k0, last + 1);
+            vl.store(tiles_lds[stage][1], k0, last + 1);
+            __syncthreads();
+            if (k0 + (S - 1) * BN <= last) {
+                kl.load(tiles_lds[ahead][0], k0 + (S - 1) * BN, last + 1);
+                vl.load(tiles_lds[ahead][1], k0 + (S - 1) * BN, last + 1);
+            }
+            read.move(stage ? 2 * TILE : -(S - 1) * 2 * TILE);
+            stage = stage + 1 == S ? 0 : stage + 1, ahead = ahead + 1 == S ? 0 : ahead + 1;
             if (k0 > w_last || k0 + BN <= w_first)
                 continue;
-            const bool masked = !(k0 >= w_full && k0 + BN - 1 <= q0);
+            const bool hard = large || !(k0 >= w_full && k0 + BN - 1 <= q0);
             uint64_t found = 0;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
@@ -193,28 +233,18 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
 #pragma unroll
                 for (int s = 0; s < H::STEPS; ++s) {
                     Frag<T> a, b;
-                    read.rows(kb, 32 * rb, s, a);
-                    read.rows(vb, 32 * rb, s, b);
+                    read.template rows<0>(32 * rb, s, a);
+                    read.template rows<TILE>(32 * rb, s, b);
                     mma(a, q[s], x);
                     mma(b, g[s], y);
                 }
-                probabilities(x, c, l, large);
+                probabilities(x, y, c, shift * c, hard, k0 + 32 * rb + 4 * h - start, seen);
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     x[r] *= y[r] - along;
-                if (masked) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const uint32_t key = k0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                        x[r] = key - start < seen ? x[r] : 0.0f;
-                    }
-                }
                 Frag<T> p[2];
                 operands(x, p);
-                if (CAREFUL && masked)
-                    add_product<true>(read, kb, 32 * rb, p, dq, found);
-                else
-                    add_product<false>(read, kb, 32 * rb, p, dq, found);
+                add_product<0, CAREFUL>(read, 32 * rb, p, dq, found);
             }
             if (CAREFUL && __any(found != 0)) {
                 found = or_wave(found);
@@ -233,39 +263,48 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
                   poison ? __builtin_nanf("") : at.scale);
 }
 
-// Columns are keys here: a lane's key and value stay in registers as operands.  PARTS: 1 dv, 2 dk, 3 both.
-template <class T, int DB, int WAVES, int BQ, int OCC, bool DIRECT, int PARTS>
-__global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at, Heads doh, Heads qh, Heads kh, Heads vh,
-                                                                 const float *lse, Heads dkh, Heads dvh, const float *delta,
-                                                                 int tiles, int64_t items)
+// Columns are keys here, and a block's waves split them (32 to a wave) and the queries (GROUPS groups of waves take a tile's rows
+// in turn, their sums joined at the end in the order of the groups): two waves on a SIMD, whose results and operands have to fit
+// 256 registers each, so keys and values stay in LDS.  HELD: in registers, for one wave on a SIMD.  PARTS: 1 dv, 2 dk, 3 both.
+template <class T, int DB, int WAVES, int GROUPS, int STAGES, int OCC, bool DIRECT, int PARTS, bool HELD>
+__global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Attention at, Heads doh, Heads qh, Heads kh, Heads vh,
+                                                                          Heads dkh, Heads dvh, const float *delta, int tiles,
+                                                                          int64_t items)
 {
     using H = HeadTile<T, DB>;
-    constexpr int BK = 32 * WAVES, THREADS = 64 * WAVES, RB = BQ / 32;
+    constexpr int BK = 32 * WAVES, BQ = 32 * GROUPS, ALL = WAVES * GROUPS, S = DIRECT ? STAGES : 2;
     constexpr bool WITH_V = PARTS & 1, WITH_K = PARTS & 2;
-    __shared__ __align__(16) char qt[2][BQ * H::ROW];
-    __shared__ __align__(16) char gt[2][BQ * H::ROW];
-    __shared__ __align__(16) float lt[2][BQ], dt[2][BQ];
+    constexpr int TILE = BQ * H::ROW, KEYS = BK * H::ROW;
+    struct Lds {
+        char tiles[S][2][TILE]; // queries, gradients
+        char keys[HELD ? 16 : KEYS], values[WITH_K && !HELD ? KEYS : 16];
+    };
+    constexpr int JOIN = GROUPS > 1 ? WAVES * 64 * 64 * DB : 0; // one group's dk or dv
+    __shared__ __align__(128) char lds[sizeof(Lds) > JOIN ? sizeof(Lds) : JOIN];
+    Lds &mem = *reinterpret_cast<Lds *>(lds);
+    __shared__ __align__(16) float stats[S][ALL][64]; // what delta holds for 32 queries; each wave's own
     __shared__ int64_t samples[kSeqSamples];
-    __shared__ int edges[WAVES][2];
+    __shared__ int edges[ALL][2];
 
     const int64_t item = shared_item(work_block(), items);
     if (item >= items)
         return;
     const int kv = (int)(item / tiles), tile = (int)(item - (int64_t)kv * tiles);
 
-    const int wave = uniform(threadIdx.x / kWave), lane = lane_id(), h = lane >> 5;
+    const int all = uniform(threadIdx.x / kWave), wave = all % WAVES, mine = all / WAVES; // keys, and rows of a tile
+    const int lane = lane_id(), h = lane >> 5;
     const int key = tile * BK + 32 * wave + (lane & 31);
-    fill_samples<THREADS>(at.seq, samples);
+    fill_samples<64 * ALL>(at.seq, samples);
     const Span span = span_of(at.seq, samples, key);
     const int end = span.on ? span.end : -1;
     const int w_first = min_wave(span.on ? key : INT_MAX), w_end = max_wave(end); // queries that see the wave's keys
     const int w_all = max_wave(span.on ? key : INT_MAX), w_until = min_wave(end); // those that see all of them
     if (lane == 0)
-        edges[wave][0] = w_first, edges[wave][1] = w_end;
+        edges[all][0] = w_first, edges[all][1] = w_end;
     __syncthreads();
     int first = INT_MAX, limit = -1;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < ALL; ++w) {
         first = edges[w][0] < first ? edges[w][0] : first;
         limit = edges[w][1] > limit ? edges[w][1] : limit;
     }
@@ -276,118 +315,120 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at,
     const int64_t at_key = key < at.seq.tokens ? key : at.seq.tokens - 1;
     const T *krow = static_cast<const T *>(kh.p) + at_key * kh.token_stride + kv * kh.head_stride;
     const T *vrow = static_cast<const T *>(vh.p) + at_key * vh.token_stride + kv * vh.head_stride;
-    Frag<T> k[H::STEPS], v[WITH_K ? H::STEPS : 1];
+    Frag<T> k[HELD ? H::STEPS : 1], v[HELD && WITH_K ? H::STEPS : 1];
+    if constexpr (HELD) {
 #pragma unroll
-    for (int s = 0; s < H::STEPS; ++s) {
-        load_frag(krow, 16 * s + 8 * h, at.dim, k[s]);
-        if constexpr (WITH_K)
-            load_frag(vrow, 16 * s + 8 * h, at.dim, v[s]);
+        for (int s = 0; s < H::STEPS; ++s) {
+            load_frag(krow, 16 * s + 8 * h, at.dim, k[s]);
+            if constexpr (WITH_K)
+                load_frag(vrow, 16 * s + 8 * h, at.dim, v[s]);
+        }
+    } else { // into the tiles, a part by each of the groups
+#pragma unroll
+        for (int s = 0; s < H::STEPS; ++s)
+            if (s % GROUPS == mine) {
+                Frag<T> f;
+                load_frag(krow, 16 * s + 8 * h, at.dim, f);
+                put_row<T, DB>(mem.keys + 32 * wave * H::ROW, s, f);
+                if constexpr (WITH_K) {
+                    load_frag(vrow, 16 * s + 8 * h, at.dim, f);
+                    put_row<T, DB>(mem.values + 32 * wave * H::ROW, s, f);
+                }
+            }
     }
     const float c = at.scale * kLog2e;
     const int per_head = (limit - first + BQ - 1) / BQ;
     const int64_t count = (int64_t)per_head * at.group;
+    const uint32_t seen = span.on ? end - key : 0; // queries that see the key, from its own on
 
     bool poison_k = false, poison_v = false;
     f32x16 dk[WITH_K ? DB : 1] = {}, dv[WITH_V ? DB : 1] = {};
-    const Reader<T, DB> read;
-    TileLoad<T, DB, BQ, WAVES, DIRECT> ql, gl;
+    TileLoad<T, DB, BQ, ALL, DIRECT> ql, gl;
     ql.begin(nullptr, qh.token_stride, at.dim);
     gl.begin(nullptr, doh.token_stride, at.dim);
-    const uint32_t seen = span.on ? end - key : 0; // queries that see the key, from its own on
     auto walk = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
-        float stat = 0.0f; // threads 0 .. BQ - 1: lse, the next BQ: D
-        int nq = first, nhead = kv * at.group;
-        auto fetch = [&](int stage) {
+        constexpr int PER = DIRECT ? ql.COUNT + gl.COUNT + 1 : 0;
+        Reader<T, DB> read(lds_address(mem.tiles[S - 1]) + 32 * mine * H::ROW); // the tile before the first
+        RowReader<T, DB> fixed(lds_address(mem.keys) + 32 * wave * H::ROW); // the values lie behind
+        int nq = first, nhead = kv * at.group; // of the next load
+        auto fetch = [&](int to) {
             ql.move(static_cast<const T *>(qh.p) + nhead * qh.head_stride);
             gl.move(static_cast<const T *>(doh.p) + nhead * doh.head_stride);
-            ql.load(qt[stage], nq, limit);
-            gl.load(gt[stage], nq, limit);
-            if (threadIdx.x < 2 * BQ) {
-                const int r = nq + (threadIdx.x & (BQ - 1));
-                stat = (threadIdx.x < BQ ? lse : delta)[(int64_t)nhead * at.seq.tokens + (r < limit ? r : limit - 1)];
-            }
-        };
-        fetch(0);
-        int stage = 0;
-        for (int64_t i = 0; i < count; ++i) {
-            const int q0 = nq;
-            ql.store(qt[stage], q0, limit);
-            gl.store(gt[stage], q0, limit);
-            if (threadIdx.x < BQ)
-                lt[stage][threadIdx.x] = octaves(stat);
-            else if (threadIdx.x < 2 * BQ)
-                dt[stage][threadIdx.x - BQ] = stat;
-            __syncthreads();
+            ql.load(mem.tiles[to][0], nq, limit);
+            gl.load(mem.tiles[to][1], nq, limit);
+            const int r = nq + 32 * mine + (lane & 31);
+            load_word(stats[to][all], delta + ((int64_t)(lane < 32 ? nhead : nhead + qh.heads) * at.seq.tokens +
+                                               (r < limit ? r : limit - 1)));
             nq += BQ;
             if (nq >= limit)
                 nq = first, ++nhead;
-            if (i + 1 < count)
-                fetch(stage ^ 1);
-            const char *qb = qt[stage], *gb = gt[stage];
-            const float *lb = lt[stage], *db = dt[stage];
-            stage ^= 1;
-            if (q0 >= w_end || q0 + BQ <= w_first)
+        };
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (i < count)
+                fetch(i);
+        int stage = 0, ahead = S - 1, q0 = first + 32 * mine; // the wave's first row
+        for (int64_t i = 0; i < count; ++i, q0 = q0 - 32 * mine + BQ < limit ? q0 + BQ : first + 32 * mine) {
+            if (i + S - 2 < count)
+                wait_loads<(S - 2) * PER>(); // of the tiles after this one
+            else
+                wait_loads<0>();
+            ql.store(mem.tiles[stage][0], q0, limit);
+            gl.store(mem.tiles[stage][1], q0, limit);
+            __syncthreads();
+            if (i + S - 1 < count)
+                fetch(ahead);
+            read.move(stage ? 2 * TILE : -(S - 1) * 2 * TILE);
+            const float *stat = stats[stage][all];
+            stage = stage + 1 == S ? 0 : stage + 1, ahead = ahead + 1 == S ? 0 : ahead + 1;
+            if (q0 >= w_end || q0 + 32 <= w_first)
                 continue;
-            const bool masked = !(q0 >= w_all && q0 + BQ <= w_until);
-            uint64_t found_q = 0, found_g = 0;
+            const bool hard = !(q0 >= w_all && q0 + 32 <= w_until) || __any(__builtin_fabsf(stat[lane & 31]) * c >= kLargeScore);
+            f32x16 x, y = {}; // from -lse / scale and -D on
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                f32x16 x = {}, y = {};
+            for (int r = 0; r < 16; ++r) {
+                x[r] = stat[8 * (r >> 2) + 4 * h + (r & 3)];
+                if constexpr (WITH_K)
+                    y[r] = stat[32 + 8 * (r >> 2) + 4 * h + (r & 3)];
+            }
 #pragma unroll
-                for (int s = 0; s < H::STEPS; ++s) {
-                    Frag<T> a, b;
-                    read.rows(qb, 32 * rb, s, a);
-                    if constexpr (WITH_K)
-                        read.rows(gb, 32 * rb, s, b);
+            for (int s = 0; s < H::STEPS; ++s) {
+                Frag<T> a, b;
+                read.template rows<0>(0, s, a);
+                if constexpr (HELD) {
                     mma(a, k[s], x);
-                    if constexpr (WITH_K)
-                        mma(b, v[s], y);
-                }
-                float l[16];
-                bool large = false;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    l[r] = lb[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
-                    large |= __builtin_fabsf(l[r]) >= kLargeScore;
-                }
-                probabilities(x, c, l, __any(large));
-                if (masked) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const uint32_t q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                        x[r] = q - key < seen ? x[r] : 0.0f;
-                    }
-                }
-                Frag<T> p[2];
-                if constexpr (WITH_V) {
-                    operands(x, p);
-                    if (CAREFUL && masked)
-                        add_product<true>(read, gb, 32 * rb, p, dv, found_g);
-                    else
-                        add_product<false>(read, gb, 32 * rb, p, dv, found_g);
+                } else {
+                    fixed.template rows<0>(s, b);
+                    mma(a, b, x);
                 }
                 if constexpr (WITH_K) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        x[r] *= y[r] - db[32 * rb + 8 * (r >> 2) + 4 * h + (r & 3)];
-                    if (masked) { // y and D may be NaN in masked places
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const uint32_t q = q0 + 32 * rb + 8 * (r >> 2) + 4 * h + (r & 3);
-                            x[r] = q - key < seen ? x[r] : 0.0f;
-                        }
+                    read.template rows<TILE>(0, s, a);
+                    if constexpr (HELD) {
+                        mma(a, v[s], y);
+                    } else {
+                        fixed.template rows<KEYS>(s, b);
+                        mma(a, b, y);
                     }
-                    operands(x, p);
-                    if (CAREFUL && masked)
-                        add_product<true>(read, qb, 32 * rb, p, dk, found_q);
-                    else
-                        add_product<false>(read, qb, 32 * rb, p, dk, found_q);
                 }
+            }
+            probabilities(x, y, c, 0.0f, hard, q0 + 4 * h - key, seen);
+            uint64_t found_q = 0, found_g = 0;
+            Frag<T> p[2];
+            if constexpr (WITH_V) {
+                operands(x, p);
+                add_product<TILE, CAREFUL>(read, 0, p, dv, found_g);
+            }
+            if constexpr (WITH_K) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x[r] *= y[r];
+                operands(x, p);
+                add_product<0, CAREFUL>(read, 0, p, dk, found_q);
             }
             if (CAREFUL && __any((found_q | found_g) != 0)) {
                 found_q = or_wave(found_q), found_g = or_wave(found_g);
-                for (int j = 0; j < BQ; ++j) {
+                for (int j = 0; j < 32; ++j) {
                     const bool sees = (uint32_t)(q0 + j - key) < seen;
                     poison_k |= (found_q >> j & 1) && sees;
                     poison_v |= (found_g >> j & 1) && sees;
@@ -401,14 +442,22 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dkv(Attention at,
         clear(dv);
         walk(std::true_type{});
     }
-    if (!span.on)
+    if (poison_k) // the row's first element tells the others, and is joined with the other groups'
+        dk[0][0] = __builtin_nanf("");
+    if (poison_v)
+        dv[0][0] = __builtin_nanf("");
+    if constexpr (WITH_K)
+        join_groups<WAVES, GROUPS>(lds, wave, mine, dk);
+    if constexpr (WITH_V)
+        join_groups<WAVES, GROUPS>(lds, wave, mine, dv);
+    if (!span.on || mine)
         return;
     if constexpr (WITH_K)
         store_row(static_cast<T *>(dkh.p) + at_key * dkh.token_stride + kv * dkh.head_stride, at.dim, dk,
-                  poison_k ? __builtin_nanf("") : at.scale);
+                  dk[0][0] == dk[0][0] ? at.scale : dk[0][0]);
     if constexpr (WITH_V)
         store_row(static_cast<T *>(dvh.p) + at_key * dvh.token_stride + kv * dvh.head_stride, at.dim, dv,
-                  poison_v ? __builtin_nanf("") : 1.0f);
+                  dv[0][0] == dv[0][0] ? 1.0f : dv[0][0]);
 }
 
 struct Grad {
@@ -421,23 +470,24 @@ struct Grad {
 
     int dtype;
 
-    template <class T, int DB, int WAVES, int BN, int OCC>
+    template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
     int queries() const
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * q.heads;
-        auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention_dq<T, DB, WAVES, BN, OCC, true>
-                                                                           : k_attention_dq<T, DB, WAVES, BN, OCC, false>;
+        auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention_dq<T, DB, WAVES, BN, STAGES, OCC, true>
+                                                                           : k_attention_dq<T, DB, WAVES, BN, STAGES, OCC, false>;
         return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, out, lse, dq, delta, tiles, items);
     }
-    template <class T, int DB, int WAVES, int BQ, int OCC, int PARTS = 3>
+    template <class T, int DB, int WAVES, int GROUPS, int STAGES, int OCC, int PARTS = 3, bool HELD = false>
     int keys() const
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * k.heads;
-        auto kernel = direct(q, dtype, at.dim) && direct(dout, dtype, at.dim) ? k_attention_dkv<T, DB, WAVES, BQ, OCC, true, PARTS>
-                                                                             : k_attention_dkv<T, DB, WAVES, BQ, OCC, false, PARTS>;
-        return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, lse, dk, dv, delta, tiles, items);
+        auto kernel = direct(q, dtype, at.dim) && direct(dout, dtype, at.dim)
+                          ? k_attention_dkv<T, DB, WAVES, GROUPS, STAGES, OCC, true, PARTS, HELD>
+                          : k_attention_dkv<T, DB, WAVES, GROUPS, STAGES, OCC, false, PARTS, HELD>;
+        return launch<WAVES * GROUPS>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, dk, dv, delta, tiles, items);
     }
 };
 
@@ -445,7 +495,7 @@ struct Grad {
 
 int64_t attention_grad_workspace(int64_t tokens, int q_heads, int, int)
 {
-    return (tokens * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16;
+    return (2 * tokens * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; // -lse / scale and -D of every row
 }
 
 int launch_attention_grad(int dtype, const Attention &at, const Heads &dout, const Heads &q, const Heads &k, const Heads &v,
@@ -457,22 +507,25 @@ int launch_attention_grad(int dtype, const Attention &at, const Heads &dout, con
     int rc;
     if (dtype == SDP4_BF16) {
         if (db <= 2)
-            return (rc = g.queries<bf16_t, 2, 4, 64, 2>()) ? rc : g.keys<bf16_t, 2, 4, 32, 2>();
+            return (rc = g.queries<bf16_t, 2, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 2, 4, 2, 2, 2>();
         if (db == 3)
-            return (rc = g.queries<bf16_t, 3, 4, 64, 2>()) ? rc : g.keys<bf16_t, 3, 4, 64, 1>();
+            return (rc = g.queries<bf16_t, 3, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 3, 4, 2, 2, 2>();
         if (db == 4)
-            return (rc = g.queries<bf16_t, 4, 4, 64, 2>()) ? rc : g.keys<bf16_t, 4, 4, 32, 1>();
-        return (rc = g.queries<bf16_t, 8, 4, 32, 1>()) ? rc : g.keys<bf16_t, 8, 4, 32, 1>();
+            return (rc = g.queries<bf16_t, 4, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 4, 4, 2, 2, 2>();
+        // both results and both operands of such heads would not fit the registers
+        if ((rc = g.queries<bf16_t, 8, 4, 32, 2, 1>()) || (rc = g.keys<bf16_t, 8, 4, 1, 2, 1, 1, true>()))
+            return rc;
+        return g.keys<bf16_t, 8, 4, 1, 2, 1, 2, true>();
     }
     if (db <= 2)
-        return (rc = g.queries<float, 2, 4, 32, 1>()) ? rc : g.keys<float, 2, 4, 32, 1>();
+        return (rc = g.queries<float, 2, 4, 32, 2, 1>()) ? rc : g.keys<float, 2, 4, 1, 2, 1, 3, true>();
     if (db == 3)
-        return (rc = g.queries<float, 3, 4, 32, 1>()) ? rc : g.keys<float, 3, 4, 32, 1>();
+        return (rc = g.queries<float, 3, 4, 32, 2, 1>()) ? rc : g.keys<float, 3, 4, 1, 2, 1, 3, true>();
     if (db == 4)
-        return (rc = g.queries<float, 4, 4, 32, 1>()) ? rc : g.keys<float, 4, 4, 32, 1>();
-    if ((rc = g.queries<float, 8, 4, 32, 1>()) || (rc = g.keys<float, 8, 4, 32, 1, 1>()))
+        return (rc = g.queries<float, 4, 4, 32, 2, 1>()) ? rc : g.keys<float, 4, 4, 1, 2, 1, 3, true>();
+    if ((rc = g.queries<float, 8, 4, 32, 2, 1>()) || (rc = g.keys<float, 8, 4, 1, 2, 1, 1, true>()))
         return rc;
-    return g.keys<float, 8, 4, 32, 1, 2>(); // both results and both operands would not fit the registers
+    return g.keys<float, 8, 4, 1, 2, 1, 2, true>();
 }
 
 } // namespace sdp4
