@@ -518,11 +518,11 @@ int launch_attention_grad(int dtype, const Attention &at, const Heads &dout, con
         return g.keys<bf16_t, 8, 4, 1, 2, 1, 2, true>();
     }
     if (db <= 2)
-        return (rc = g.queries<float, 2, 4, 32, 2, 1>()) ? rc : g.keys<float, 2, 4, 1, 2, 1, 3, true>();
+        return (rc = g.queries<float, 2, 4, 32, 2, 1>()) ? rc : g.keys<float, 2, 2, 2, 2, 1, 3, true>();
     if (db == 3)
-        return (rc = g.queries<float, 3, 4, 32, 2, 1>()) ? rc : g.keys<float, 3, 4, 1, 2, 1, 3, true>();
+        return (rc = g.queries<float, 3, 4, 32, 2, 1>()) ? rc : g.keys<float, 3, 2, 2, 2, 1, 3, true>();
     if (db == 4)
-        return (rc = g.queries<float, 4, 4, 32, 2, 1>()) ? rc : g.keys<float, 4, 4, 1, 2, 1, 3, true>();
+        return (rc = g.queries<float, 4, 4, 32, 2, 1>()) ? rc : g.keys<float, 4, 2, 2, 2, 1, 3, true>();
     if ((rc = g.queries<float, 8, 4, 32, 2, 1>()) || (rc = g.keys<float, 8, 4, 1, 2, 1, 1, true>()))
         return rc;
     return g.keys<float, 8, 4, 1, 2, 1, 2, true>();
