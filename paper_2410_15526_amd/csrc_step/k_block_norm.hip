@@ -20,31 +20,44 @@ namespace {
 
 // Sums over a block's waves, the same in every lane: lanes, then waves in order through LDS (two places in turn, so that one
 // barrier a sum is enough).
-template <int WAVES, int COUNT>
+constexpr int kMostWaves = 8;
+template <int COUNT>
 struct BlockSums {
-    float (*lds)[WAVES][COUNT];
-    int turn = 0;
+    float (*lds)[COUNT][kMostWaves];
+    int waves, turn = 0;
+    SDP4_DEV BlockSums(float (*l)[COUNT][kMostWaves]) : lds(l), waves(blockDim.x / kWave)
+    {
+        for (int i = threadIdx.x; i < 2 * COUNT * kMostWaves; i += blockDim.x)
+            (&lds[0][0][0])[i] = 0.0f; // of the waves that are not there
+        __syncthreads();
+    }
     SDP4_DEV void add(float (&v)[COUNT])
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i)
             v[i] = sum_lanes(v[i], kWave);
-        if constexpr (WAVES > 1) {
-            if (lane_id() == 0) {
+        if (waves == 1)
+            return;
+        if (lane_id() == 0) {
 #pragma unroll
-                for (int i = 0; i < COUNT; ++i)
-                    lds[turn][threadIdx.x / kWave][i] = v[i];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) {
-                v[i] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w)
-                    v[i] += lds[turn][w][i];
-            }
-            turn ^= 1;
+            for (int i = 0; i < COUNT; ++i)
+                lds[turn][i][threadIdx.x / kWave] = v[i];
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            float w[kMostWaves];
+#pragma unroll
+            for (int j = 0; j < kMostWaves; ++j)
+                w[j] = lds[turn][i][j];
+#pragma unroll
+            for (int n = kMostWaves / 2; n > 0; n /= 2)
+#pragma unroll
+                for (int j = 0; j < n; ++j)
+                    w[j] += w[j + n];
+            v[i] = w[0];
+        }
+        turn ^= 1;
     }
 };
 
@@ -52,53 +65,116 @@ struct BlockSums {
 template <class X, class Y>
 constexpr int kJoint = sizeof(X) == 4 || sizeof(Y) == 4 ? 4 : 8;
 
-template <class T, int N, int C>
-SDP4_DEV void fetch(const T *row, int64_t cols, const int (&c)[C], Raw<T, N> (&r)[C])
-{
+// A lane's places in a row: C accesses of N elements.  WHOLE: the row is whole accesses, so that a place is in it or not;
+// otherwise the last one is read and written as load_row, end_row and store_elems do.
+template <int N, int C, bool WHOLE>
+struct Places {
+    int64_t cols;
+    int at[C];
+    SDP4_DEV explicit Places(int64_t n) : cols(n)
+    {
 #pragma unroll
-    for (int i = 0; i < C; ++i)
-        load_row(row, c[i], cols, r[i]);
-}
-template <class T, int N>
-SDP4_DEV void take(const Raw<T, N> &r, int c, int64_t cols, float (&v)[N])
-{
-    r.get(v);
-    end_row(c, cols, v);
-}
-template <class T, int N>
-SDP4_DEV void weight_at(const T *w, int c, int64_t cols, float (&v)[N])
-{
-    if (w) {
-        load_row(w, c, cols, v);
-        end_row(c, cols, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            v[j] = 1.0f;
+        for (int i = 0; i < C; ++i)
+            at[i] = N * (i * (int)blockDim.x + (int)threadIdx.x);
     }
-}
+    SDP4_DEV bool in(int i) const { return at[i] < (int)cols; }
+    template <class T>
+    SDP4_DEV void load(const T *row, Raw<T, N> (&r)[C]) const
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if constexpr (WHOLE)
+                r[i].template load<true>(row + (uint32_t)(in(i) ? at[i] : 0));
+            else
+                load_row(row, at[i], cols, r[i]);
+        }
+    }
+    template <class T>
+    SDP4_DEV void load_kept(const T *row, Raw<T, N> (&r)[C]) const // of weights, which every row reads again
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if constexpr (WHOLE)
+                r[i].template load<false>(row + (uint32_t)(in(i) ? at[i] : 0));
+            else
+                load_row(row, at[i], cols, r[i]);
+        }
+    }
+    // What was loaded, moved to its places where the row ends inside an access, with zeros beyond the row.
+    template <class T>
+    SDP4_DEV void settle(Raw<T, N> (&r)[C]) const
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (at[i] + N > (int)cols) {
+                float v[N];
+                if constexpr (WHOLE) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        v[j] = 0.0f;
+                } else {
+                    r[i].get(v);
+                    end_row(at[i], cols, v);
+                }
+                r[i].put(v); // the same numbers: as they came
+            }
+    }
+    template <class T>
+    SDP4_DEV void weight(const Raw<T, N> (&r)[C], bool there, int i, float (&v)[N]) const
+    {
+        if (there) {
+            r[i].get(v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[j] = 1.0f;
+        }
+    }
+    template <class T>
+    SDP4_DEV void store(T *row, int i, const float (&v)[N]) const
+    {
+        if constexpr (WHOLE) {
+            if (in(i)) {
+                Raw<T, N> r;
+                r.put(v);
+                r.store(row + (uint32_t)at[i]);
+            }
+        } else {
+            store_elems(row + at[i], cols - at[i], v);
+        }
+    }
+};
 
-// A block of WAVES waves for a row, C accesses of a lane.
-template <class X, class Y, int WAVES, int C>
-__global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t rows, int64_t cols, Rows<const X *> branch,
-                                                           Rows<const Y *> res, Rows<Y *> y, Rows<X *> h)
+// A block for a row.
+template <class X, class Y, int C, bool WHOLE>
+__global__ __launch_bounds__(64 * kMostWaves) void k_block_norm(BlockNorm p, int64_t rows, int64_t cols, Rows<const X *> branch,
+                                                                Rows<const Y *> res, Rows<Y *> y, Rows<X *> h)
 {
     constexpr int N = kJoint<X, Y>;
-    __shared__ float lds[2][WAVES][1];
-    BlockSums<WAVES, 1> sums{lds};
+    __shared__ __align__(16) float lds[2][1][kMostWaves];
     const int64_t row = work_block();
     if (row >= rows)
         return;
-    int c[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-        c[i] = N * (i * 64 * WAVES + (int)threadIdx.x);
-    Raw<X, N> br[C];
+    const Places<N, C, WHOLE> at(cols);
+    Raw<X, N> br[C], w1[C], w2[C];
     Raw<Y, N> rr[C];
     if (branch.p)
-        fetch(branch.p + row * branch.stride, cols, c, br);
+        at.load(branch.p + row * branch.stride, br);
     if (res.p)
-        fetch(res.p + row * res.stride, cols, c, rr);
+        at.load(res.p + row * res.stride, rr);
+    if (p.post_weight)
+        at.load_kept(static_cast<const X *>(p.post_weight), w1);
+    if (p.pre_weight)
+        at.load_kept(static_cast<const X *>(p.pre_weight), w2);
+    BlockSums<1> sums(lds);
+    if (branch.p)
+        at.settle(br);
+    if (res.p)
+        at.settle(rr);
+    if (p.post_weight)
+        at.settle(w1);
+    if (p.pre_weight)
+        at.settle(w2);
     float v[C][N];
     float by = p.branch_scale;
     if (p.gate)
@@ -107,7 +183,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t 
         float s[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            take(br[i], c[i], cols, v[i]);
+            br[i].get(v[i]);
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 s[0] = __builtin_fmaf(v[i][j], v[i][j], s[0]);
@@ -119,7 +195,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t 
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             float w[N];
-            weight_at(static_cast<const X *>(p.post_weight), c[i], cols, w);
+            at.weight(w1, p.post_weight, i, w);
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 v[i][j] = v[i][j] * w[j] * by;
@@ -135,7 +211,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t 
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             float w[N];
-            take(rr[i], c[i], cols, w);
+            rr[i].get(w);
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 v[i][j] = __builtin_fmaf(w[j], p.residual_scale, v[i][j]);
@@ -144,7 +220,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t 
     if (y.p) {
 #pragma unroll
         for (int i = 0; i < C; ++i)
-            store_elems(y.p + row * y.stride + c[i], cols - c[i], v[i]);
+            at.store(y.p + row * y.stride, i, v[i]);
     }
     if (h.p) {
         float s[1] = {0.0f};
@@ -158,169 +234,215 @@ __global__ __launch_bounds__(64 * WAVES) void k_block_norm(BlockNorm p, int64_t 
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             float w[N];
-            weight_at(static_cast<const X *>(p.pre_weight), c[i], cols, w);
+            at.weight(w2, p.pre_weight, i, w);
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 v[i][j] = v[i][j] * r * w[j];
-            store_elems(h.p + row * h.stride + c[i], cols - c[i], v[i]);
+            at.store(h.p + row * h.stride, i, v[i]);
         }
     }
 }
 
-// Rows part, part + parts, ... of a block; the weight gradients of its rows go to the workspace, from where the sums over the
-// parts are taken in order.
-template <class X, class Y, int WAVES, int C>
-__global__ __launch_bounds__(64 * WAVES) void k_block_norm_grad(BlockNorm p, int64_t rows, int64_t cols, int64_t pitch, int parts,
-                                                                BlockNormGrad<X, Y> g)
+// Rows part, part + parts, ... of a block, so that the chip's blocks walk through memory together; the next row's loads are under
+// way before the present one is stored.  The weight gradients of a block's rows go to the workspace, from where the sums over the
+// parts are taken in order.  JOINT: the sums with the branch are wanted, for a post norm or the gate's gradient.
+template <class X, class Y, int C, bool WHOLE, bool JOINT>
+__global__ __launch_bounds__(64 * kMostWaves) void k_block_norm_grad(BlockNorm p, int64_t rows, int64_t cols, int64_t pitch, int parts,
+                                                                     BlockNormGrad<X, Y> g)
 {
     constexpr int N = kJoint<X, Y>;
-    __shared__ float lds[2][WAVES][3];
-    BlockSums<WAVES, 3> sums{lds};
+    constexpr int SUMS = JOINT ? 6 : 2;
+    __shared__ __align__(16) float lds[2][SUMS][kMostWaves];
     const int64_t part = work_block();
     if (part >= parts)
         return;
-    int c[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-        c[i] = N * (i * 64 * WAVES + (int)threadIdx.x);
-    float dpost[C][N] = {}, dpre[C][N] = {};
-    for (int64_t row = part; row < rows; row += parts) {
-        Raw<X, N> dhr[C], br[C];
-        Raw<Y, N> dyr[C], yr[C];
+    const Places<N, C, WHOLE> at(cols);
+    // a row as it lies in memory: half the registers of its values where it is bfloat16
+    struct Row {
+        Raw<X, N> dh[C], b[C];
+        Raw<Y, N> dy[C], y[C];
+        float gate;
+    };
+    auto fetch = [&](int64_t row, Row &r) {
         if (g.dh.p) {
-            fetch(g.dh.p + row * g.dh.stride, cols, c, dhr);
-            fetch(g.y.p + row * g.y.stride, cols, c, yr);
+            at.load(g.dh.p + row * g.dh.stride, r.dh);
+            at.load(g.y.p + row * g.y.stride, r.y);
         }
-        if (g.dy.p)
-            fetch(g.dy.p + row * g.dy.stride, cols, c, dyr);
         if (g.branch.p)
-            fetch(g.branch.p + row * g.branch.stride, cols, c, br);
-        float t[C][N], b[C][N];
-        float s[3] = {0.0f, 0.0f, 0.0f}; // y^2, dh w_pre y, b^2
+            at.load(g.branch.p + row * g.branch.stride, r.b);
+        if (g.dy.p)
+            at.load(g.dy.p + row * g.dy.stride, r.dy);
+        r.gate = p.gate ? p.gate[row] : 1.0f;
+    };
+    Row now, next;
+    fetch(part, now);
+    Raw<X, N> w1[C], w2[C];
+    if (p.post_weight)
+        at.load_kept(static_cast<const X *>(p.post_weight), w1);
+    if (p.pre_weight)
+        at.load_kept(static_cast<const X *>(p.pre_weight), w2);
+    BlockSums<SUMS> sums(lds);
+    if (p.post_weight)
+        at.settle(w1);
+    if (p.pre_weight)
+        at.settle(w2);
+    float dpost[C][N] = {}, dpre[C][N] = {};
+    const float over = 1.0f / (float)cols;
+    for (int64_t row = part; row < rows; row += parts) {
+        const float by = p.branch_scale * now.gate;
+        if (g.dh.p)
+            at.settle(now.dh), at.settle(now.y);
+        if (g.dy.p)
+            at.settle(now.dy);
+        if (g.branch.p)
+            at.settle(now.b);
+        // One round of sums a row: of y^2, g y, b^2 with g = dh w_pre, and of dy u, g u, y u with u = b w_post, of which the sum
+        // of t u is made.
+        float s[SUMS] = {};
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            if (g.dh.p) {
-                float y[N], w[N];
-                take(dhr[i], c[i], cols, t[i]);
-                take(yr[i], c[i], cols, y);
-                weight_at(static_cast<const X *>(p.pre_weight), c[i], cols, w);
+            float v[N], y[N], b[N], w[N];
+            if constexpr (JOINT) {
+                now.b[i].get(b);
+                at.weight(w1, p.post_weight, i, w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    s[0] = __builtin_fmaf(y[j], y[j], s[0]);
-                    s[1] = __builtin_fmaf(t[i][j] * w[j], y[j], s[1]);
+                    s[2] = __builtin_fmaf(b[j], b[j], s[2]);
+                    b[j] *= w[j];
+                }
+                if (g.dy.p) {
+                    now.dy[i].get(v);
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        s[3] = __builtin_fmaf(v[j], b[j], s[3]);
                 }
             }
-            if (g.branch.p) {
-                take(br[i], c[i], cols, b[i]);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    s[2] = __builtin_fmaf(b[i][j], b[i][j], s[2]);
-            }
-        }
-        sums.add(s);
-        const float ry = 1.0f / __builtin_sqrtf(s[0] / (float)cols + p.pre_eps);
-        const float along = s[1] / (float)cols * ry * ry;                     // of y, by which dh w_pre is shortened
-        const float rb = p.post_norm ? 1.0f / __builtin_sqrtf(s[2] / (float)cols + p.post_eps) : 1.0f;
-        const float gate = p.gate ? p.gate[row] : 1.0f, by = p.branch_scale * gate;
-        float q[3] = {0.0f, 0.0f, 0.0f}; // t u / r_b, and nothing else
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
             if (g.dh.p) {
-                float y[N], w[N];
-                take(yr[i], c[i], cols, y);
-                weight_at(static_cast<const X *>(p.pre_weight), c[i], cols, w);
+                now.dh[i].get(v);
+                now.y[i].get(y);
+                at.weight(w2, p.pre_weight, i, w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    dpre[i][j] = __builtin_fmaf(t[i][j], y[j] * ry, dpre[i][j]);
-                    t[i][j] = ry * (t[i][j] * w[j] - y[j] * along);
+                    v[j] *= w[j];
+                    s[0] = __builtin_fmaf(y[j], y[j], s[0]);
+                    s[1] = __builtin_fmaf(v[j], y[j], s[1]);
+                }
+                if constexpr (JOINT) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        s[4] = __builtin_fmaf(v[j], b[j], s[4]);
+                        s[5] = __builtin_fmaf(y[j], b[j], s[5]);
+                    }
+                }
+            }
+        }
+        if (row + parts < rows)
+            fetch(row + parts, next);
+        sums.add(s);
+        const float ry = 1.0f / __builtin_sqrtf(s[0] * over + p.pre_eps);
+        const float along = s[1] * over * ry * ry; // of y, by which g is shortened
+        float rb = 1.0f, mean = 0.0f;
+        if constexpr (JOINT) {
+            const float tu = g.dh.p ? s[3] + ry * (s[4] - along * s[5]) : s[3];
+            if (p.post_norm) {
+                rb = 1.0f / __builtin_sqrtf(s[2] * over + p.post_eps);
+                mean = by * tu * rb * rb * over;
+            }
+            if (g.dgate && threadIdx.x == 0)
+                g.dgate[row] = p.branch_scale * rb * tu;
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float t[N], w[N], b[N];
+            if (g.dh.p) {
+                float y[N];
+                now.dh[i].get(t);
+                now.y[i].get(y);
+                at.weight(w2, p.pre_weight, i, w);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    dpre[i][j] = __builtin_fmaf(t[j], y[j] * ry, dpre[i][j]);
+                    t[j] = ry * (t[j] * w[j] - y[j] * along);
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    t[i][j] = 0.0f;
+                    t[j] = 0.0f;
             }
             if (g.dy.p) {
                 float d[N];
-                take(dyr[i], c[i], cols, d);
+                now.dy[i].get(d);
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    t[i][j] += d[j];
+                    t[j] += d[j];
             }
             if (g.dres.p) {
                 float o[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    o[j] = t[i][j] * p.residual_scale;
-                store_elems(g.dres.p + row * g.dres.stride + c[i], cols - c[i], o);
+                    o[j] = t[j] * p.residual_scale;
+                at.store(g.dres.p + row * g.dres.stride, i, o);
             }
-            float w[N];
-            weight_at(static_cast<const X *>(p.post_weight), c[i], cols, w);
+            at.weight(w1, p.post_weight, i, w);
             if (g.branch.p) {
+                now.b[i].get(b);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    dpost[i][j] = __builtin_fmaf(t[i][j] * by, b[i][j] * rb, dpost[i][j]);
-                    q[0] = __builtin_fmaf(t[i][j] * w[j], b[i][j], q[0]);
-                }
+                for (int j = 0; j < N; ++j)
+                    dpost[i][j] = __builtin_fmaf(t[j] * by, b[j] * rb, dpost[i][j]);
             }
+            if (g.dbranch.p) {
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                t[i][j] *= w[j] * by;
-        }
-        float mean = 0.0f;
-        if (p.post_norm || g.dgate) {
-            sums.add(q);
-            if (g.dgate && threadIdx.x == 0)
-                g.dgate[row] = p.branch_scale * rb * q[0];
-            mean = p.post_norm ? by * q[0] * rb * rb / (float)cols : 0.0f;
-        }
-        if (g.dbranch.p) {
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                if (p.post_norm) {
+                for (int j = 0; j < N; ++j)
+                    t[j] *= w[j] * by;
+                if (JOINT && p.post_norm) {
 #pragma unroll
                     for (int j = 0; j < N; ++j)
-                        t[i][j] = rb * (t[i][j] - b[i][j] * mean);
+                        t[j] = rb * (t[j] - b[j] * mean);
                 }
-                store_elems(g.dbranch.p + row * g.dbranch.stride + c[i], cols - c[i], t[i]);
+                at.store(g.dbranch.p + row * g.dbranch.stride, i, t);
             }
         }
+        now = next;
     }
 #pragma unroll
     for (int i = 0; i < C; ++i)
+        if (at.in(i)) { // the pitch is a multiple of 8
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (c[i] + j < cols) {
+            for (int j = 0; j < N; j += 4) {
                 if (g.post_parts)
-                    g.post_parts[part * pitch + c[i] + j] = dpost[i][j];
+                    store_elems(g.post_parts + part * pitch + at.at[i] + j, 4, *reinterpret_cast<const float(*)[4]>(&dpost[i][j]));
                 if (g.pre_parts)
-                    g.pre_parts[part * pitch + c[i] + j] = dpre[i][j];
+                    store_elems(g.pre_parts + part * pitch + at.at[i] + j, 4, *reinterpret_cast<const float(*)[4]>(&dpre[i][j]));
             }
+        }
 }
 
-constexpr int kMostParts = 512;
+// 256 / 512 / 768 / 1024 parts: 8192 x 5120 bfloat16 100 / 105 / 109 / 113 us, 2047 x 4097 37 / 40 / 50 / 56: more blocks a
+// compute unit gain less than their partial sums cost.
+constexpr int kMostParts = 256;
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
 int parts_of(int64_t rows) { return (int)(rows < kMostParts ? rows : kMostParts); }
 
-// A body with the waves and accesses of rows of `places` accesses.
+// A body with the accesses of a lane for rows of `places` accesses (as few as eight waves leave), and whether they are whole.
 template <class F>
-int with_shape(int64_t places, F body)
+int with_shape(int64_t cols, int n, F body)
 {
     using std::integral_constant;
-    if (places <= 64)
-        return body(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    if (places <= 128)
-        return body(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-    if (places <= 256)
-        return body(integral_constant<int, 1>{}, integral_constant<int, 4>{});
-    if (places <= 512)
-        return body(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    if (places <= 768)
-        return body(integral_constant<int, 4>{}, integral_constant<int, 3>{});
-    if (places <= 1024)
-        return body(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-    if (places <= 2048)
-        return body(integral_constant<int, 8>{}, integral_constant<int, 4>{});
-    return body(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    const int64_t places = (cols + n - 1) / n;
+    auto waves = [&](int c) { return (int)((places + 64 * c - 1) / (64 * c)); };
+    auto with = [&](auto c) {
+        return cols % n == 0 ? body(c, integral_constant<bool, true>{}, waves(c)) : body(c, integral_constant<bool, false>{}, waves(c));
+    };
+    constexpr int most = 64 * kMostWaves;
+    if (places <= most)
+        return with(integral_constant<int, 1>{});
+    if (places <= 2 * most)
+        return with(integral_constant<int, 2>{});
+    if (places <= 3 * most)
+        return with(integral_constant<int, 3>{});
+    if (places <= 4 * most)
+        return with(integral_constant<int, 4>{});
+    return with(integral_constant<int, 8>{});
 }
 
 } // namespace
@@ -338,8 +460,8 @@ int launch_block_norm(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows
             using X = decltype(x_tag);
             using Y = decltype(y_tag);
             constexpr int N = kJoint<X, Y>;
-            return with_shape((cols + N - 1) / N, [&](auto waves, auto chunks) {
-                return launch<waves>(k_block_norm<X, Y, waves, chunks>, rows, kUncapped, s, p, rows, cols, typed<const X>(branch),
+            return with_shape(cols, N, [&](auto accesses, auto whole, int waves) {
+                return launch_waves(waves, k_block_norm<X, Y, accesses, whole>, rows, kUncapped, s, p, rows, cols, typed<const X>(branch),
                                      typed<const Y>(residual), typed<Y>(y), typed<X>(h));
             });
         });
@@ -359,8 +481,10 @@ int launch_block_norm_grad(int x_dtype, int y_dtype, const BlockNorm &p, int64_t
             constexpr int N = kJoint<X, Y>;
             const BlockNormGrad<X, Y> g{typed<const X>(a.dh), typed<const Y>(a.dy), typed<const X>(a.branch), typed<const Y>(a.y),
                                         typed<X>(a.dbranch), typed<Y>(a.dresidual), a.dgate, post, pre};
-            return with_shape((cols + N - 1) / N, [&](auto waves, auto chunks) {
-                return launch<waves>(k_block_norm_grad<X, Y, waves, chunks>, parts, kUncapped, s, p, rows, cols, pitch, parts, g);
+            return with_shape(cols, N, [&](auto accesses, auto whole, int waves) {
+                auto kernel = p.post_norm || a.dgate ? k_block_norm_grad<X, Y, accesses, whole, true>
+                                                     : k_block_norm_grad<X, Y, accesses, whole, false>;
+                return launch_waves(waves, kernel, parts, kUncapped, s, p, rows, cols, pitch, parts, g);
             });
         });
     });
