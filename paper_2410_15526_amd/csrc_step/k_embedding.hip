@@ -8,8 +8,8 @@
 //     in the other tiles;
 //  3. where each token's rows begin, by binary search, and the sums of runs of
 //     kRun sorted rows of one token;
-//  4. the table, every row written once: zeros, or the sum of its rows, whole
-//     runs of them from step 3.
+//  4. the table, every row written once: the sums, with whole runs from step
+//     3, and zeros elsewhere.
 // The rest is HBM's: dy is read once, the table written once.
 #include "step_device.hpp"
 
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void k_embedding(Tokens t, int64_t cols, float
 // ---------------------------------------------------------------------------
 // sorting
 // ---------------------------------------------------------------------------
-constexpr int kTileLog2 = 13, kTile = 1 << kTileLog2, kRun = 64;
+constexpr int kTileLog2 = 13, kTile = 1 << kTileLog2, kRun = 32;
 constexpr int kSortRows = 32, kSortThreads = 512, kShares = kSortThreads / kSortRows; // rows of a block; threads of a row
 
 // Tokens without a row of the table sort behind all others.
@@ -73,8 +73,16 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_tiles(Tokens t, int tile_
     if (first >= t.rows)
         return;
     const int size = 1 << tile_log2;
-    for (int i = threadIdx.x; i < size; i += kSortThreads)
-        all[i] = key_of(t, base + i);
+    for (int i = threadIdx.x; i < size; i += 4 * kSortThreads) {
+        uint32_t k[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            k[u] = key_of(t, base + i + u * kSortThreads);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * kSortThreads < size)
+                all[i + u * kSortThreads] = k[u];
+    }
     __syncthreads();
     const int mine = (int)(first - base), share = threadIdx.x / kSortRows, r = threadIdx.x % kSortRows;
     const uint32_t key = all[mine + r];
@@ -82,10 +90,12 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_tiles(Tokens t, int tile_
     const int each = size / kShares, a = share * each, b = a + each;
     int count = 0;
     const int before = b < mine ? b : mine, after = a > mine + kSortRows ? a : mine + kSortRows;
+#pragma unroll 8
     for (int j = a; j < before; j += 4) {
         const u32x4 k = *reinterpret_cast<const u32x4 *>(all + j);
         count += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
     }
+#pragma unroll 8
     for (int j = after; j < b; j += 4) {
         const u32x4 k = *reinterpret_cast<const u32x4 *>(all + j);
         count += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
@@ -141,28 +151,39 @@ __global__ __launch_bounds__(256) void k_merge_tiles(int64_t rows, const uint32_
 // ---------------------------------------------------------------------------
 // sums
 // ---------------------------------------------------------------------------
-// Adds rows order[a .. b) of dy (scaled) to v, in order: a wave, the same rows in all lanes, eight loads under way.
-template <class X, int N>
-SDP4_DEV void add_rows(const Rows<const X *> &dy, const uint32_t *order, int64_t a, int64_t b, int64_t c, int64_t cols, float (&v)[N])
+// Adds U rows of dy to v, in order: a wave, the same rows in all lanes, A accesses of each.  row(u) names them.
+template <int U, class X, int N, int A, class F>
+SDP4_DEV void add_batch(const Rows<const X *> &dy, F row, const int (&c)[A], int64_t cols, float (&v)[A][N])
 {
-    constexpr int U = 8;
-    for (int64_t i = a; i < b; i += U) {
-        Raw<X, N> r[U];
+    Raw<X, N> r[U][A];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t row = uniform(order[i + u < b ? i + u : b - 1]);
-            load_row(dy.p + (int64_t)row * dy.stride, c, cols, r[u]);
-        }
+    for (int u = 0; u < U; ++u) {
+        const X *p = dy.p + (int64_t)uniform((uint32_t)row(u)) * dy.stride;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int k = 0; k < A; ++k)
+            load_row(p, c[k], cols, r[u][k]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
             float w[N];
-            r[u].get(w);
-            end_row(c, cols, w);
+            r[u][k].get(w);
+            end_row(c[k], cols, w);
 #pragma unroll
             for (int j = 0; j < N; ++j)
-                v[j] += i + u < b ? w[j] : 0.0f;
+                v[k][j] += w[j];
         }
-    }
+}
+// `count` rows: as many at a time as there are, up to U.
+template <int U, class X, int N, int A, class F>
+SDP4_DEV void add_rows(const Rows<const X *> &dy, int64_t count, F row, const int (&c)[A], int64_t cols, float (&v)[A][N])
+{
+    int64_t i = 0;
+    for (; i + U <= count; i += U)
+        add_batch<U>(dy, [&](int u) { return row(i + u); }, c, cols, v);
+    if constexpr (U > 1)
+        add_rows<U / 2>(dy, count - i, [&](int64_t u) { return row(i + u); }, c, cols, v);
 }
 
 template <int N>
@@ -183,83 +204,139 @@ template <class X, int N>
 __global__ __launch_bounds__(256) void k_runs(Tokens t, int64_t cols, Rows<const X *> dy, const uint32_t *keys, const uint32_t *order,
                                               int64_t token_blocks, uint32_t *starts, int64_t col_parts, int64_t pitch, float *runs)
 {
+    constexpr int SAMPLES = 1024; // every so many sorted tokens: most steps of a search are made in LDS
+    __shared__ uint32_t samples[SAMPLES];
     const int64_t block = work_block();
     if (block < token_blocks) {
+        const int64_t step = (t.rows + SAMPLES - 1) / SAMPLES;
+#pragma unroll
+        for (int i = 0; i < SAMPLES / 256; ++i) {
+            const int k = i * 256 + threadIdx.x;
+            samples[k] = k * step < t.rows ? keys[k * step] : ~0u;
+        }
+        __syncthreads();
         const int64_t v = block * 256 + threadIdx.x;
-        if (v <= t.vocab)
-            starts[v] = (uint32_t)count_below<false>(keys, t.rows, (uint32_t)v);
+        if (v > t.vocab)
+            return;
+        const int64_t behind = count_below<false>(samples, SAMPLES, (uint32_t)v); // the first sample that is not below
+        const int64_t from = behind ? (behind - 1) * step + 1 : 0, to = behind * step < t.rows ? behind * step : t.rows;
+        starts[v] = (uint32_t)(from < to ? from + count_below<false>(keys + from, to - from, (uint32_t)v) : to);
         return;
     }
     const int64_t w = (block - token_blocks) * 4 + uniform(threadIdx.x / kWave), run = w / col_parts, part = w - run * col_parts;
     const int64_t a = run * kRun;
     if (a + kRun > t.rows || keys[a] != keys[a + kRun - 1] || keys[a] >= (uint32_t)t.vocab)
         return;
-    const int64_t c = N * (part * kWave + lane_id());
-    float v[N] = {};
-    add_rows(dy, order, a, a + kRun, c < cols ? c : 0, cols, v);
-    if (c < cols) {
+    const int place = N * ((int)part * kWave + lane_id()), c[1] = {place < cols ? place : 0};
+    float v[1][N] = {};
+    add_rows<8>(dy, kRun, [&](int64_t i) { return order[a + i]; }, c, cols, v);
+    if (place < cols) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            runs[run * pitch + c + j] = v[j];
+            runs[run * pitch + place + j] = v[0][j];
     }
 }
 
-// A wave for 64 accesses of a table row, or (ADD) of the row of a sorted position where its token's rows begin.
+// Two kinds of blocks, evenly mixed (`sums` of `blocks` are of the first), so that the trips to memory of the one run beside the
+// other's stores.  A wave of the first kind takes 64 or 128 accesses of the row of a sorted position: where a token's rows begin,
+// their sum goes to the table (ADD: onto what it holds).  A wave of the second writes zeros, kZeros accesses of the
+// table in order, where a row has no token.
+//
+// 8192 x 5120 bfloat16 into 50000 float32 rows, all launches: 234 us, of which zeros alone take 165 (a fill 156).  One kind of
+// wave for a part of each table row 335, sums in front of all zeros 325, sums that look their rows up in three trips 305.
+constexpr int kZeros = 4;
+template <bool ADD>
+constexpr int kWide = ADD ? 1 : 2;
 template <class X, class Y, bool ADD>
 __global__ __launch_bounds__(256) void k_table(Tokens t, int64_t cols, float scale, Rows<const X *> dy, const uint32_t *keys,
                                                const uint32_t *order, const uint32_t *starts, int64_t pitch, const float *runs,
-                                               Divisor per_row, int64_t waves, Rows<Y *> table)
+                                               Divisor wide_parts, Divisor parts, int64_t sums, Divisor blocks, Rows<Y *> table)
 {
-    constexpr int N = kEmbed<X, Y>;
-    const int64_t w = work_block() * 4 + uniform(threadIdx.x / kWave);
-    if (w >= waves)
+    constexpr int N = kEmbed<X, Y>, W = kWide<ADD>, U = 8 / W; // U rows of W accesses under way
+    const int64_t block = work_block();
+    if (block >= (int64_t)blocks.d)
         return;
+    uint64_t rest;
+    const int64_t before = (int64_t)divide((uint64_t)block * (uint64_t)sums, blocks, rest); // blocks of the first kind so far
+    const int wave = uniform(threadIdx.x / kWave);
     uint64_t part;
-    int64_t token = (int64_t)divide((uint64_t)w, per_row, part);
-    int64_t a, b;
-    if constexpr (ADD) {
-        a = token;
-        const uint32_t k = uniform(keys[a]);
-        if (k >= (uint32_t)t.vocab || (a > 0 && uniform(keys[a - 1]) == k))
+    if (rest + (uint64_t)sums < blocks.d) { // the next one counts as many
+        if (ADD)
             return;
-        token = k, b = uniform(starts[token + 1]);
-    } else {
-        a = uniform(starts[token]), b = uniform(starts[token + 1]);
-    }
-    const int64_t place = N * ((int64_t)part * kWave + lane_id()), c = place < cols ? place : 0;
-    float v[N] = {};
-    const int64_t whole = (a + kRun - 1) / kRun, behind = b / kRun; // whole runs of the token's rows
-    if (behind <= whole) {
-        add_rows(dy, order, a, b, c, cols, v);
-    } else {
-        add_rows(dy, order, a, whole * kRun, c, cols, v);
-        for (int64_t i = whole; i < behind; i += 8) {
-            float r[8][N];
+        const int64_t w = ((block - before) * 4 + wave) * kZeros;
+        int64_t token[kZeros], place[kZeros];
+        bool none[kZeros];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                load_sums(runs + (i + u < behind ? i + u : behind - 1) * pitch + c, r[u]);
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    v[j] += i + u < behind ? r[u][j] : 0.0f;
+        for (int k = 0; k < kZeros; ++k) {
+            token[k] = (int64_t)divide((uint64_t)(w + k), parts, part);
+            place[k] = N * ((int64_t)part * kWave + lane_id());
+            none[k] = false;
+            if (token[k] < t.vocab)
+                none[k] = starts[token[k]] == starts[token[k] + 1];
         }
-        add_rows(dy, order, behind * kRun, b, c, cols, v);
-    }
-    Y *row = table.p + token * table.stride;
-    if constexpr (ADD) {
-        float before[N];
-        load_row(row, c, cols, before);
-        end_row(c, cols, before);
+        const float zeros[N] = {};
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            v[j] = __builtin_fmaf(v[j], scale, before[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            v[j] *= scale;
+        for (int k = 0; k < kZeros; ++k)
+            if (none[k])
+                store_elems(table.p + token[k] * table.stride + place[k], cols - place[k], zeros);
+        return;
     }
-    store_elems(row + place, cols - place, v);
+    const int64_t a = (int64_t)divide((uint64_t)(before * 4 + wave), wide_parts, part);
+    if (a >= t.rows)
+        return;
+    // the next 64 sorted rows, a lane each: what most tokens need, in one trip to memory
+    const int64_t mine = a + lane_id() < t.rows ? a + lane_id() : t.rows - 1;
+    const uint32_t key = keys[mine], row_of = order[mine], last = keys[a > 0 ? a - 1 : 0];
+    const uint32_t token = uniform(key);
+    if (token >= (uint32_t)t.vocab || (a > 0 && uniform(last) == token))
+        return;
+    int place[W], c[W];
+    float v[W][N] = {};
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        place[k] = N * (((int)part * W + k) * kWave + lane_id());
+        c[k] = place[k] < cols ? place[k] : 0;
+    }
+    const uint64_t others = ~__ballot(key == token && a + lane_id() < t.rows);
+    if (others) {
+        add_rows<U>(dy, __builtin_ctzll(others), [&](int64_t i) { return __builtin_amdgcn_readlane(row_of, (int)i); }, c, cols, v);
+    } else { // 64 rows or more: whole runs, and the rows before and behind them
+        const int64_t b = uniform(starts[token + 1]), whole = (a + kRun - 1) / kRun, behind = b / kRun;
+        add_rows<U>(dy, whole * kRun - a, [&](int64_t i) { return order[a + i]; }, c, cols, v);
+        for (int64_t i = whole; i < behind; i += U) {
+            float r[U][W][N];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    load_sums(runs + (i + u < behind ? i + u : behind - 1) * pitch + c[k], r[u][k]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        v[k][j] += i + u < behind ? r[u][k][j] : 0.0f;
+        }
+        add_rows<U>(dy, b - behind * kRun, [&](int64_t i) { return order[behind * kRun + i]; }, c, cols, v);
+    }
+    Y *row = table.p + (int64_t)token * table.stride;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        if constexpr (ADD) {
+            float held[N];
+            load_row(row, c[k], cols, held);
+            end_row(c[k], cols, held);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[k][j] = __builtin_fmaf(v[k][j], scale, held[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                v[k][j] *= scale;
+        }
+        store_elems(row + place[k], cols - place[k], v[k]);
+    }
 }
 
 // The workspace: sorted tokens and rows, the same before the tiles are merged, starts, sums of runs.
@@ -334,12 +411,15 @@ int launch_embedding_grad(const Tokens &t, int64_t cols, float scale, bool accum
                                at(l.order), token_blocks, at(l.starts), per_row, l.pitch, runs);
             if (rc)
                 return rc;
-            const int64_t waves = (accumulate ? t.rows : t.vocab) * per_row;
-            if (waves == 0)
+            const int64_t each = accumulate ? kWide<true> : kWide<false>, wide = (per_row + each - 1) / each;
+            const int64_t sums = (t.rows * wide + 3) / 4;
+            const int64_t blocks = sums + (accumulate ? 0 : (t.vocab * per_row + 4 * kZeros - 1) / (4 * kZeros));
+            if (blocks == 0)
                 return 0;
             auto k = accumulate ? k_table<X, Y, true> : k_table<X, Y, false>;
-            return launch<4>(k, (waves + 3) / 4, kUncapped, s, t, cols, scale, typed<const X>(dy), at(l.keys), at(l.order),
-                             at(l.starts), l.pitch, runs, Divisor((uint64_t)per_row), waves, typed<Y>(dtable));
+            return launch<4>(k, blocks, kUncapped, s, t, cols, scale, typed<const X>(dy), at(l.keys), at(l.order), at(l.starts),
+                             l.pitch, runs, Divisor((uint64_t)wide), Divisor((uint64_t)per_row), sums, Divisor((uint64_t)blocks),
+                             typed<Y>(dtable));
         });
     });
 }
