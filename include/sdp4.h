@@ -323,6 +323,7 @@ int sdp4_fill_f32(float *y, int64_t n, float value, void *stream);
 #define SDP4_MAX_ATTENTION_DIM 256
 #define SDP4_MAX_TOKENS ((int64_t)1 << 30)   /* rows of a packed batch; its sequences */
 #define SDP4_MAX_HIDDEN 16384                /* columns of a normed row */
+#define SDP4_MAX_GRAD_TOKENS ((int64_t)1 << 21) /* rows of one embedding gradient */
 
 /*
  * Bias, dropout and residual:
@@ -629,6 +630,7 @@ int sdp4_embedding(const int64_t *tokens, int64_t rows, const void *table, int t
  *   accumulate  0: the whole of dtable is written, rows of no token with zeros;
  *               else the sums are added to what dtable holds, and rows of no
  *               token are left alone
+ *   rows        0 .. SDP4_MAX_GRAD_TOKENS (more: in several calls that accumulate)
  *   dtable      [vocab][cols] dtable_dtype
  *   workspace   sdp4_embedding_grad_workspace() bytes, which serve any smaller
  *               number of rows too

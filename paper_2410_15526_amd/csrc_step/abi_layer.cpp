@@ -295,6 +295,7 @@ int sdp4_embedding_grad(const int64_t *tokens, int64_t rows, const void *dout, i
 {
     const Matrix d{dout, dout_dtype, dout_stride}, t{dtable, dtable_dtype, dtable_stride};
     if (!valid_dtype(dout_dtype) || !valid_dtype(dtable_dtype) || !valid_tokens(rows, vocab, cols, scale) ||
+        rows > SDP4_MAX_GRAD_TOKENS ||
         !valid_matrix(d, rows, cols) || !valid_matrix(t, vocab, cols))
         return SDP4_EINVAL;
     if (cols == 0 || (rows == 0 && accumulate))
@@ -316,7 +317,9 @@ int sdp4_embedding_grad(const int64_t *tokens, int64_t rows, const void *dout, i
 
 int64_t sdp4_embedding_grad_workspace(int64_t rows, int64_t vocab, int64_t cols)
 {
-    return valid_tokens(rows, vocab, cols, 1.0f) ? sdp4::embedding_grad_workspace(rows, vocab, cols) : -1;
+    return valid_tokens(rows, vocab, cols, 1.0f) && rows <= SDP4_MAX_GRAD_TOKENS
+               ? sdp4::embedding_grad_workspace(rows, vocab, cols)
+               : -1;
 }
 
 } // extern "C"

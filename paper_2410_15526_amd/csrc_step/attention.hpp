@@ -306,6 +306,37 @@ struct TileLoad {
     SDP4_DEV void store(char *, int, int) const {}
 };
 
+// A lane's row of a result, times `by`: four elements at a time, which meet their neighbours in the L2 cache.  (Stores past the
+// caches wrote 4.5 times the bytes: 8192 tokens, 40 heads of 128 bfloat16, 376 MB instead of 84, and 296 us instead of 275 among other calls.)
+template <class T, int DB>
+SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
+{
+    const int h = lane_id() >> 5;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int d = 32 * db + 8 * a + 4 * h;
+            float w[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                w[b] = o[db][4 * a + b] * by;
+            Raw<T, 4> r;
+            r.put(w);
+            if (d + 4 <= dim) {
+                if constexpr (sizeof(T) == 4)
+                    *reinterpret_cast<u32x4_b4 *>(row + d) = r.v;
+                else
+                    *reinterpret_cast<u32x2_b2 *>(row + d) = r.v;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (d + b < dim)
+                        row[d + b] = from_f32<T>(w[b]);
+            }
+        }
+}
+
 // A number for each lane from its own address into LDS, as TileLoad does.
 SDP4_DEV void load_word(float *to, const float *from)
 {

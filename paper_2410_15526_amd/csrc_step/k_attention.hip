@@ -198,18 +198,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
         return;
     // a row whose scores are all -inf: zeros
     const float inv = poison ? __builtin_nanf("") : total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-    T *orow = static_cast<T *>(oh.p) + (int64_t)row * oh.token_stride + head * oh.head_stride;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int d = 32 * db + 8 * a + 4 * h;
-            float w[4];
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-                w[b] = o[db][4 * a + b] * inv;
-            store_elems(orow + d, (int64_t)at.dim - d, w);
-        }
+    store_row(static_cast<T *>(oh.p) + (int64_t)row * oh.token_stride + head * oh.head_stride, at.dim, o, inv);
     if (lse && h == 0) // a small reference was taken as the rounded product
         lse[(int64_t)head * at.seq.tokens + row] =
             total > 0.0f ? (__builtin_fabsf(m * c) < kLargeScore ? (m * c + __log2f(total)) * kLn2 : m * at.scale + __logf(total))

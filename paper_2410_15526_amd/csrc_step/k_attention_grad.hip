@@ -108,23 +108,6 @@ SDP4_DEV void join_groups(char *lds, int wave, int mine, f32x16 (&x)[DB])
     }
 }
 
-template <class T, int DB>
-SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
-{
-    const int h = lane_id() >> 5;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int d = 32 * db + 8 * a + 4 * h;
-            float w[4];
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-                w[b] = o[db][4 * a + b] * by;
-            store_elems(row + d, (int64_t)dim - d, w);
-        }
-}
-
 template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, Heads doh, Heads qh, Heads kh, Heads vh, Heads oh,
                                                                 const float *lse, Heads dqh, float *delta, int tiles,

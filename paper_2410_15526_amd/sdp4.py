@@ -29,7 +29,7 @@ OK, EINVAL, EALIGN, ERANGE, EHIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
 MIN_GROUP, MAX_GROUP, MAX_HADAMARD, MAX_PEERS = 32, 4096, 1024, 16
 MAX_TOP, MAX_VOCAB, MAX_HEAD_DIM = 32, 1 << 20, 512
-MIN_ATTENTION_DIM, MAX_ATTENTION_DIM, MAX_TOKENS, MAX_HIDDEN = 8, 256, 1 << 30, 16384
+MIN_ATTENTION_DIM, MAX_ATTENTION_DIM, MAX_TOKENS, MAX_HIDDEN, MAX_GRAD_TOKENS = 8, 256, 1 << 30, 16384, 1 << 21
 
 
 class Sdp4Error(RuntimeError):

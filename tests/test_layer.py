@@ -77,7 +77,8 @@ def attention(q=(A, 512, 64, 4), k=(B, 512, 64, 2), v=(D, 512, 64, 2), out=(E, 2
 @pytest.mark.cpu_only
 @pytest.mark.parametrize("kw,want", [
     (dict(dt=2), EINVAL), (dict(dim=7), EINVAL), (dict(dim=257), EINVAL), (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL),
-    (dict(scale=math.inf), EINVAL), (dict(scale=math.nan), EINVAL), (dict(sequences=-1), EINVAL), (dict(sequences=1 << 31), EINVAL),
+    (dict(scale=math.inf), EINVAL), (dict(scale=math.nan), EINVAL), (dict(scale=2.0 ** -41), EINVAL), (dict(scale=2.0 ** 41), EINVAL),
+    (dict(sequences=-1), EINVAL), (dict(sequences=1 << 31), EINVAL),
     (dict(offsets=W + 4), EALIGN), (dict(tokens=-1), EINVAL), (dict(tokens=(1 << 30) + 1), EINVAL), (dict(q=None), EINVAL),
     (dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(out=None), EINVAL), (dict(q=(None, 512, 64, 4)), EINVAL),
     (dict(k=(B, 512, 64, 3), v=(D, 512, 64, 3)), EINVAL), (dict(v=(D, 512, 64, 4)), EINVAL), (dict(out=(E, 256, 64, 3)), EINVAL),
@@ -181,7 +182,7 @@ def embed_grad(t=A, rows=4, d=B, dt=0, ds=64, vocab=100, cols=64, scale=1.0, acc
 @pytest.mark.cpu_only
 @pytest.mark.parametrize("kw,want", [
     (dict(tt=2), EINVAL), (dict(dt=3), EINVAL), (dict(rows=-1), EINVAL), (dict(vocab=0), EINVAL), (dict(scale=math.nan), EINVAL),
-    (dict(ds=60), EINVAL), (dict(ts=60), EINVAL), (dict(t=None), EINVAL), (dict(d=None), EINVAL), (dict(tab=None), EINVAL),
+    (dict(rows=(1 << 21) + 1, nb=1 << 40), EINVAL), (dict(ds=60), EINVAL), (dict(ts=60), EINVAL), (dict(t=None), EINVAL), (dict(d=None), EINVAL), (dict(tab=None), EINVAL),
     (dict(t=A + 4), EALIGN), (dict(d=B + 2), EALIGN), (dict(tab=D + 2), EALIGN), (dict(ws=None), EINVAL), (dict(nb=16), EINVAL),
     (dict(ws=W + 8), EALIGN), (dict(tab=B), EINVAL), (dict(tab=A), EINVAL), (dict(ws=A), EINVAL), (dict(ws=B), EINVAL),
     (dict(ws=D), EINVAL), (dict(rows=0, acc=1), OK), (dict(cols=0), OK),
