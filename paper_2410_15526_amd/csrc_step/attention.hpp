@@ -516,6 +516,14 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // would otherwise move exponents by more than the 2^-12 that it is here: as much as the rounding of such a score itself.
 constexpr float kLargeScore = 4096.0f;
 
+// The value of lane ^ 32, without a trip through LDS.
+SDP4_DEV float other_half(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false); // (low, low) and (high, high)
+    return __uint_as_float(lane_id() < 32 ? both[1] : both[0]);
+}
+
 SDP4_DEV float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 } // namespace sdp4
