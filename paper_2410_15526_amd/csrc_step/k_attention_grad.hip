@@ -67,6 +67,19 @@ SDP4_DEV void add_product(const Reader<T, DB> &read, int r0, const Frag<T> (&p)[
         }
 }
 
+// The walk of a block in `count` pieces, each by a block of its own, whose results go to memory and are summed by k_join_pieces.
+struct Pieces {
+    static constexpr int kMost = 8;
+    int count;
+    float *parts; // [count][tokens][heads][pitch]
+    SDP4_DEV int64_t from(int piece, int64_t steps) const { return steps * piece / count; }
+    static SDP4_DEV int pitch(int dim) { return (dim + 3) / 4 * 4; }
+    SDP4_DEV float *row(int piece, const Attention &at, int64_t row, int head, int heads) const
+    {
+        return parts + (((int64_t)piece * at.seq.tokens + row) * heads + head) * pitch(at.dim);
+    }
+};
+
 template <int DB>
 SDP4_DEV bool has_nan(const f32x16 (&x)[DB])
 {
@@ -108,10 +121,12 @@ SDP4_DEV void join_groups(char *lds, int wave, int mine, f32x16 (&x)[DB])
     }
 }
 
+// Columns are queries, as in the forward pass, and the tiles are its tiles.  Four sequences of 2048, 40 heads of 128 over 8,
+// bfloat16: 320 us (three products: 800 TFLOP/s), 358 with eight waves a block.
 template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, Heads doh, Heads qh, Heads kh, Heads vh, Heads oh,
                                                                 const float *lse, Heads dqh, float *delta, int tiles,
-                                                                int64_t items)
+                                                                int64_t items, Pieces pieces)
 {
     using H = HeadTile<T, DB>;
     constexpr int BM = 32 * WAVES, THREADS = 64 * WAVES, RB = BN / 32;
@@ -121,9 +136,11 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
     __shared__ int64_t samples[kSeqSamples];
     __shared__ int edges[WAVES][2];
 
-    const int64_t item = shared_item(work_block(), items);
-    if (item >= items)
+    const int64_t unit = shared_item(work_block(), items * pieces.count);
+    if (unit >= items * pieces.count)
         return;
+    const int64_t item = unit / pieces.count;
+    const int piece = (int)(unit - item * pieces.count);
     const int64_t per_head = (int64_t)tiles * at.group;
     const int kv = (int)(item / per_head);
     const int64_t rest = item - kv * per_head;
@@ -148,6 +165,9 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
     if (last < 0)
         return;
     first = (int)uniform((uint32_t)first), last = (int)uniform((uint32_t)last);
+    const int steps = (last - first) / BN + 1, till = first + (int)pieces.from(piece + 1, steps) * BN - 1;
+    first += (int)pieces.from(piece, steps) * BN;
+    last = till < last ? till : last; // before first: nothing in this piece
 
     const int64_t at_row = row < at.seq.tokens ? row : at.seq.tokens - 1;
     const T *qrow = static_cast<const T *>(qh.p) + at_row * qh.token_stride + head * qh.head_stride;
@@ -171,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
     // p are 0) and -D.
     const float c = at.scale * kLog2e, row_lse = lse[at_stat];
     const float shift = row_lse == -__builtin_inff() ? row_lse : -row_lse * (1.0f / at.scale);
-    if (h == 0 && span.on)
+    if (h == 0 && span.on && piece == 0)
         delta[at_stat] = shift, delta[(int64_t)qh.heads * at.seq.tokens + at_stat] = -along;
     const bool large = __any(span.on && __builtin_fabsf(shift) * c >= kLargeScore);
     const T *kp = static_cast<const T *>(kh.p) + kv * kh.head_stride, *vp = static_cast<const T *>(vh.p) + kv * vh.head_stride;
@@ -241,18 +261,28 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
         clear(dq);
         walk(std::true_type{});
     }
-    if (span.on)
-        store_row(static_cast<T *>(dqh.p) + at_row * dqh.token_stride + head * dqh.head_stride, at.dim, dq,
-                  poison ? __builtin_nanf("") : at.scale);
+    if (!span.on)
+        return;
+    const float by = poison ? __builtin_nanf("") : at.scale;
+    if (pieces.count > 1)
+        store_row(pieces.row(piece, at, at_row, head, qh.heads), at.dim, dq, by);
+    else
+        store_row(static_cast<T *>(dqh.p) + at_row * dqh.token_stride + head * dqh.head_stride, at.dim, dq, by);
 }
 
 // Columns are keys here, and a block's waves split them (32 to a wave) and the queries (GROUPS groups of waves take a tile's rows
 // in turn, their sums joined at the end in the order of the groups): two waves on a SIMD, whose results and operands have to fit
 // 256 registers each, so keys and values stay in LDS.  HELD: in registers, for one wave on a SIMD.  PARTS: 1 dv, 2 dk, 3 both.
+//
+// The same heads: 404 us (four products: 850 TFLOP/s), tiles with the longest walks first.  Both launches together took 960 us when this form came, 1213 with HELD and
+// one wave on a SIMD, 1505 with launches of their own for dk and dv.  What bounds it: the fixed operands come out of LDS for each
+// tile again, and the two waves wait for p and dS.
+// float32 heads are HELD, as their operands are twice as large, with 64 keys a block, as a batch may have few: 1,871 rows, 12 heads
+// of 80 over 4, both launches 565 us, 913 with one group of four waves for 128 keys.
 template <class T, int DB, int WAVES, int GROUPS, int STAGES, int OCC, bool DIRECT, int PARTS, bool HELD>
 __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Attention at, Heads doh, Heads qh, Heads kh, Heads vh,
                                                                           Heads dkh, Heads dvh, const float *delta, int tiles,
-                                                                          int64_t items)
+                                                                          int64_t items, Pieces pieces)
 {
     using H = HeadTile<T, DB>;
     constexpr int BK = 32 * WAVES, BQ = 32 * GROUPS, ALL = WAVES * GROUPS, S = DIRECT ? STAGES : 2;
@@ -267,17 +297,20 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
     Lds &mem = *reinterpret_cast<Lds *>(lds);
     __shared__ __align__(16) float stats[S][ALL][64]; // what delta holds for 32 queries; each wave's own
     __shared__ int64_t samples[kSeqSamples];
-    __shared__ int edges[ALL][2];
+    __shared__ int edges[ALL][2], work[kMostOrdered], found_tile;
 
-    const int64_t item = shared_item(work_block(), items);
-    if (item >= items)
+    const int64_t unit = shared_item(work_block(), items * pieces.count);
+    if (unit >= items * pieces.count)
         return;
-    const int kv = (int)(item / tiles), tile = (int)(item - (int64_t)kv * tiles);
+    const int64_t item = unit / pieces.count;
+    const int piece = (int)(unit - item * pieces.count);
+    const int kv = (int)(item / tiles);
+    fill_samples<64 * ALL>(at.seq, samples);
+    const int tile = ordered_tile<64 * ALL, BK>(at.seq, samples, work, found_tile, tiles, (int)(item - (int64_t)kv * tiles));
 
     const int all = uniform(threadIdx.x / kWave), wave = all % WAVES, mine = all / WAVES; // keys, and rows of a tile
     const int lane = lane_id(), h = lane >> 5;
     const int key = tile * BK + 32 * wave + (lane & 31);
-    fill_samples<64 * ALL>(at.seq, samples);
     const Span span = span_of(at.seq, samples, key);
     const int end = span.on ? span.end : -1;
     const int w_first = min_wave(span.on ? key : INT_MAX), w_end = max_wave(end); // queries that see the wave's keys
@@ -321,7 +354,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
     }
     const float c = at.scale * kLog2e;
     const int per_head = (limit - first + BQ - 1) / BQ;
-    const int64_t count = (int64_t)per_head * at.group;
+    const int64_t steps = (int64_t)per_head * at.group, begin = pieces.from(piece, steps), count = pieces.from(piece + 1, steps);
     const uint32_t seen = span.on ? end - key : 0; // queries that see the key, from its own on
 
     bool poison_k = false, poison_v = false;
@@ -334,7 +367,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
         constexpr int PER = DIRECT ? ql.COUNT + gl.COUNT + 1 : 0;
         Reader<T, DB> read(lds_address(mem.tiles[S - 1]) + 32 * mine * H::ROW); // the tile before the first
         RowReader<T, DB> fixed(lds_address(mem.keys) + 32 * wave * H::ROW); // the values lie behind
-        int nq = first, nhead = kv * at.group; // of the next load
+        int nq = first + (int)(begin % per_head) * BQ, nhead = kv * at.group + (int)(begin / per_head); // of the next load
         auto fetch = [&](int to) {
             ql.move(static_cast<const T *>(qh.p) + nhead * qh.head_stride);
             gl.move(static_cast<const T *>(doh.p) + nhead * doh.head_stride);
@@ -347,12 +380,12 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
             if (nq >= limit)
                 nq = first, ++nhead;
         };
+        int stage = 0, ahead = S - 1, q0 = nq + 32 * mine; // the wave's first row
 #pragma unroll
         for (int i = 0; i < S - 1; ++i)
-            if (i < count)
+            if (begin + i < count)
                 fetch(i);
-        int stage = 0, ahead = S - 1, q0 = first + 32 * mine; // the wave's first row
-        for (int64_t i = 0; i < count; ++i, q0 = q0 - 32 * mine + BQ < limit ? q0 + BQ : first + 32 * mine) {
+        for (int64_t i = begin; i < count; ++i, q0 = q0 - 32 * mine + BQ < limit ? q0 + BQ : first + 32 * mine) {
             if (i + S - 2 < count)
                 wait_loads<(S - 2) * PER>(); // of the tiles after this one
             else
@@ -435,12 +468,84 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
         join_groups<WAVES, GROUPS>(lds, wave, mine, dv);
     if (!span.on || mine)
         return;
-    if constexpr (WITH_K)
-        store_row(static_cast<T *>(dkh.p) + at_key * dkh.token_stride + kv * dkh.head_stride, at.dim, dk,
-                  dk[0][0] == dk[0][0] ? at.scale : dk[0][0]);
-    if constexpr (WITH_V)
-        store_row(static_cast<T *>(dvh.p) + at_key * dvh.token_stride + kv * dvh.head_stride, at.dim, dv,
-                  dv[0][0] == dv[0][0] ? 1.0f : dv[0][0]);
+    if constexpr (WITH_K) {
+        const float by = dk[0][0] == dk[0][0] ? at.scale : dk[0][0];
+        if (pieces.count > 1)
+            store_row(pieces.row(piece, at, at_key, kv, dkh.heads), at.dim, dk, by);
+        else
+            store_row(static_cast<T *>(dkh.p) + at_key * dkh.token_stride + kv * dkh.head_stride, at.dim, dk, by);
+    }
+    if constexpr (WITH_V) {
+        const float by = dv[0][0] == dv[0][0] ? 1.0f : dv[0][0];
+        if (pieces.count > 1) // behind those of dk
+            store_row(pieces.row(pieces.count + piece, at, at_key, kv, dvh.heads), at.dim, dv, by);
+        else
+            store_row(static_cast<T *>(dvh.p) + at_key * dvh.token_stride + kv * dvh.head_stride, at.dim, dv, by);
+    }
+}
+
+// The sums over the pieces, in their order: a thread for four elements of a head.
+struct Joined {
+    Heads to;
+    const float *from; // [count][tokens][heads][pitch]
+    int count;
+};
+struct Joins {
+    Joined a[3];
+    int slots; // heads of all of them
+};
+template <class T>
+__global__ __launch_bounds__(256) void k_join_pieces(Attention at, Joins joins, int64_t threads)
+{
+    __shared__ int64_t samples[kSeqSamples];
+    fill_samples<256>(at.seq, samples);
+    const int64_t id = work_block() * 256 + threadIdx.x;
+    if (id >= threads)
+        return;
+    const int places = Pieces::pitch(at.dim) / 4;
+    const int64_t at_head = id / places, row = at_head / joins.slots;
+    const int d = 4 * (int)(id - at_head * places);
+    int head = (int)(at_head - row * joins.slots);
+    Joined j = joins.a[0];
+#pragma unroll
+    for (int i = 1; i < 3; ++i)
+        if (head >= j.to.heads)
+            head -= j.to.heads, j = joins.a[i];
+    if (!span_of(at.seq, samples, (int)row).on)
+        return;
+    const float *from = j.from + (row * j.to.heads + head) * Pieces::pitch(at.dim) + d;
+    const int64_t step = (int64_t)at.seq.tokens * j.to.heads * Pieces::pitch(at.dim);
+    float4 part[Pieces::kMost];
+#pragma unroll
+    for (int p = 0; p < Pieces::kMost; ++p)
+        part[p] = p < j.count ? *reinterpret_cast<const float4 *>(from + p * step) : float4{};
+    float4 sum = part[0];
+#pragma unroll
+    for (int p = 1; p < Pieces::kMost; ++p)
+        if (p < j.count)
+            sum.x += part[p].x, sum.y += part[p].y, sum.z += part[p].z, sum.w += part[p].w;
+    const float w[4] = {sum.x, sum.y, sum.z, sum.w};
+    T *to = static_cast<T *>(j.to.p) + row * j.to.token_stride + head * j.to.head_stride + d;
+    store_elems(to, at.dim - d, w);
+}
+
+// As many pieces as make kPieceBlocks blocks, of four steps at least: where a batch has fewer blocks than the chip has room for, its
+// longest walk would be the time.  1,871 rows of nine sequences, 12 float32 heads of 80 over 4 (dq and dkv, with the join's 12 us):
+// 184 and 360 us whole, 111 and 159 for 512 blocks, 129 and 140 (join 17) for 1024.  Four sequences of 2048, 40 heads of 128
+// over 8 in bfloat16 make 512 blocks by keys, and two pieces of each would add 38 us of partial sums.
+constexpr int64_t kPieceBlocks = 512, kPieceRows = 128 * kPieceBlocks;
+int pieces_of(int64_t blocks, int64_t steps)
+{
+    int64_t n = kPieceBlocks / blocks;
+    n = n < steps / 4 ? n : steps / 4;
+    return n < 2 ? 1 : n < Pieces::kMost ? (int)n : Pieces::kMost;
+}
+int64_t stat_floats(int64_t tokens, int q_heads) { return (2 * tokens * q_heads + 3) / 4 * 4; } // -lse / scale and -D of every row
+// Of pieces for any number of tokens up to this one: a block has 128 rows at most.
+int64_t piece_floats(int64_t tokens, int heads, int dim)
+{
+    const int64_t rows = Pieces::kMost * tokens * heads;
+    return (rows < kPieceRows ? rows : kPieceRows) * ((dim + 3) / 4 * 4);
 }
 
 struct Grad {
@@ -448,67 +553,110 @@ struct Grad {
     const Heads &dout, &q, &k, &v, &out;
     const float *lse;
     const Heads &dq, &dk, &dv;
-    float *delta;
+    float *delta, *parts_q, *parts_k;
     hipStream_t s;
 
     int dtype;
+    int pieces_q = 1, pieces_k = 1;
 
     template <class T, int DB, int WAVES, int BN, int STAGES, int OCC>
-    int queries() const
+    int queries()
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * q.heads;
+        pieces_q = pieces_of(items, (at.seq.tokens + BN - 1) / BN);
         auto kernel = direct(k, dtype, at.dim) && direct(v, dtype, at.dim) ? k_attention_dq<T, DB, WAVES, BN, STAGES, OCC, true>
                                                                            : k_attention_dq<T, DB, WAVES, BN, STAGES, OCC, false>;
-        return launch<WAVES>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, out, lse, dq, delta, tiles, items);
+        return launch<WAVES>(kernel, shared_blocks(items * pieces_q), kUncapped, s, at, dout, q, k, v, out, lse, dq, delta, tiles,
+                             items, Pieces{pieces_q, parts_q});
     }
     template <class T, int DB, int WAVES, int GROUPS, int STAGES, int OCC, int PARTS = 3, bool HELD = false>
-    int keys() const
+    int keys()
     {
         const int tiles = (at.seq.tokens + 32 * WAVES - 1) / (32 * WAVES);
         const int64_t items = (int64_t)tiles * k.heads;
+        pieces_k = pieces_of(items, (int64_t)((at.seq.tokens + 32 * GROUPS - 1) / (32 * GROUPS)) * at.group);
         auto kernel = direct(q, dtype, at.dim) && direct(dout, dtype, at.dim)
                           ? k_attention_dkv<T, DB, WAVES, GROUPS, STAGES, OCC, true, PARTS, HELD>
                           : k_attention_dkv<T, DB, WAVES, GROUPS, STAGES, OCC, false, PARTS, HELD>;
-        return launch<WAVES * GROUPS>(kernel, shared_blocks(items), kUncapped, s, at, dout, q, k, v, dk, dv, delta, tiles, items);
+        return launch<WAVES * GROUPS>(kernel, shared_blocks(items * pieces_k), kUncapped, s, at, dout, q, k, v, dk, dv, delta, tiles,
+                                      items, Pieces{pieces_k, parts_k});
     }
+    template <class T>
+    int join() const
+    {
+        Joins joins{};
+        int n = 0;
+        if (pieces_q > 1)
+            joins.a[n++] = {dq, parts_q, pieces_q};
+        const int64_t pitch = (at.dim + 3) / 4 * 4;
+        if (pieces_k > 1) {
+            joins.a[n++] = {dk, parts_k, pieces_k};
+            joins.a[n++] = {dv, parts_k + pieces_k * (int64_t)at.seq.tokens * k.heads * pitch, pieces_k};
+        }
+        for (const Joined &j : joins.a)
+            joins.slots += j.to.heads;
+        if (!joins.slots)
+            return 0;
+        const int64_t threads = (int64_t)at.seq.tokens * joins.slots * (pitch / 4);
+        return launch<4>(k_join_pieces<T>, (threads + 255) / 256, kUncapped, s, at, joins, threads);
+    }
+    // The launches by heads of up to 128 elements, and of more, where both results and both operands would not fit the registers.
+    template <class T>
+    int all();
 };
+
+template <>
+int Grad::all<bf16_t>()
+{
+    const int db = (at.dim + 31) / 32;
+    int rc;
+    if (db <= 2)
+        return (rc = queries<bf16_t, 2, 4, 64, 2, 2>()) ? rc : keys<bf16_t, 2, 4, 2, 2, 2>();
+    if (db == 3)
+        return (rc = queries<bf16_t, 3, 4, 64, 2, 2>()) ? rc : keys<bf16_t, 3, 4, 2, 2, 2>();
+    if (db == 4)
+        return (rc = queries<bf16_t, 4, 4, 64, 2, 2>()) ? rc : keys<bf16_t, 4, 4, 2, 2, 2>();
+    if ((rc = queries<bf16_t, 8, 4, 32, 2, 1>()) || (rc = keys<bf16_t, 8, 4, 1, 2, 1, 1, true>()))
+        return rc;
+    return keys<bf16_t, 8, 4, 1, 2, 1, 2, true>();
+}
+template <>
+int Grad::all<float>()
+{
+    const int db = (at.dim + 31) / 32;
+    int rc;
+    if (db <= 2)
+        return (rc = queries<float, 2, 4, 32, 2, 1>()) ? rc : keys<float, 2, 2, 2, 2, 1, 3, true>();
+    if (db == 3)
+        return (rc = queries<float, 3, 4, 32, 2, 1>()) ? rc : keys<float, 3, 2, 2, 2, 1, 3, true>();
+    if (db == 4)
+        return (rc = queries<float, 4, 4, 32, 2, 1>()) ? rc : keys<float, 4, 2, 2, 2, 1, 3, true>();
+    if ((rc = queries<float, 8, 4, 32, 2, 1>()) || (rc = keys<float, 8, 4, 1, 2, 1, 1, true>()))
+        return rc;
+    return keys<float, 8, 4, 1, 2, 1, 2, true>();
+}
 
 } // namespace
 
-int64_t attention_grad_workspace(int64_t tokens, int q_heads, int, int)
+int64_t attention_grad_workspace(int64_t tokens, int q_heads, int k_heads, int dim)
 {
-    return (2 * tokens * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; // -lse / scale and -D of every row
+    return (stat_floats(tokens, q_heads) + piece_floats(tokens, q_heads, dim) + 2 * piece_floats(tokens, k_heads, dim)) *
+           (int64_t)sizeof(float);
 }
 
 int launch_attention_grad(int dtype, const Attention &at, const Heads &dout, const Heads &q, const Heads &k, const Heads &v,
                           const Heads &out, const float *lse, const Heads &dq, const Heads &dk, const Heads &dv,
                           float *workspace, hipStream_t s)
 {
-    const Grad g{at, dout, q, k, v, out, lse, dq, dk, dv, workspace, s, dtype};
-    const int db = (at.dim + 31) / 32;
-    int rc;
-    if (dtype == SDP4_BF16) {
-        if (db <= 2)
-            return (rc = g.queries<bf16_t, 2, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 2, 4, 2, 2, 2>();
-        if (db == 3)
-            return (rc = g.queries<bf16_t, 3, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 3, 4, 2, 2, 2>();
-        if (db == 4)
-            return (rc = g.queries<bf16_t, 4, 4, 64, 2, 2>()) ? rc : g.keys<bf16_t, 4, 4, 2, 2, 2>();
-        // both results and both operands of such heads would not fit the registers
-        if ((rc = g.queries<bf16_t, 8, 4, 32, 2, 1>()) || (rc = g.keys<bf16_t, 8, 4, 1, 2, 1, 1, true>()))
-            return rc;
-        return g.keys<bf16_t, 8, 4, 1, 2, 1, 2, true>();
-    }
-    if (db <= 2)
-        return (rc = g.queries<float, 2, 4, 32, 2, 1>()) ? rc : g.keys<float, 2, 2, 2, 2, 1, 3, true>();
-    if (db == 3)
-        return (rc = g.queries<float, 3, 4, 32, 2, 1>()) ? rc : g.keys<float, 3, 2, 2, 2, 1, 3, true>();
-    if (db == 4)
-        return (rc = g.queries<float, 4, 4, 32, 2, 1>()) ? rc : g.keys<float, 4, 2, 2, 2, 1, 3, true>();
-    if ((rc = g.queries<float, 8, 4, 32, 2, 1>()) || (rc = g.keys<float, 8, 4, 1, 2, 1, 1, true>()))
-        return rc;
-    return g.keys<float, 8, 4, 1, 2, 1, 2, true>();
+    float *parts_q = workspace + stat_floats(at.seq.tokens, q.heads);
+    float *parts_k = parts_q + piece_floats(at.seq.tokens, q.heads, at.dim);
+    Grad g{at, dout, q, k, v, out, lse, dq, dk, dv, workspace, parts_q, parts_k, s, dtype};
+    return with_type(dtype, [&](auto tag) {
+        using T = decltype(tag);
+        const int rc = g.all<T>();
+        return rc ? rc : g.join<T>();
+    });
 }
 
 } // namespace sdp4

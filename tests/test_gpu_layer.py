@@ -129,6 +129,34 @@ def test_attention_of_long_sequences(dtype):
     assert all(t.equal(x, y) for x, y in zip(a, b))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hk,dim,layout", [(4, 2, 40, "dense"), (2, 2, 77, "odd"), (3, 1, 128, "heads"), (2, 1, 250, "dense")])
+def test_attention_gradient_in_pieces(hq, hk, dim, layout, dtype):
+    """Few blocks and long walks: several blocks share one, some of them with nothing to do."""
+    t = torch()
+    say("attention pieces", hq, hk, dim, layout, dtype)
+    lengths = [1, 900, 0, 3, 1100, 64]
+    c = Case(10, lengths, 7, hq, hk, dim, dtype, lead=2, layout=layout)
+    c.check()
+    clean = [x.clone() for x in c.backward()]
+    for buf, view in zip(c.bufs, (c.q, c.k, c.v)):
+        assert int((~t.isnan(buf)).sum()) == sum(lengths) * view.shape[1] * dim
+    for x, y in zip(clean, c.backward()):                    # the same bits again
+        assert t.equal(x[2:-7], y[2:-7])
+    at = 2 + 1 + 900 + 3 + 600                               # one value of the second long sequence, and what no row sees
+    for x in (c.q, c.k, c.v, c.dout):
+        x[at, :, dim // 2] = NAN
+        x[:2], x[-7:] = NAN, float("inf")
+    c.forward()
+    spoilt = [x.clone() for x in c.backward()]
+    first, last = at - 600, 2 + sum(lengths) - 64            # its sequence
+    for x, y in zip(clean, spoilt):
+        assert t.equal(x[2:first], y[2:first]) and t.equal(x[last:-7], y[last:-7])
+        assert bool(t.isnan(y[at]).all())
+    assert t.equal(clean[0][first:at], spoilt[0][first:at]) and bool(t.isnan(spoilt[0][at:last]).all())
+    assert all(bool(t.isnan(y[first:at]).all()) for y in spoilt[1:])
+
+
 @pytest.mark.parametrize("count", [255, 256, 257, 1000, 5000])
 def test_attention_of_many_sequences(count):
     r = np.random.default_rng(count)
