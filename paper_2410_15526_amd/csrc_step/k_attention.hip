@@ -35,11 +35,12 @@ SDP4_DEV void spread()
 // WAVES waves of 32 rows each, BN keys at a time, STAGES tiles in LDS.  The scores are computed transposed, keys by rows, so that
 // a lane holds one row's: its maximum and sum need one exchange, and p is the second product's operand as it lies.
 //
-// Four sequences of 2048, 40 heads of 128 over 8, bfloat16: 230 us, 747 TFLOP/s of the pairs that rows see (a library product of
-// 8192^3 reaches 1143); one sequence of 16384, 16 heads over 4: 1410 us, 780.  Neither memory nor either kind of unit alone is
-// the bound: two waves on a SIMD wait for their own scores, maxima and exponentials.  Two, since a row's results, queries and
-// scores take 224 registers; eight waves on a tile in place of four took 280 us where this took 248, 64
-// keys a tile halve the barriers and exchanges of 32 (265 and 295), and more tiles ahead change nothing: loads are not waited for.
+// Four sequences of 2048, 40 heads of 128 over 8, bfloat16: 230 to 247 us by card, 695 to 747 TFLOP/s of the pairs that rows
+// see (a library product of 8192^3 reaches 1143); one sequence of 16384, 16 heads over 4: 1436 us, 766.  Neither memory nor
+// either kind of unit alone is the bound: two waves on a SIMD wait for their own scores, maxima and exponentials.  Two, since a
+// row's results, queries and scores take 224 registers; eight waves on a tile in place of four took 280 us where this took 248,
+// 64 keys a tile halve the barriers and exchanges of 32 (265 and 295), and more tiles ahead change nothing: loads are not
+// waited for.
 // Heads of more than 128 take one wave on a SIMD and 32 keys, as their registers allow.
 template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Heads qh, Heads kh, Heads vh, Heads oh, float *lse,

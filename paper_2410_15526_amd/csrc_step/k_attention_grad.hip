@@ -10,7 +10,8 @@
 // walks the queries of all heads of the group for each block of keys.  The
 // scores are computed twice (seven products in place of five), which costs
 // less than adding dq up over the blocks of keys: each result is summed in
-// registers, in one order, and written once.
+// registers, in one order, and written once.  Where a batch makes few blocks,
+// their walks are split, and a third launch sums the parts in their order.
 #include "attention.hpp"
 
 namespace sdp4 {
