@@ -90,7 +90,9 @@ class Decoder:
             qkv = (h @ w["qkv"].t()).view(rows, 3 * c.heads, d)
             q, k = autograd.qk_norm_rope(qkv[:, :c.heads], qkv[:, c.heads:2 * c.heads], w["q_norm"], w["k_norm"], 1e-6,
                                          self.table, positions)
-            a = autograd.attention(q, k, qkv[:, 2 * c.heads:], sequences).view(rows, c.hidden)
+            # float32 heads: scores, probabilities and both products unrounded, one rounding of the result
+            q, k, v = (t.float() for t in (q, k, qkv[:, 2 * c.heads:]))
+            a = autograd.attention(q, k, v, sequences).to(x.dtype).view(rows, c.hidden)
             x, h = self.join(a @ w["out"].t(), w["out_bias"], w.get("attention_norm"), x, p, offset[0])
             u = torch.nn.functional.gelu(h @ w["up"].t())
             x, h = self.join(u @ w["down"].t(), w["down_bias"], w.get("mlp_norm"), x, p, offset[1])
