@@ -50,9 +50,9 @@ struct LaunchShape {
 };
 LaunchShape shape_for(const void *kernel, int64_t nwork_blocks, int cap, hipError_t &err);
 
-// Launch `kernel` with blocks of `waves` (or WAVES) wavefronts.
-template <typename... Params, typename... Args>
-int launch_waves(int waves, void (*kernel)(Params...), int64_t nwork_blocks, int cap, hipStream_t stream, Args... args)
+// Launch `kernel` with blocks of WAVES wavefronts.
+template <int WAVES, typename... Params, typename... Args>
+int launch(void (*kernel)(Params...), int64_t nwork_blocks, int cap, hipStream_t stream, Args... args)
 {
     hipError_t err;
     const LaunchShape sh = shape_for(reinterpret_cast<const void *>(kernel), nwork_blocks, cap, err);
@@ -64,16 +64,11 @@ int launch_waves(int waves, void (*kernel)(Params...), int64_t nwork_blocks, int
         int i = 0;
         ((argv[i++] = static_cast<void *>(&v)), ...);
     }, values);
-    err = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(sh.x, sh.y), dim3(64 * waves), argv,
+    err = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(sh.x, sh.y), dim3(64 * WAVES), argv,
                           sh.dyn_lds, stream);
     if (err != hipSuccess)
         return set_hip_error(err);
     return 0;
-}
-template <int WAVES, typename... Params, typename... Args>
-int launch(void (*kernel)(Params...), int64_t nwork_blocks, int cap, hipStream_t stream, Args... args)
-{
-    return launch_waves(WAVES, kernel, nwork_blocks, cap, stream, args...);
 }
 
 int launch_qwd_encode(const float *w_new, const void *w_prev, bool bf16, bool sym, int64_t n, int group,

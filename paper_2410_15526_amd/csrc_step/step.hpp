@@ -9,6 +9,16 @@
 
 namespace sdp4 {
 
+// launch() with a number of wavefronts known at run time: at least WAVES, at most eight.
+template <int WAVES = 1, typename... Params, typename... Args>
+int launch_waves(int waves, void (*kernel)(Params...), int64_t nwork_blocks, int cap, hipStream_t stream, Args... args)
+{
+    if constexpr (WAVES < 8)
+        if (waves > WAVES)
+            return launch_waves<WAVES + 1>(waves, kernel, nwork_blocks, cap, stream, args...);
+    return launch<WAVES>(kernel, nwork_blocks, cap, stream, args...);
+}
+
 // A two-dimensional array with unit stride in a row.
 template <class P>
 struct Rows {

@@ -140,3 +140,9 @@ def test_source_digest_leaves_out_the_marshalling_of_the_python_binding(tmp_path
     d0 = bench.source_digest()
     (csrc / "binding.cpp").write_text("x")
     assert bench.source_digest() == d0
+
+
+def test_recorded_traffic_is_of_these_kernels():
+    """The committed record serves the benchmark: it was taken on the kernel sources as they are."""
+    for kernel in ("qwd_encode", "qwd_decode", "grad_quant", "reduce_intra", "reduce_inter"):
+        assert bench.traffic_for(kernel)
