@@ -253,13 +253,16 @@ SDP4_DEV void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
+// A buffer of plain bytes from an address on, without a stride: offsets from kBufferBytes on lie outside and read zeros.
+constexpr uint32_t kBufferBytes = 1u << 31, kBufferFormat = 0x00020000;
+
 // Rows first .. first + ROWS - 1 of one head on their way from global memory to a tile: load() starts them; after wait_loads()
 // and store() they are in the tile, for all waves from the next barrier on.  Rows from `limit` on hold other rows of the head: they are masked, and masked
-// rows may hold anything.  Elements from `dim` on meet zeros of the other operand.
+// rows may hold anything.  Elements from `dim` on are zeros.
 //
 // Straight into LDS, past the registers, where every row begins on 16 bytes and holds whole chunks: an instruction moves 64
-// chunks to 64 places in turn, so the lanes fetch what belongs at theirs.  A place beyond the head's elements gets the row's
-// first chunk, which is as finite as the row.
+// chunks to 64 places in turn, so the lanes fetch what belongs at theirs.  A place beyond the head's elements gets zeros, as its
+// offset lies outside the buffer: whatever stood there would meet zeros of the other operand, and 0 times an infinity is NaN.
 template <class T, int DB, int ROWS, int WAVES, bool DIRECT>
 struct TileLoad {
     using H = HeadTile<T, DB>;
@@ -277,14 +280,15 @@ struct TileLoad {
         for (int i = 0; i < COUNT; ++i) {
             const int id = (wave * COUNT + i) * 64 + lane_id(), r = id / H::CHUNKS, c = (id % H::CHUNKS) ^ H::twist(r);
             row[i] = r;
-            element[i] = (c * H::N < dim ? c : 0) * 16;
+            element[i] = c * H::N < dim ? c * 16 : kBufferBytes;
             offset[i] = row[i] * (uint32_t)pitch + element[i];
         }
     }
     SDP4_DEV void move(const T *h) { head = reinterpret_cast<const char *>(h); }
     SDP4_DEV void load(char *tile, int first, int limit)
     {
-        const uint64_t base = uniform((uint64_t)(head + first * pitch));
+        const uint64_t from = uniform((uint64_t)(head + first * pitch));
+        const u32x4 base = {(uint32_t)from, (uint32_t)(from >> 32), kBufferBytes, kBufferFormat};
         const uint32_t at = lds_address(tile) + uniform(threadIdx.x / kWave) * (COUNT * 1024);
         if (first + ROWS <= limit) {
 #pragma unroll
@@ -299,9 +303,12 @@ struct TileLoad {
         }
     }
     // No register is written, so the compiler need not know that this is under way: wait_loads() sees to it.
-    SDP4_DEV static void start(uint32_t at, uint32_t off, uint64_t base)
+    SDP4_DEV static void start(uint32_t at, uint32_t off, u32x4 base)
     {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :
+                     : "s"(at), "v"(off), "s"(base)
+                     : "memory");
     }
     SDP4_DEV void store(char *, int, int) const {}
 };

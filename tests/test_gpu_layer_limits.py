@@ -38,3 +38,69 @@ def test_decoder_attention_is_float32(monkeypatch):
         wants = ref.attention_grad(dout, q, k, v, out, lse, lengths, scale, "f32")
         for got, (want, bound), name in zip(grads, wants, ("dq", "dk", "dv")):
             close(got, want, last(want, bound), name)
+
+
+# ---------------------------------------------------------------------------
+# an infinity in the first elements of a head that does not fill its columns
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 40, 48, 72, 80, 104, 136, 160, 200, 248])
+def test_attention_key_of_score_minus_infinity(dim, dtype):
+    """A key whose first element makes its scores -inf weighs nothing, and rows that see no other come out as zeros, however the
+    heads are laid out."""
+    t = torch()
+    from tests.test_gpu_layer import Case
+    lengths, inf = [50, 41], float("inf")
+    results = []
+    for layout in ("dense", "odd"):
+        say("attention of an infinite key", dim, dtype, layout)
+        c = Case(60, lengths, 0, 4, 2, dim, dtype, layout=layout)
+        c.q[:, :, 0] = c.q[:, :, 0].abs() + 0.5
+        for at in (0, 17, 50, 51, 90):                       # the first of a sequence: row `at` sees no other key
+            c.k[at, :, 0] = -inf
+        results.append([x.clone() for x in c.forward()] + [x.clone() for x in c.backward()])
+    (out, lse, *_), q, k, v = results[0], f64(c.q), f64(c.k), f64(c.v)
+    assert bool((out[[0, 50, 51]] == 0).all()) and bool(t.isneginf(lse[:, [0, 50, 51]]).all())
+    keep = np.isfinite(k[:, 0, 0])
+    k0 = np.where(keep[:, None, None], k, 0.0)
+    for a, b in ((0, 50), (50, 91)):
+        for h in range(4):
+            s = c.scale * q[a:b, h] @ k0[a:b, h // 2].T
+            seen = np.tril(np.ones(s.shape, bool)) & keep[a:b]
+            rows = seen.any(1)
+            s = np.where(seen, s, -np.inf)[rows]
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            val = v[a:b, h // 2]
+            want, size = p @ val, p @ np.abs(val)
+            # as for any other scores: dim + 2 half steps of a score's terms, 10 of the score, those of the sums, the result's
+            err = (dim + 2) * ref.U * c.scale * (np.abs(q[a:b, h]) @ np.abs(k0[a:b, h // 2]).T).max() + \
+                10 * ref.U * np.abs(np.where(np.isfinite(s), s, 0.0)).max() + 8 * ref.U
+            low = ref.V * (1 + 2.0 ** -7) if dtype == "bf16" else 0.0
+            close(f64(out)[a:b, h][rows], want, size * (2 * err + 80 * ref.U + low) + ref.rounding(dtype) * np.abs(want) + ref.TINY,
+                  (a, h))
+    for x, y, name in zip(*results, ("out", "lse", "dq", "dk", "dv")):
+        assert t.equal(x.isnan(), y.isnan()) and t.equal(x.nan_to_num(), y.nan_to_num()), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 40, 80, 104, 136, 200])
+def test_attention_query_of_score_minus_infinity(dim, dtype):
+    """A query whose scores are all -inf gives no weight to any value: dv is finite, and that of the other queries."""
+    t = torch()
+    from tests.test_gpu_layer import Case
+    results = []
+    for layout in ("dense", "odd"):
+        say("attention of an infinite query", dim, dtype, layout)
+        c = Case(61, [70], 0, 4, 2, dim, dtype, layout=layout)
+        c.k[:, :, 0] = c.k[:, :, 0].abs() + 0.5
+        c.q[33, :, 0] = -float("inf")
+        out, lse = c.forward()
+        assert bool((out[33] == 0).all()) and bool(t.isneginf(lse[:, 33]).all())
+        results.append(c.backward()[2].clone())
+    dout, q = f64(c.dout), f64(c.q)
+    dout[33], q[33] = 0.0, 0.0
+    finite = np.where(np.isfinite(f64(lse)), f64(lse), 0.0)
+    want, bound = ref.attention_grad(dout, q, f64(c.k), f64(c.v), f64(out), finite, [70], c.scale, dtype)[2]
+    close(results[0], want, bound, "dv")
+    assert t.equal(*results)
