@@ -302,13 +302,11 @@ struct TileLoad {
             }
         }
     }
-    // No register is written, so the compiler need not know that this is under way: wait_loads() sees to it.
+    // Where in LDS: register m0, which the compiler sets as the operand that it is, one wait state before the load.  No register
+    // is written, so the compiler need not know that this is under way: wait_loads() sees to it.
     SDP4_DEV static void start(uint32_t at, uint32_t off, u32x4 base)
     {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     :
-                     : "s"(at), "v"(off), "s"(base)
-                     : "memory");
+        asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "{m0}"(at), "v"(off), "s"(base) : "memory");
     }
     SDP4_DEV void store(char *, int, int) const {}
 };
@@ -348,7 +346,7 @@ SDP4_DEV void store_row(T *row, int dim, const f32x16 (&o)[DB], float by)
 SDP4_DEV void load_word(float *to, const float *from)
 {
     const uint32_t at = lds_address(to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(at), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" : : "{m0}"(at), "v"(from) : "memory");
 }
 
 // Through registers, for all other heads: a head's last chunk, where it is not whole, is read as the head's last whole one and

@@ -211,3 +211,20 @@ def test_workspaces_serve_fewer_rows():
               lambda n: L.sdp4_attention_grad_workspace(n, 12, 4, 80)):
         sizes = [f(n) for n in sorted(rows)]
         assert sizes == sorted(sizes)
+
+
+def test_inline_assembly_names_the_registers_that_it_writes():
+    """m0 says where in LDS a load goes: it is an operand, so that the compiler knows, and no statement sets it by itself."""
+    import glob
+    import os
+    import re
+    root = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2410_15526_amd")
+    loads = 0
+    for path in sorted(glob.glob(os.path.join(root, "csrc*", "*.h*"))):
+        with open(path) as f:
+            for text in re.findall(r"\basm\b(?:\s+volatile)?\s*\((.*?)\)\s*;", f.read(), re.S):
+                assert not re.search(r"s_\w+\s+m0\b", text), (path, text)
+                if re.search(r"_lds_|\blds\b", text):
+                    loads += 1
+                    assert '"{m0}"(' in text, (path, text)
+    assert loads > 0
