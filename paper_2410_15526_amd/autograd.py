@@ -18,6 +18,8 @@ from . import sdp4
 
 
 def _workspace(nbytes: int, device):
+    if nbytes < 0:
+        raise ValueError("sdp4: sizes out of range")
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
@@ -251,16 +253,19 @@ class _Embedding(torch.autograd.Function):
         tokens, = ctx.saved_tensors
         shape, dtype, scale = ctx.args
         dout = _laid_out(dout)
-        dtable = torch.empty(shape, dtype=dtype, device=dout.device)
-        work = _workspace(sdp4.sdp4_embedding_grad_workspace(tokens.shape[0], *shape), dout.device)
-        sdp4.sdp4_embedding_grad(tokens, dout, scale, dtable, work)
-        return None, dtable, None, None
+        rows, most = tokens.shape[0], sdp4.MAX_GRAD_TOKENS
+        # more rows than a call takes: their sums are added up in float32, rounded once
+        dtable = torch.empty(shape, dtype=dtype if rows <= most else torch.float32, device=dout.device)
+        work = _workspace(sdp4.sdp4_embedding_grad_workspace(min(rows, most), *shape), dout.device)
+        for a in range(0, max(rows, 1), most):
+            sdp4.sdp4_embedding_grad(tokens[a:a + most], dout[a:a + most], scale, dtable, work, accumulate=a > 0)
+        return None, dtable.to(dtype), None, None
 
 
 def embedding(tokens, table, scale: float = 1.0, dtype=None):
     """scale * table[tokens] for tokens [rows] (negative: zeros), in the table's
     type by default; see ``sdp4_embedding``.  The table's gradient is summed
-    token by token in float32."""
+    token by token in float32, over any number of rows."""
     return _Embedding.apply(_dense(tokens), _laid_out(table), float(scale), table.dtype if dtype is None else dtype)
 
 

@@ -5,7 +5,7 @@ import pytest
 
 from tests import _layer as ref
 from tests._gpu import say, torch
-from tests.test_gpu_step import close, f64
+from tests.test_gpu_step import close, dt, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -38,6 +38,55 @@ def test_decoder_attention_is_float32(monkeypatch):
         wants = ref.attention_grad(dout, q, k, v, out, lse, lengths, scale, "f32")
         for got, (want, bound), name in zip(grads, wants, ("dq", "dk", "dv")):
             close(got, want, last(want, bound), name)
+
+
+# ---------------------------------------------------------------------------
+# the embedding's gradient over more rows than one call takes
+# ---------------------------------------------------------------------------
+def table_gradient(ids, table, dout, scale):
+    from paper_2410_15526_amd import autograd
+    leaf = table.detach().requires_grad_()
+    autograd.embedding(ids, leaf, scale, dout.dtype).backward(dout)
+    return leaf.grad
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_embedding_gradient_in_several_calls(dtype, monkeypatch):
+    """Rows of a few more calls than one, holes among them; the sums are float32 over the calls and rounded once."""
+    t = torch()
+    from paper_2410_15526_amd import sdp4
+    g = t.Generator(device="cuda").manual_seed(5)
+    ids = t.randint(-2, 45, (1000,), device="cuda", generator=g)
+    table, dout = (t.randn(n, 37, device="cuda", generator=g).to(dt(dtype)) for n in (41, 1000))
+    want = ref.embedding_grad(ids.cpu().numpy(), f64(dout), 0.5, 41, None, dtype)
+    size = ref.embedding_grad(ids.cpu().numpy(), np.abs(f64(dout)), 0.5, 41, None, dtype)[0]
+    rows, plain = [], sdp4.sdp4_embedding_grad
+
+    def watched(ids, dout, *args, **kw):
+        rows.append(len(ids))
+        plain(ids, dout, *args, **kw)
+
+    monkeypatch.setattr(sdp4, "sdp4_embedding_grad", watched)
+    for limit in (1000, 999, 300, 1):
+        say("embedding gradient", dtype, limit)
+        monkeypatch.setattr(sdp4, "MAX_GRAD_TOKENS", limit)
+        rows.clear()
+        got = table_gradient(ids, table, dout, 0.5)
+        calls = -(-1000 // limit)                            # one more rounding of a sum in each
+        assert got.dtype == table.dtype and len(rows) == calls and max(rows) <= limit and sum(rows) == 1000
+        close(got, want[0], want[1] + (calls - 1) * ref.U * size, limit)
+
+
+def test_embedding_gradient_beyond_one_call():
+    t = torch()
+    from paper_2410_15526_amd import sdp4
+    rows = sdp4.MAX_GRAD_TOKENS + 3
+    say("embedding gradient", rows)
+    g = t.Generator(device="cuda").manual_seed(6)
+    ids = t.randint(0, 1000, (rows,), device="cuda", generator=g)
+    table, dout = (t.randn(n, 4, device="cuda", generator=g) for n in (1000, rows))
+    got = table_gradient(ids, table, dout, 1.0)
+    close(got, *ref.embedding_grad(ids.cpu().numpy(), f64(dout), 1.0, 1000, None, "f32"), "gradient")
 
 
 # ---------------------------------------------------------------------------
