@@ -727,6 +727,9 @@ def _block(arrays, post_eps, post_weight, gate, branch_scale, residual_scale, pr
         out.append((p, stride))
     if shape is None:
         raise ValueError("sdp4: no matrix given")
+    for w, what in ((post_weight, "post_weight"), (pre_weight, "pre_weight")):
+        if types[0] is None and w is not None:      # no matrix of the branch's type: its weights have it
+            types[0] = _float_dtype(w, what)
     x_type = types[0] if types[0] is not None else types[1]
     y_type = types[1] if types[1] is not None else types[0]
     weight = torch.float32 if x_type == F32 else torch.bfloat16

@@ -153,3 +153,22 @@ def test_attention_query_of_score_minus_infinity(dim, dtype):
     want, bound = ref.attention_grad(dout, q, f64(c.k), f64(c.v), f64(out), finite, [70], c.scale, dtype)[2]
     close(results[0], want, bound, "dv")
     assert t.equal(*results)
+
+
+# ---------------------------------------------------------------------------
+# block norms of two types, of which one result is used
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("general", [False, True])
+def test_norm_of_a_stream_whose_next_input_is_not_used(general, monkeypatch):
+    """A float32 stream beside bfloat16 weights, and a gradient by y alone."""
+    t = torch()
+    from paper_2410_15526_amd import autograd, sdp4
+    if general:
+        sdp4.lib()
+        monkeypatch.setattr(sdp4, "_fast", None)
+    x = t.randn(9, 50, device="cuda").requires_grad_()
+    w = t.ones(50, dtype=t.bfloat16, device="cuda").requires_grad_()
+    y, h = autograd.block_norm(None, x, w, residual_scale=2.0, dtype=t.bfloat16)
+    assert y.dtype == t.float32 and h.dtype == t.bfloat16
+    (3 * y).sum().backward()
+    assert bool((x.grad == 6).all()) and bool((w.grad == 0).all())
