@@ -18,7 +18,7 @@ from dataclasses import dataclass
 
 import torch
 
-from . import autograd
+from . import autograd, sdp4
 from .pipeline import HotPath
 
 
@@ -72,7 +72,7 @@ class Decoder:
         self.path.w_prev.copy_(self.path.w_new)
         self.moments = [torch.zeros(n, device="cuda") for _ in range(2)]
         self.table = autograd.rope_table(cfg.seq, d)
-        # what attention adds to the scores of one sequence, for forms of the model that spell it out
+        # what attention adds to the scores of one sequence, where it is spelled out
         self.mask = torch.full((cfg.seq, cfg.seq), float("-inf"), device="cuda").triu(1)
 
     def logits(self, tokens, weights, step: int, p: float):
@@ -81,8 +81,11 @@ class Decoder:
         rows, d = tokens.numel(), c.hidden // c.heads
         positions = torch.arange(c.seq, device="cuda").repeat(tokens.shape[0])
         sequences = torch.arange(0, rows + 1, c.seq, device="cuda")
-        x = autograd.embedding(tokens.reshape(-1), weights["embed"])
-        h = autograd.block_norm(None, x)[1]
+        if c.width <= sdp4.MAX_VOCAB:
+            x = autograd.embedding(tokens.reshape(-1), weights["embed"])
+        else:
+            x = weights["embed"][tokens.reshape(-1)]
+        x, h = self.normed(x)
         for i in range(c.layers):
             w = {k[len(f"{i}."):]: v for k, v in weights.items() if k.startswith(f"{i}.")}
             # masks of this step, layer and place: a range of element numbers each
@@ -90,18 +93,33 @@ class Decoder:
             qkv = (h @ w["qkv"].t()).view(rows, 3 * c.heads, d)
             q, k = autograd.qk_norm_rope(qkv[:, :c.heads], qkv[:, c.heads:2 * c.heads], w["q_norm"], w["k_norm"], 1e-6,
                                          self.table, positions)
-            # float32 heads: scores, probabilities and both products unrounded, one rounding of the result
-            q, k, v = (t.float() for t in (q, k, qkv[:, 2 * c.heads:]))
-            a = autograd.attention(q, k, v, sequences).to(x.dtype).view(rows, c.hidden)
+            a = self.attend(q, k, qkv[:, 2 * c.heads:], sequences).view(rows, c.hidden)
             x, h = self.join(a @ w["out"].t(), w["out_bias"], w.get("attention_norm"), x, p, offset[0])
             u = torch.nn.functional.gelu(h @ w["up"].t())
             x, h = self.join(u @ w["down"].t(), w["down_bias"], w.get("mlp_norm"), x, p, offset[1])
         return h @ weights["embed"].t()
 
+    # Attention, norms and the embedding are torch's at sizes beyond those of the operators.
+    def attend(self, q, k, v, sequences):
+        """Attention of float32 heads: scores, probabilities and both products unrounded, one rounding of the result."""
+        c, (rows, _, d) = self.cfg, q.shape
+        if sdp4.MIN_ATTENTION_DIM <= d <= sdp4.MAX_ATTENTION_DIM:
+            return autograd.attention(q.float(), k.float(), v.float(), sequences).to(q.dtype)
+        dtype = q.dtype
+        q, k, v = (t.reshape(-1, c.seq, c.heads, d).transpose(1, 2).float().contiguous() for t in (q, k, v))
+        a = torch.softmax(q @ k.transpose(2, 3).contiguous() * d ** -0.5 + self.mask, -1) @ v
+        return a.transpose(1, 2).reshape(rows, c.heads, d).to(dtype)
+
+    def normed(self, x):
+        """The residual stream and its norm, the next block's input."""
+        if self.cfg.hidden <= sdp4.MAX_HIDDEN:
+            return autograd.block_norm(None, x)
+        return x, x * torch.rsqrt((x.float() ** 2).mean(1, keepdim=True) + 1e-6).to(x.dtype)
+
     def join(self, branch, bias, post_weight, x, p: float, offset: int):
         """The residual stream behind a block, and the next block's input."""
         if post_weight is None:
-            return autograd.block_norm(None, autograd.dropout_add(branch, bias, x, p, self.seed, offset))
+            return self.normed(autograd.dropout_add(branch, bias, x, p, self.seed, offset))
         branch = autograd.dropout_add(branch, bias, None, p, self.seed, offset)
         return autograd.block_norm(branch, x, post_weight=post_weight, post_eps=1e-6)
 

@@ -172,3 +172,39 @@ def test_norm_of_a_stream_whose_next_input_is_not_used(general, monkeypatch):
     assert y.dtype == t.float32 and h.dtype == t.bfloat16
     (3 * y).sum().backward()
     assert bool((x.grad == 6).all()) and bool((w.grad == 0).all())
+
+
+# ---------------------------------------------------------------------------
+# the decoder's sizes beyond those of the operators
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("hidden,heads", [(256, 64), (768, 2)])
+def test_decoder_with_heads_beyond_the_operators(hidden, heads):
+    """Heads of 4 and of 384 elements: gradients against float32, to the 30 roundings of the decoder's other sizes."""
+    torch()
+    from paper_2410_15526_amd.decoder import Config, Decoder, sequences
+    from tests.test_gpu_decoder import plain_loss
+    model = Decoder(Config(batch=2, hidden=hidden, heads=heads, layers=1), seed=3)
+    tokens, targets = sequences(model.cfg, 2, 0)
+    loss = model.backward(tokens, targets, p=0.0)
+    leaves = {k: v.detach().float().requires_grad_() for k, v in model.weights.items()}
+    want = plain_loss(model, tokens, targets, leaves)
+    want.backward()
+    assert abs(float(loss) - float(want.detach())) < 0.02 * float(want.detach())
+    for k, v in leaves.items():
+        rel = float((model.grads[k] - v.grad).norm() / v.grad.norm())
+        assert rel < 0.06, (k, rel)
+
+
+def test_decoder_beyond_the_widest_norm():
+    """More columns than a block norm takes, no layers: the embedding, a norm and the loss."""
+    torch()
+    from paper_2410_15526_amd import sdp4
+    from paper_2410_15526_amd.decoder import Config, Decoder, sequences
+    from tests.test_gpu_decoder import plain_loss
+    model = Decoder(Config(vocab=60, width=64, batch=2, hidden=sdp4.MAX_HIDDEN + 256, heads=64, layers=0), seed=3)
+    tokens, targets = sequences(model.cfg, 2, 0)
+    model.backward(tokens, targets, p=0.0)
+    leaves = {k: v.detach().float().requires_grad_() for k, v in model.weights.items()}
+    plain_loss(model, tokens, targets, leaves).backward()
+    got, want = model.grads["embed"], leaves["embed"].grad
+    assert float((got - want).norm() / want.norm()) < 0.06
