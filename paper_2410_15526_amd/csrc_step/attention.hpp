@@ -14,6 +14,7 @@
 // of a step of 16 at place 4 a + b.
 #pragma once
 
+#include "shares.hpp"
 #include "step_device.hpp"
 
 #include <limits.h>
@@ -506,15 +507,6 @@ SDP4_DEV int min_wave(int v)
     return (int)uniform((uint32_t)v);
 }
 SDP4_DEV int max_wave(int v) { return -min_wave(-v); }
-
-// Work items in eight shares, one for each XCD: blocks are dealt to the XCDs in turn, so the blocks of one share, which read the
-// same keys and values, meet in one L2.
-SDP4_DEV int64_t shared_item(int64_t block, int64_t items)
-{
-    const int64_t each = (items + 7) / 8;
-    return (block & 7) * each + (block >> 3);
-}
-inline int64_t shared_blocks(int64_t items) { return 8 * ((items + 7) / 8); }
 
 // Which of the tiles of ROWS keys is number `place` by the rows that follow up to its sequence's end, those with most first, so
 // that no long walk begins when the others end.  (Four sequences of 2048, 40 heads of 128 over 8: dk and dv in 404 us, in the order of

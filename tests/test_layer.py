@@ -228,3 +228,42 @@ def test_inline_assembly_names_the_registers_that_it_writes():
                     loads += 1
                     assert '"{m0}"(' in text, (path, text)
     assert loads > 0
+
+
+@pytest.fixture(scope="module")
+def shares(tmp_path_factory):
+    """csrc_step/shares.hpp, compiled for the host."""
+    import os
+    import subprocess
+    root = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2410_15526_amd", "csrc_step")
+    folder = tmp_path_factory.mktemp("shares")
+    (folder / "shares.cpp").write_text("""
+#include "shares.hpp"
+#include <vector>
+extern "C" int64_t blocks(int64_t items) { return sdp4::shared_blocks(items); }
+extern "C" void deal(int64_t blocks, int64_t items, int64_t *out)
+{
+    for (int64_t b = 0; b < blocks; ++b)
+        out[b] = sdp4::shared_item(b, items);
+}
+""")
+    lib = str(folder / "shares.so")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", root, str(folder / "shares.cpp"), "-o", lib], check=True)
+    L = C.CDLL(lib)
+    L.blocks.restype, L.blocks.argtypes, L.deal.argtypes = C.c_int64, [C.c_int64], [C.c_int64, C.c_int64, C.c_void_p]
+    return L
+
+
+def dealt(shares, blocks, items):
+    out = np.empty(blocks, np.int64)
+    shares.deal(blocks, items, out.ctypes.data)
+    return out
+
+
+@pytest.mark.parametrize("items", [1, 7, 8, 9, 63, 1000, (1 << 22) - 8, (1 << 22) + 1, (1 << 22) + 4096])
+def test_every_work_item_is_dealt_once(items, shares):
+    """Grids of more than 2^22 blocks are rounded up to whole rows of 2^22: the blocks of the rest have nothing to do."""
+    n = shares.blocks(items)
+    grid = n if n <= 1 << 22 else -(-n >> 22) << 22
+    got = dealt(shares, grid, items)
+    assert np.array_equal(np.sort(got[got < items]), np.arange(items)) and got.min() >= 0
