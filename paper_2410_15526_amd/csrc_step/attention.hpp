@@ -509,15 +509,18 @@ SDP4_DEV int min_wave(int v)
 SDP4_DEV int max_wave(int v) { return -min_wave(-v); }
 
 // Which of the tiles of ROWS keys is number `place` by the rows that follow up to its sequence's end, those with most first, so
-// that no long walk begins when the others end.  (Four sequences of 2048, 40 heads of 128 over 8: dk and dv in 404 us, in the order of
-// memory 590.  By queries, of which a launch has more blocks, the forward pass took 251 us so and 237 in the order of memory.)
-// Many tiles are left in order, as their ends are a small part.
+// that no long walk begins when the others end; a head's places are dealt to the XCDs (dealt_place).  dk and dv of four sequences
+// of 2048, heads of 128, 5 query heads to one of 1 / 2 / 4 / 8 / 12: the whole backward pass in 163 / 216 / 372 / 696 / 1101 us,
+// in the order of memory 171 / 210 / 373 / 828 / 1137, by work in runs 194 / 269 / 434 / 713 / 1105.  Twelve sequences of 16384
+// rows in all, 16 heads over 4: 824, 972, 911; one of 16384: 3995, 4674, 4696.  Each block looks for its tile first: where
+// walks are short or blocks many, the order of memory is up to 6 % faster (40 sequences of 8192 rows, 8 heads over 1: 138 against
+// 144; twelve of 16384, 16 heads of 64: 480 against 507).  By queries, of which a launch has more blocks, the forward pass took
+// 251 us so and 237 in the order of memory.  More tiles than kMostOrdered are left in order, as their ends are a small part.
 constexpr int kMostOrdered = 256;
+SDP4_DEV bool by_work(const Sequences &s, int tiles) { return s.offsets && tiles <= kMostOrdered; }
 template <int THREADS, int ROWS>
 SDP4_DEV int ordered_tile(const Sequences &s, const int64_t *samples, int (&work)[kMostOrdered], int &found, int tiles, int place)
 {
-    if (!s.offsets || tiles > kMostOrdered)
-        return place;
     for (int t = threadIdx.x; t < tiles; t += THREADS) {
         const int a = t * ROWS, b = a + ROWS < s.tokens ? a + ROWS - 1 : s.tokens - 1;
         const Span x = span_of(s, samples, a), y = span_of(s, samples, b);

@@ -303,11 +303,14 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
     const int64_t unit = shared_item(work_block(), items * pieces.count);
     if (unit >= items * pieces.count)
         return;
-    const int64_t item = unit / pieces.count;
-    const int piece = (int)(unit - item * pieces.count);
-    const int kv = (int)(item / tiles);
+    const int per_head = tiles * pieces.count, kv = (int)(unit / per_head);
+    const bool sorted = by_work(at.seq, tiles);
+    const int place = sorted ? dealt_place(unit, per_head, items * pieces.count) : (int)(unit - (int64_t)kv * per_head);
+    const int piece = place % pieces.count;
     fill_samples<64 * ALL>(at.seq, samples);
-    const int tile = ordered_tile<64 * ALL, BK>(at.seq, samples, work, found_tile, tiles, (int)(item - (int64_t)kv * tiles));
+    int tile = place / pieces.count;
+    if (sorted)
+        tile = ordered_tile<64 * ALL, BK>(at.seq, samples, work, found_tile, tiles, tile);
 
     const int all = uniform(threadIdx.x / kWave), wave = all % WAVES, mine = all / WAVES; // keys, and rows of a tile
     const int lane = lane_id(), h = lane >> 5;
@@ -354,8 +357,8 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
             }
     }
     const float c = at.scale * kLog2e;
-    const int per_head = (limit - first + BQ - 1) / BQ;
-    const int64_t steps = (int64_t)per_head * at.group, begin = pieces.from(piece, steps), count = pieces.from(piece + 1, steps);
+    const int a_head = (limit - first + BQ - 1) / BQ; // steps over one query head
+    const int64_t steps = (int64_t)a_head * at.group, begin = pieces.from(piece, steps), count = pieces.from(piece + 1, steps);
     const uint32_t seen = span.on ? end - key : 0; // queries that see the key, from its own on
 
     bool poison_k = false, poison_v = false;
@@ -368,7 +371,7 @@ __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Atte
         constexpr int PER = DIRECT ? ql.COUNT + gl.COUNT + 1 : 0;
         Reader<T, DB> read(lds_address(mem.tiles[S - 1]) + 32 * mine * H::ROW); // the tile before the first
         RowReader<T, DB> fixed(lds_address(mem.keys) + 32 * wave * H::ROW); // the values lie behind
-        int nq = first + (int)(begin % per_head) * BQ, nhead = kv * at.group + (int)(begin / per_head); // of the next load
+        int nq = first + (int)(begin % a_head) * BQ, nhead = kv * at.group + (int)(begin / a_head); // of the next load
         auto fetch = [&](int to) {
             ql.move(static_cast<const T *>(qh.p) + nhead * qh.head_stride);
             gl.move(static_cast<const T *>(doh.p) + nhead * doh.head_stride);

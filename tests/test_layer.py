@@ -246,11 +246,17 @@ extern "C" void deal(int64_t blocks, int64_t items, int64_t *out)
     for (int64_t b = 0; b < blocks; ++b)
         out[b] = sdp4::shared_item(b, items);
 }
+extern "C" void places(int per_head, int64_t units, int64_t *out)
+{
+    for (int64_t x = 0; x < units; ++x)
+        out[x] = sdp4::dealt_place(x, per_head, units);
+}
 """)
     lib = str(folder / "shares.so")
     subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", root, str(folder / "shares.cpp"), "-o", lib], check=True)
     L = C.CDLL(lib)
     L.blocks.restype, L.blocks.argtypes, L.deal.argtypes = C.c_int64, [C.c_int64], [C.c_int64, C.c_int64, C.c_void_p]
+    L.places.argtypes = [C.c_int, C.c_int64, C.c_void_p]
     return L
 
 
@@ -267,3 +273,18 @@ def test_every_work_item_is_dealt_once(items, shares):
     grid = n if n <= 1 << 22 else -(-n >> 22) << 22
     got = dealt(shares, grid, items)
     assert np.array_equal(np.sort(got[got < items]), np.arange(items)) and got.min() >= 0
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 4, 5, 7, 8, 9, 12, 16, 40])
+@pytest.mark.parametrize("per_head", [1, 2, 5, 16, 29, 64, 100, 256, 2048])
+def test_sorted_walks_are_dealt_evenly(heads, per_head, shares):
+    """Each head's places once, and no share with more than its number of mean walks and two of the longest: of whole heads it
+    has all, of the one that begins and the one that ends in it an even sample."""
+    units = heads * per_head
+    place = np.empty(units, np.int64)
+    shares.places(per_head, units, place.ctypes.data)
+    assert np.array_equal(np.sort(place.reshape(heads, per_head), 1), np.tile(np.arange(per_head), (heads, 1)))
+    walks = np.sort(np.arange(per_head) % 16 + 1)[::-1].astype(float)          # sequences of 16 tiles
+    for share in range(8):
+        mine = place[share * -(-units // 8):(share + 1) * -(-units // 8)]
+        assert walks[mine].sum() <= len(mine) * walks.mean() + 2 * walks.max()
