@@ -425,15 +425,16 @@ constexpr int kMostParts = 256;
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
 int parts_of(int64_t rows) { return (int)(rows < kMostParts ? rows : kMostParts); }
 
-// A body with the accesses of a lane for rows of `places` accesses (as few as eight waves leave), and whether they are whole.
-template <class F>
-int with_shape(int64_t cols, int n, F body)
+// A body with the accesses of a lane (as few as eight waves leave) for rows of `cols` elements, N in an access, and whether they
+// are whole.
+template <int N, class F>
+int with_shape(int64_t cols, F body)
 {
     using std::integral_constant;
-    const int64_t places = (cols + n - 1) / n;
+    const int64_t places = (cols + N - 1) / N;
     auto waves = [&](int c) { return (int)((places + 64 * c - 1) / (64 * c)); };
     auto with = [&](auto c) {
-        return cols % n == 0 ? body(c, integral_constant<bool, true>{}, waves(c)) : body(c, integral_constant<bool, false>{}, waves(c));
+        return cols % N == 0 ? body(c, integral_constant<bool, true>{}, waves(c)) : body(c, integral_constant<bool, false>{}, waves(c));
     };
     constexpr int most = 64 * kMostWaves;
     if (places <= most)
@@ -442,9 +443,10 @@ int with_shape(int64_t cols, int n, F body)
         return with(integral_constant<int, 2>{});
     if (places <= 3 * most)
         return with(integral_constant<int, 3>{});
-    if (places <= 4 * most)
-        return with(integral_constant<int, 4>{});
-    return with(integral_constant<int, 8>{});
+    if constexpr (4 * most * N < SDP4_MAX_HIDDEN)
+        if (places > 4 * most)
+            return with(integral_constant<int, 8>{});
+    return with(integral_constant<int, 4>{});
 }
 
 } // namespace
@@ -462,7 +464,7 @@ int launch_block_norm(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows
             using X = decltype(x_tag);
             using Y = decltype(y_tag);
             constexpr int N = kJoint<X, Y>;
-            return with_shape(cols, N, [&](auto accesses, auto whole, int waves) {
+            return with_shape<N>(cols, [&](auto accesses, auto whole, int waves) {
                 return launch_waves(waves, k_block_norm<X, Y, accesses, whole>, rows, kUncapped, s, p, rows, cols, typed<const X>(branch),
                                      typed<const Y>(residual), typed<Y>(y), typed<X>(h));
             });
@@ -483,7 +485,7 @@ int launch_block_norm_grad(int x_dtype, int y_dtype, const BlockNorm &p, int64_t
             constexpr int N = kJoint<X, Y>;
             const BlockNormGrad<X, Y> g{typed<const X>(a.dh), typed<const Y>(a.dy), typed<const X>(a.branch), typed<const Y>(a.y),
                                         typed<X>(a.dbranch), typed<Y>(a.dresidual), a.dgate, post, pre};
-            return with_shape(cols, N, [&](auto accesses, auto whole, int waves) {
+            return with_shape<N>(cols, [&](auto accesses, auto whole, int waves) {
                 auto kernel = p.post_norm || a.dgate ? k_block_norm_grad<X, Y, accesses, whole, true>
                                                      : k_block_norm_grad<X, Y, accesses, whole, false>;
                 return launch_waves(waves, kernel, parts, kUncapped, s, p, rows, cols, pitch, parts, g);

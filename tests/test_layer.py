@@ -288,3 +288,16 @@ def test_sorted_walks_are_dealt_evenly(heads, per_head, shares):
     for share in range(8):
         mine = place[share * -(-units // 8):(share + 1) * -(-units // 8)]
         assert walks[mine].sum() <= len(mine) * walks.mean() + 2 * walks.max()
+
+
+def test_every_block_norm_of_the_library_is_reached():
+    """A lane has as few accesses as eight waves leave: no kernel is built for more than the widest row asks for."""
+    import re
+    import subprocess
+    names = subprocess.run(["nm", "-C", sdp4._LIB_PATH], capture_output=True, text=True, check=True).stdout
+    found = set(re.findall(r"k_block_norm(?:_grad)?<(unsigned short|float), (unsigned short|float), (\d+), ", names))
+    assert len(found) >= 16
+    for x, y, accesses in found:
+        elements = 8 if x == y == "unsigned short" else 4
+        fewer = {1: 0, 2: 1, 3: 2, 4: 3, 8: 4}[int(accesses)]
+        assert 64 * 8 * fewer * elements < sdp4.MAX_HIDDEN, (x, y, accesses)
