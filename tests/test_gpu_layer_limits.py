@@ -90,6 +90,22 @@ def test_embedding_gradient_beyond_one_call():
 
 
 # ---------------------------------------------------------------------------
+# more tiles of keys than are sorted
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,rows", [("bf16", 33100), ("f32", 16700)])
+def test_attention_of_more_tiles_than_are_sorted(dtype, rows):
+    """Tiles of 128 and 64 keys, 256 of them sorted at most: many sequences, one of them long."""
+    from tests.test_gpu_layer import Case
+    say("attention of many tiles", dtype, rows)
+    r = np.random.default_rng(rows)
+    lengths = []
+    while sum(lengths) < rows:
+        lengths.append(int(r.integers(0, 250)) if len(lengths) != 40 else 1500)
+    Case(62, lengths, 11, 2, 1, 64, dtype, lead=3).check()
+
+
+
+# ---------------------------------------------------------------------------
 # an infinity in the first elements of a head that does not fill its columns
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
