@@ -486,8 +486,8 @@ int launch_block_norm_grad(int x_dtype, int y_dtype, const BlockNorm &p, int64_t
             const BlockNormGrad<X, Y> g{typed<const X>(a.dh), typed<const Y>(a.dy), typed<const X>(a.branch), typed<const Y>(a.y),
                                         typed<X>(a.dbranch), typed<Y>(a.dresidual), a.dgate, post, pre};
             return with_shape<N>(cols, [&](auto accesses, auto whole, int waves) {
-                auto kernel = p.post_norm || a.dgate ? k_block_norm_grad<X, Y, accesses, whole, true>
-                                                     : k_block_norm_grad<X, Y, accesses, whole, false>;
+                auto kernel = (p.post_norm && a.branch.p) || a.dgate ? k_block_norm_grad<X, Y, accesses, whole, true>
+                                                                     : k_block_norm_grad<X, Y, accesses, whole, false>;
                 return launch_waves(waves, kernel, parts, kUncapped, s, p, rows, cols, pitch, parts, g);
             });
         });

@@ -190,6 +190,25 @@ def test_norm_of_a_stream_whose_next_input_is_not_used(general, monkeypatch):
     assert bool((x.grad == 6).all()) and bool((w.grad == 0).all())
 
 
+@pytest.mark.parametrize("cols", [64, 1000, 4097])
+def test_gradients_that_need_no_branch(cols):
+    """The residual stream's gradient and the next norm's weight's, with and without the branch in hand."""
+    t = torch()
+    from tests.test_gpu_layer import Joint
+    c = Joint(63, 300, cols, "bf16", "f32", "post")
+    c.w2 = t.randn(cols, device="cuda").bfloat16()
+    y = t.randn(300, cols, device="cuda")
+    both = c.backward(y)
+    from paper_2410_15526_amd import sdp4
+    from tests.test_gpu_step import scratch
+    p, w1, gate, b, r = c.head()
+    dr, dw = t.full_like(y, float("nan")), t.full((cols,), float("nan"), device="cuda")
+    sdp4.sdp4_block_norm_grad(c.dh, c.dy, None, y, p, w1, gate, b, r, 1e-6, c.w2, None, dr, None, dw, None,
+                              scratch(sdp4.sdp4_block_norm_grad_workspace(300, cols)))
+    assert t.equal(dr, both["dresidual"]) and t.equal(dw, both["dpre_weight"])
+
+
+
 # ---------------------------------------------------------------------------
 # the decoder's sizes beyond those of the operators
 # ---------------------------------------------------------------------------
