@@ -419,11 +419,18 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_block_norm_grad(BlockNorm p
         }
 }
 
-// 256 / 512 / 768 / 1024 parts: 8192 x 5120 bfloat16 100 / 105 / 109 / 113 us, 2047 x 4097 37 / 40 / 50 / 56: more blocks a
-// compute unit gain less than their partial sums cost.
-constexpr int kMostParts = 256;
+// As many parts as make eight waves on each compute unit where a lane takes eight elements of a row: a row of few waves leaves the
+// others idle and waits for its own loads and sums.  256 / 512 / 1024 / 2048 parts, bfloat16 with both norms and their weights, us:
+// 8192 x 256 43 / 27 / 19 / 19, 65536 x 256 298 / 165 / 85 / 64, 8192 x 768 52 / 36 / 27 / 34, 8192 x 2048 56 / 48 / 58 / 66,
+// 8192 x 3000 67 / 72 / 83 / 104, 8192 x 5120 102 / 110 / 125 / 156: beyond these the partial sums of more
+// parts cost more than their blocks gain.  Without weights 65536 x 64 175 / 94 / 50 / 32, 8192 x 5120 62 / 63 / 65 / 70.
+constexpr int kWideRow = 512; // elements of a wave
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
-int parts_of(int64_t rows) { return (int)(rows < kMostParts ? rows : kMostParts); }
+int parts_of(int64_t rows, int64_t cols)
+{
+    const int64_t waves = (cols + kWideRow - 1) / kWideRow, most = 256 * (waves < 8 ? 8 / waves : 1);
+    return (int)(rows < most ? rows : most);
+}
 
 // A body with the accesses of a lane (as few as eight waves leave) for rows of `cols` elements, N in an access, and whether they
 // are whole.
@@ -453,7 +460,7 @@ int with_shape(int64_t cols, F body)
 
 int64_t block_norm_grad_workspace(int64_t rows, int64_t cols)
 {
-    return rows <= 0 || cols <= 0 ? 0 : 2 * parts_of(rows) * pitch_of(cols) * (int64_t)sizeof(float);
+    return rows <= 0 || cols <= 0 ? 0 : 2 * parts_of(rows, cols) * pitch_of(cols) * (int64_t)sizeof(float);
 }
 
 int launch_block_norm(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows, int64_t cols, Rows<const void *> branch,
@@ -475,7 +482,7 @@ int launch_block_norm(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows
 int launch_block_norm_grad(int x_dtype, int y_dtype, const BlockNorm &p, int64_t rows, int64_t cols, const BlockNormArrays &a,
                            float *workspace, hipStream_t s)
 {
-    const int parts = parts_of(rows);
+    const int parts = parts_of(rows, cols);
     const int64_t pitch = pitch_of(cols);
     float *post = a.dpost_weight ? workspace : nullptr, *pre = a.dpre_weight ? workspace + (post ? parts * pitch : 0) : nullptr;
     const int rc = with_type(x_dtype, [&](auto x_tag) {

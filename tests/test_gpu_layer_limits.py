@@ -209,6 +209,26 @@ def test_gradients_that_need_no_branch(cols):
 
 
 
+@pytest.mark.parametrize("x,y", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,cols", [(4101, 203), (4500, 8), (2100, 700), (1100, 1500), (520, 3001)])
+def test_block_norm_gradients_of_more_rows_than_parts(rows, cols, x, y):
+    """Blocks that walk several rows, at each number of blocks that the width of a row allows."""
+    t = torch()
+    from tests.test_gpu_layer import Joint
+    for kind in ("full", "pre"):
+        say("block norm rows", rows, cols, x, y, kind)
+        c = Joint(64, rows, cols, x, y, kind)
+        yo, ho = (t.full((rows, cols), float("nan"), dtype=dt(ty), device="cuda") for ty in (y, x))
+        c.forward(c.branch, c.residual, yo, ho)
+        got, want = c.backward(yo), c.want_grad(yo)
+        for k, v in got.items():
+            if v is not None:
+                close(v, *want[k], (k, kind))
+        again = c.backward(yo)
+        assert all(v is None or t.equal(v, again[k]) for k, v in got.items())
+
+
+
 # ---------------------------------------------------------------------------
 # the decoder's sizes beyond those of the operators
 # ---------------------------------------------------------------------------

@@ -301,3 +301,15 @@ def test_every_block_norm_of_the_library_is_reached():
         elements = 8 if x == y == "unsigned short" else 4
         fewer = {1: 0, 2: 1, 3: 2, 4: 3, 8: 4}[int(accesses)]
         assert 64 * 8 * fewer * elements < sdp4.MAX_HIDDEN, (x, y, accesses)
+
+
+@pytest.mark.cpu_only
+def test_narrow_rows_fill_the_chip():
+    """Sums of narrow rows' weight gradients over as many blocks as make eight waves on each of 256 compute units, of wide rows
+    over 256 blocks: the workspace holds two sums of each."""
+    f = sdp4.lib().sdp4_block_norm_grad_workspace
+    for cols in (8, 64, 256, 512, 768, 1024, 1536, 2048, 3000, 5120, 16384):
+        parts, waves = f(1 << 20, cols) // (8 * -(-cols // 8) * 8), -(-cols // 512)
+        assert parts >= 256 and (parts * waves > 1024 or waves > 4), (cols, parts)
+        assert parts == 256 or parts * waves <= 2048
+        assert f(parts // 2, cols) == f(1 << 20, cols) // 2
