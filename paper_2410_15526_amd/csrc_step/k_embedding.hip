@@ -2,10 +2,11 @@
 //
 // The gradient of a table row is the sum of the rows of dy whose token it is.
 // To take it in one order whatever the timing, the rows are sorted by token:
-//  1. tiles of kTile rows, each row's place in its tile counted against the
-//     whole tile (a comparison a pair: no exchange between lanes, no passes);
-//  2. with more than one tile, each row's place among all by binary searches
-//     in the other tiles;
+//  1. one tile of up to kTile rows, or tiles of 2^kManyLog2: each row's place
+//     in its tile counted against the whole tile (a comparison a pair: no
+//     exchange between lanes, no passes);
+//  2. with more than one tile, kWays of them merged at a time until one is
+//     left: each row's place by binary searches in the others;
 //  3. where each token's rows begin, by binary search, and the sums of runs of
 //     kRun sorted rows of one token;
 //  4. the table, every row written once: the sums, with whole runs from step
@@ -54,6 +55,11 @@ __global__ __launch_bounds__(256) void k_embedding(Tokens t, int64_t cols, float
 // sorting
 // ---------------------------------------------------------------------------
 constexpr int kTileLog2 = 13, kTile = 1 << kTileLog2, kRun = 32;
+// Rows of a tile where one is not enough, and runs merged at a time.  The whole gradient of 65536 / 524288 / 2^21 rows of 64
+// columns, 1000 tokens, in us: 95 / 408 / 1546; runs of two 98 / 411 / 1500, of eight 101 / 421 / 1600, of 16 108 / 464 / 1709; eight
+// with tiles of 1024 rows 105 / 414 / 1534, of 4096 110 / 495 / 1906; tiles of 8192, each row searched for in all others, 123 / 811
+// / 4966.
+constexpr int kManyLog2 = 11, kWaysLog2 = 2, kWays = 1 << kWaysLog2;
 // A block places 32 rows, so that 8192 take all 256 compute units: 17 us, 8 for 2047 rows.  Bound by the comparisons, a pair each.
 constexpr int kSortRows = 32, kSortThreads = 512, kShares = kSortThreads / kSortRows; // rows of a block; threads of a row
 
@@ -130,20 +136,23 @@ SDP4_DEV int64_t count_below(const uint32_t *keys, int64_t n, uint32_t key)
     return a;
 }
 
-__global__ __launch_bounds__(256) void k_merge_tiles(int64_t rows, const uint32_t *keys, const uint32_t *order, uint32_t *to_keys,
-                                                     uint32_t *to_order)
+// kWays sorted runs of 2^run_log2 rows each become one: a row's place among the others' by a search in each of them.
+__global__ __launch_bounds__(256) void k_merge_runs(int64_t rows, int run_log2, const uint32_t *keys, const uint32_t *order,
+                                                    uint32_t *to_keys, uint32_t *to_order)
 {
     const int64_t i = work_block() * 256 + threadIdx.x;
     if (i >= rows)
         return;
     const uint32_t key = keys[i];
-    const int64_t mine = i >> kTileLog2;
-    int64_t place = i - (mine << kTileLog2);
-    for (int64_t tile = 0, at = 0; at < rows; ++tile, at += kTile) {
-        const int64_t n = rows - at < kTile ? rows - at : kTile;
-        if (tile < mine)
+    const int64_t mine = i >> run_log2, first = mine / kWays * kWays;
+    int64_t place = (first << run_log2) + i - (mine << run_log2);
+    for (int64_t run = first; run < first + kWays; ++run) {
+        const int64_t at = run << run_log2, n = rows - at < (int64_t)1 << run_log2 ? rows - at : (int64_t)1 << run_log2;
+        if (n <= 0)
+            break;
+        if (run < mine)
             place += count_below<true>(keys + at, n, key);
-        else if (tile > mine)
+        else if (run > mine)
             place += count_below<false>(keys + at, n, key);
     }
     to_keys[place] = key, to_order[place] = order[i];
@@ -387,16 +396,19 @@ int launch_embedding_grad(const Tokens &t, int64_t cols, float scale, bool accum
     char *base = static_cast<char *>(workspace);
     auto at = [&](int64_t offset) { return reinterpret_cast<uint32_t *>(base + offset); };
     const bool merged = t.rows > kTile;
-    int tile_log2 = kTileLog2;
-    while (tile_log2 > 6 && (1 << (tile_log2 - 1)) >= t.rows) // one tile: only as large as the rows take
+    int tile_log2 = merged ? kManyLog2 : kTileLog2, passes = 0;
+    while (!merged && tile_log2 > 6 && (1 << (tile_log2 - 1)) >= t.rows) // one tile: only as large as the rows take
         --tile_log2;
+    while (merged && (int64_t)1 << (tile_log2 + passes * kWaysLog2) < t.rows)
+        ++passes;
     int rc = 0;
     if (t.rows > 0) {
+        uint32_t *keys[2] = {at(l.keys), at(l.tile_keys)}, *order[2] = {at(l.order), at(l.tile_order)}; // in turn, the first at the end
         rc = launch<kSortThreads / kWave>(k_sort_tiles, (t.rows + kSortRows - 1) / kSortRows, kUncapped, s, t, tile_log2,
-                                          at(merged ? l.tile_keys : l.keys), at(merged ? l.tile_order : l.order));
-        if (!rc && merged)
-            rc = launch<4>(k_merge_tiles, (t.rows + 255) / 256, kUncapped, s, t.rows, at(l.tile_keys), at(l.tile_order), at(l.keys),
-                           at(l.order));
+                                          keys[passes % 2], order[passes % 2]);
+        for (int p = passes; p > 0 && !rc; --p, tile_log2 += kWaysLog2)
+            rc = launch<4>(k_merge_runs, (t.rows + 255) / 256, kUncapped, s, t.rows, tile_log2, keys[p % 2], order[p % 2],
+                           keys[(p - 1) % 2], order[(p - 1) % 2]);
     }
     if (rc)
         return rc;

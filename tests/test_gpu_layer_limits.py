@@ -89,6 +89,22 @@ def test_embedding_gradient_beyond_one_call():
     close(got, *ref.embedding_grad(ids.cpu().numpy(), f64(dout), 1.0, 1000, None, "f32"), "gradient")
 
 
+@pytest.mark.parametrize("rows", [8193, 8200, 10240, 32768, 32769, 131072, 131073, 140001])
+def test_embedding_gradient_over_merged_runs(rows):
+    """Numbers of rows around those at which another pass of merges begins; tokens of few rows, of many and of none."""
+    t = torch()
+    from paper_2410_15526_amd import sdp4
+    g = t.Generator(device="cuda").manual_seed(rows)
+    ids = (5000 * t.rand(rows, device="cuda", generator=g) ** 3).long()
+    ids[::5], ids[1::1000] = 77, -1
+    dout = t.randn(rows, 9, device="cuda", generator=g)
+    d = t.full((5000, 9), float("nan"), device="cuda")
+    work = t.full((sdp4.sdp4_embedding_grad_workspace(rows, 5000, 9),), 0xFF, dtype=t.uint8, device="cuda")
+    sdp4.sdp4_embedding_grad(ids, dout, 1.0, d, work)
+    close(d, *ref.embedding_grad(ids.cpu().numpy(), f64(dout), 1.0, 5000, None, "f32"), rows)
+
+
+
 # ---------------------------------------------------------------------------
 # more tiles of keys than are sorted
 # ---------------------------------------------------------------------------
