@@ -93,17 +93,20 @@ class Decoder:
             qkv = (h @ w["qkv"].t()).view(rows, 3 * c.heads, d)
             q, k = autograd.qk_norm_rope(qkv[:, :c.heads], qkv[:, c.heads:2 * c.heads], w["q_norm"], w["k_norm"], 1e-6,
                                          self.table, positions)
-            a = self.attend(q, k, qkv[:, 2 * c.heads:], sequences).view(rows, c.hidden)
+            a = self.attend(q, k, qkv[:, 2 * c.heads:], sequences).reshape(rows, c.hidden)
             x, h = self.join(a @ w["out"].t(), w["out_bias"], w.get("attention_norm"), x, p, offset[0])
             u = torch.nn.functional.gelu(h @ w["up"].t())
             x, h = self.join(u @ w["down"].t(), w["down_bias"], w.get("mlp_norm"), x, p, offset[1])
         return h @ weights["embed"].t()
 
-    # Attention, norms and the embedding are torch's at sizes beyond those of the operators.
+    # Attention, norms and the embedding are torch's at sizes beyond those of the operators, or where these are slower.
     def attend(self, q, k, v, sequences):
         """Attention of float32 heads: scores, probabilities and both products unrounded, one rounding of the result."""
         c, (rows, _, d) = self.cfg, q.shape
-        if sdp4.MIN_ATTENTION_DIM <= d <= sdp4.MAX_ATTENTION_DIM:
+        # Kernels of float32 heads beyond 128 elements spill registers.  Milliseconds of a whole backward(), heads of 256, by the
+        # operator and spelled out: 64 sequences of 512, 2 heads 8.3 and 8.6, 4 of 2048, 4 heads 8.1 and 8.2, 2 of 4096 12.5 and
+        # 12.5, one of 4096, 2 heads 6.3 and 3.9, one of 8192 15.9 and 11.2.
+        if sdp4.MIN_ATTENTION_DIM <= d <= (128 if c.seq > 2048 else sdp4.MAX_ATTENTION_DIM):
             return autograd.attention(q.float(), k.float(), v.float(), sequences).to(q.dtype)
         dtype = q.dtype
         q, k, v = (t.reshape(-1, c.seq, c.heads, d).transpose(1, 2).float().contiguous() for t in (q, k, v))

@@ -248,14 +248,15 @@ def test_block_norm_gradients_of_more_rows_than_parts(rows, cols, x, y):
 # ---------------------------------------------------------------------------
 # the decoder's sizes beyond those of the operators
 # ---------------------------------------------------------------------------
-@pytest.mark.parametrize("hidden,heads", [(256, 64), (768, 2)])
-def test_decoder_with_heads_beyond_the_operators(hidden, heads):
-    """Heads of 4 and of 384 elements: gradients against float32, to the 30 roundings of the decoder's other sizes."""
+@pytest.mark.parametrize("hidden,heads,seq,batch", [(256, 64, 64, 2), (768, 2, 64, 2), (768, 2, 64, 1), (512, 2, 2176, 1), (256, 1, 64, 2)])
+def test_decoder_with_heads_beyond_the_operators(hidden, heads, seq, batch):
+    """Heads of 4 and of 384 elements, long sequences of heads of 256 and short ones: gradients against float32, to the 30
+    roundings of the decoder's other sizes."""
     torch()
     from paper_2410_15526_amd.decoder import Config, Decoder, sequences
     from tests.test_gpu_decoder import plain_loss
-    model = Decoder(Config(batch=2, hidden=hidden, heads=heads, layers=1), seed=3)
-    tokens, targets = sequences(model.cfg, 2, 0)
+    model = Decoder(Config(batch=batch, hidden=hidden, heads=heads, layers=1, seq=seq), seed=3)
+    tokens, targets = sequences(model.cfg, batch, 0)
     loss = model.backward(tokens, targets, p=0.0)
     leaves = {k: v.detach().float().requires_grad_() for k, v in model.weights.items()}
     want = plain_loss(model, tokens, targets, leaves)
