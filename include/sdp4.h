@@ -524,7 +524,8 @@ typedef struct {
  * scores are all -inf, out is 0 and lse -inf.
  *
  * Scores, their sums and the results are float32; with bfloat16 heads the
- * probabilities are rounded to bfloat16 for their product with the values.
+ * probabilities are rounded to bfloat16 for their product with the values
+ * (float32 heads have no rounding but float32's).
  *
  *   q, k, v   k and v have the same number of heads
  *   out       heads like q, any strides; no overlap with an input

@@ -35,13 +35,15 @@ SDP4_DEV void spread()
 // WAVES waves of 32 rows each, BN keys at a time, STAGES tiles in LDS.  The scores are computed transposed, keys by rows, so that
 // a lane holds one row's: its maximum and sum need one exchange, and p is the second product's operand as it lies.
 //
-// Four sequences of 2048, 40 heads of 128 over 8, bfloat16: 230 to 247 us by card, 695 to 747 TFLOP/s of the pairs that rows
-// see (a library product of 8192^3 reaches 1143); one sequence of 16384, 16 heads over 4: 1436 us, 766.  Neither memory nor
+// Four sequences of 2048, 40 heads of 128 over 8, bfloat16: 220 to 248 us by card and inputs, 693 to 781 TFLOP/s of the pairs that
+// rows see (a library product of 8192^3 reaches 1143); one sequence of 16384, 16 heads over 4: 1345 to 1420 us, 774 to 817, where
+// four key heads over eight XCDs give every other one three times the work of the rest.  float32: the four 1528 us, 112 TFLOP/s.  Neither memory nor
 // either kind of unit alone is the bound: two waves on a SIMD wait for their own scores, maxima and exponentials.  Two, since a
 // row's results, queries and scores take 224 registers; eight waves on a tile in place of four took 280 us where this took 248,
 // 64 keys a tile halve the barriers and exchanges of 32 (265 and 295), and more tiles ahead change nothing: loads are not
 // waited for.
-// Heads of more than 128 take one wave on a SIMD and 32 keys, as their registers allow.
+// Heads of more than 128 take one wave on a SIMD and 32 keys, as their registers allow: four of 2048, 8 heads of 256, 264 us in
+// bfloat16 and 1124 in float32, which spills a few registers.
 template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Heads qh, Heads kh, Heads vh, Heads oh, float *lse,
                                                              int tiles, int64_t items)
@@ -180,7 +182,11 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention(Attention at, Hea
                 ref = large ? 0.0f : ref;
             }
             float part[4] = {};
-            Frag<T> p[2 * RB]; // bfloat16: the one rounding on the way to the second product
+            // bfloat16: the one rounding on the way to the second product, whose operands the matrix instructions take so.  One
+            // sequence of 2048, heads of 128: out is off by 2.0e-3 of itself, its own rounding alone by 1.6e-3.  A second product
+            // with what the rounding leaves would bring 1.6e-3, and takes 317 us where this takes 248 (four of 2048, 40 heads over
+            // 8), 1828 for 1345 (one of 16384, 16 over 4).  float32 heads have none.
+            Frag<T> p[2 * RB];
 #pragma unroll
             for (int s = 0; s < 2 * RB; ++s) {
                 float w[8];

@@ -39,6 +39,8 @@ SDP4_DEV void probabilities(f32x16 &x, f32x16 &y, float c, float add, bool hard,
         x[r] = exp2_of(x[r]);
 }
 
+// p or dS as operands of the second products: with bfloat16 heads their one rounding, as in the forward pass (gradients are off by
+// 2.4e-3 of themselves, with only their own rounding by 1.7e-3).
 template <class T>
 SDP4_DEV void operands(const f32x16 &x, Frag<T> (&f)[2])
 {
@@ -123,7 +125,7 @@ SDP4_DEV void join_groups(char *lds, int wave, int mine, f32x16 (&x)[DB])
 }
 
 // Columns are queries, as in the forward pass, and the tiles are its tiles.  Four sequences of 2048, 40 heads of 128 over 8,
-// bfloat16: 320 us (three products: 800 TFLOP/s), 358 with eight waves a block.
+// bfloat16: 320 to 370 us by inputs in the last-level cache (three products: 700 to 800 TFLOP/s), 358 for 320 with eight waves a block.
 template <class T, int DB, int WAVES, int BN, int STAGES, int OCC, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, Heads doh, Heads qh, Heads kh, Heads vh, Heads oh,
                                                                 const float *lse, Heads dqh, float *delta, int tiles,
@@ -275,11 +277,13 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void k_attention_dq(Attention at, 
 // in turn, their sums joined at the end in the order of the groups): two waves on a SIMD, whose results and operands have to fit
 // 256 registers each, so keys and values stay in LDS.  HELD: in registers, for one wave on a SIMD.  PARTS: 1 dv, 2 dk, 3 both.
 //
-// The same heads: 404 us (four products: 850 TFLOP/s), tiles with the longest walks first.  Both launches together took 960 us when this form came, 1213 with HELD and
-// one wave on a SIMD, 1505 with launches of their own for dk and dv.  What bounds it: the fixed operands come out of LDS for each
-// tile again, and the two waves wait for p and dS.
+// The same heads: 404 to 488 us by inputs in the last-level cache (four products: 700 to 850 TFLOP/s), tiles with the longest walks
+// first; the whole backward pass 665 to 747.  Both launches together took 960 us when this form came, 1213 with HELD and one wave
+// on a SIMD, 1505 with launches of their own for dk and dv.  What bounds it: the fixed operands come out of LDS for each tile
+// again, and the two waves wait for p and dS.
 // float32 heads are HELD, as their operands are twice as large, with 64 keys a block, as a batch may have few: 1,871 rows, 12 heads
-// of 80 over 4, both launches 565 us, 913 with one group of four waves for 128 keys.
+// of 80 over 4, both launches 565 us when this form came, 913 with one group of four waves for 128 keys; 242 now, in pieces.
+// Four of 2048, 40 heads of 128 over 8 in float32, the whole pass: 5407 us.
 template <class T, int DB, int WAVES, int GROUPS, int STAGES, int OCC, bool DIRECT, int PARTS, bool HELD>
 __global__ __launch_bounds__(64 * WAVES * GROUPS, OCC) void k_attention_dkv(Attention at, Heads doh, Heads qh, Heads kh, Heads vh,
                                                                           Heads dkh, Heads dvh, const float *delta, int tiles,
@@ -535,8 +539,11 @@ __global__ __launch_bounds__(256) void k_join_pieces(Attention at, Joins joins, 
 
 // As many pieces as make kPieceBlocks blocks, of four steps at least: where a batch has fewer blocks than the chip has room for, its
 // longest walk would be the time.  1,871 rows of nine sequences, 12 float32 heads of 80 over 4 (dq and dkv, with the join's 12 us):
-// 184 and 360 us whole, 111 and 159 for 512 blocks, 129 and 140 (join 17) for 1024.  Four sequences of 2048, 40 heads of 128
-// over 8 in bfloat16 make 512 blocks by keys, and two pieces of each would add 38 us of partial sums.
+// 184 and 360 us whole, 111 and 159 for 512 blocks, 129 and 140 (join 17) for 1024, before walks were dealt to the XCDs.  The whole
+// pass for 256 / 512 / 1024 blocks: that batch 380 / 244 / 276; bfloat16, one sequence of 4096, 8 heads of 128 over 2, 262 / 222 /
+// 231; 3000 rows, 12 of 96 over 4, 221 / 184 / 181; two of 2048, 12 of 64, 124 / 124 / 139; four of 512, 8 of 64 over 2, 47 / 49 /
+// 56; float32, one of 2048, 12 of 64, 423 / 408 / 346.  Four sequences of 2048, 40 heads of 128 over 8 in bfloat16 make 512 blocks
+// by keys, and two pieces of each would add 38 us of partial sums.
 constexpr int64_t kPieceBlocks = 512, kPieceRows = 128 * kPieceBlocks;
 int pieces_of(int64_t blocks, int64_t steps)
 {

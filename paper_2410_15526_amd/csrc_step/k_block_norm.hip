@@ -247,7 +247,9 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_block_norm(BlockNorm p, int
 // Rows part, part + parts, ... of a block, so that the chip's blocks walk through memory together; the next row's loads are under
 // way before the present one is stored.  The weight gradients of a block's rows go to the workspace, from where the sums over the
 // parts are taken in order.  8192 x 5120 bfloat16, both norms and a gate: 96 us and 6 for the sums over the parts (six arrays:
-// 5.2 TB/s); what is waited for is the row's one exchange of sums, with one or two blocks on a compute unit.  JOINT: the sums with the branch are wanted, for a post norm or the gate's gradient.
+// 5.2 TB/s); what is waited for is the row's one exchange of sums, with one or two blocks on a compute unit.  Rows of more than
+// 8192 columns do not fit the registers: 4096 x 8192 82 us, x 12288 196 (bfloat16) and 808 (float32), x 16384 754.
+// JOINT: the sums with the branch are wanted, for a post norm or the gate's gradient.
 template <class X, class Y, int C, bool WHOLE, bool JOINT>
 __global__ __launch_bounds__(64 * kMostWaves) void k_block_norm_grad(BlockNorm p, int64_t rows, int64_t cols, int64_t pitch, int parts,
                                                                      BlockNormGrad<X, Y> g)
