@@ -187,6 +187,17 @@ def test_attention_query_of_score_minus_infinity(dim, dtype):
     assert t.equal(*results)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 40, 80, 104, 200])
+def test_padded_heads_do_not_see_what_is_masked(dim, dtype):
+    """Heads that do not fill their columns: other sequences, later rows and rows in no sequence, holding NaN or infinities."""
+    from tests.test_gpu_layer import test_attention_does_not_see_what_is_masked
+    for value in (float("nan"), float("inf"), -float("inf")):
+        say("masked", dim, dtype, value)
+        test_attention_does_not_see_what_is_masked(dim, value, dtype)
+
+
+
 # ---------------------------------------------------------------------------
 # block norms of two types, of which one result is used
 # ---------------------------------------------------------------------------
