@@ -105,7 +105,7 @@ class Decoder:
         c, (rows, _, d) = self.cfg, q.shape
         # Kernels of float32 heads beyond 128 elements spill registers.  Milliseconds of a whole backward(), heads of 256, by the
         # operator and spelled out: 64 sequences of 512, 2 heads 8.3 and 8.6, 4 of 2048, 4 heads 8.1 and 8.2, 2 of 4096 12.5 and
-        # 12.5, one of 4096, 2 heads 6.3 and 3.9, one of 8192 15.9 and 11.2.
+        # 11.6, one of 4096, 2 heads 6.3 and 3.5, one of 8192 15.9 and 10.7.
         if sdp4.MIN_ATTENTION_DIM <= d <= (128 if c.seq > 2048 else sdp4.MAX_ATTENTION_DIM):
             return autograd.attention(q.float(), k.float(), v.float(), sequences).to(q.dtype)
         dtype = q.dtype
